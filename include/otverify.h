@@ -38,10 +38,11 @@ extern "C" {
 #define OT_OK                 0
 #define OT_ERR_NULL          -1   /* a required pointer is NULL                                              */
 #define OT_ERR_SHAPE         -2   /* a size is out of range, over capacity, or row offsets are not monotone  */
-#define OT_ERR_DTYPE         -3   /* dtype is neither OT_BF16 nor OT_F32                                     */
+#define OT_ERR_DTYPE         -3   /* a type that the call does not take                                      */
 #define OT_ERR_MAP           -4   /* direct map entry out of range, or two draft ids share a target id       */
 #define OT_ERR_NGRAM         -5   /* n-gram entry length or id out of range                                  */
-#define OT_ERR_CTX_MISMATCH  -6   /* the n-gram cache was built for another context                          */
+#define OT_ERR_CTX_MISMATCH  -6   /* the n-gram cache was built for another context; of ot_lm_head, ot_token_logprobs, their
+                                     gradients and ot_distill_loss_grad: another HIP device than the context's is current */
 #define OT_ERR_HIP           -7   /* a HIP call failed; ot_last_error() carries hipGetErrorString            */
 #define OT_ERR_NOMEM         -8   /* host or device allocation failed                                        */
 
@@ -55,6 +56,7 @@ extern "C" {
  * Nothing is refused for size.                                                                                */
 #define OT_BF16 0
 #define OT_F32  1
+#define OT_F16  2                 /* of a 4-bit head's scales only                                            */
 
 /* ---- per-sequence output flags ------------------------------------------------------------------------ */
 #define OT_FLAG_UNMAPPABLE 1      /* a drafted id had neither a cache hit nor a direct image: proposal cut   */
@@ -109,6 +111,30 @@ typedef struct ot_verify_config {
  * stream before returning.  *out is NULL on failure.                                                         */
 int  ot_verify_init(const ot_verify_config* cfg, ot_ctx** out);
 void ot_verify_destroy(ot_ctx* ctx);          /* synchronises the stream, frees everything; NULL is a no-op   */
+
+/* ---- a target head of 4-bit weights --------------------------------------------------------------------- */
+/* W[k][v] = scale[k / group][v] * (code[k][v] - zero[k / group][v]) with codes of 0..15: a quarter of the OT_BF16 weights'
+ * bytes, and up to 176 rows the weight stream is what bounds a step.  Codes times hidden states are exact, their sums over a
+ * group and the sums of scaled groups are fp32; the hidden states are not rounded, so the logits are those of the weights above
+ * to fp32 rounding.  A hidden row with an infinity or a NaN has NaN logits; hidden states are taken to stay below 2^100.   */
+typedef struct ot_quant_weights {
+  int32_t        group;        /* 32, 64 or 128: so many consecutive hidden indices share a scale and a zero point; d may end
+                                  inside a group                                                              */
+  int32_t        scale_dtype;  /* OT_BF16 or OT_F16                                                           */
+  const uint8_t* codes;        /* DEVICE [d / 2, V_t] row-major: byte (i, v) holds the codes of hidden indices 2 i (low four
+                                  bits) and 2 i + 1 of column v                                               */
+  const void*    scales;       /* DEVICE [ceil(d / group), V_t] row-major                                     */
+  const uint8_t* zeros;        /* DEVICE [ceil(d / group), V_t] zero points (the low four bits count), or NULL: 8 */
+} ot_quant_weights;
+/* ot_verify_init for such a head: cfg->W is not read, cfg->dtype has to be OT_BF16 (the type of hidden states and draft logits).
+ * The weights are read during init only and re-tiled into a private copy of d * V_t / 2 bytes and 4 bytes per scale.
+ * The context serves every entry point; its steps run in separate launches whatever cfg->draft_side asks for.     */
+int  ot_verify_init_quantized(const ot_verify_config* cfg, const ot_quant_weights* weights, ot_ctx** out);
+
+/* The logits alone: z = h . W of M hidden rows through the context's head of any type.  hidden: DEVICE [M, d] row-major,
+ * cfg.dtype (OT_BF16: from a multiple of 16 bytes on); logits: DEVICE fp32, row m at logits + m * ld, ld >= V_t; 0 <= M <= max_batch * (max_k + 1).  Nothing of the
+ * context's workspace is touched.                                                                              */
+int  ot_lm_head(ot_ctx* ctx, int32_t M, const void* hidden, float* logits, int64_t ld);
 
 /* ---- the n-gram cache ---------------------------------------------------------------------------------- */
 /* The cache C = {(t_i, [d_j]_{j=1:n})} (Section "Cross-vocabulary N-gram Cache") lives on the device as an
@@ -245,6 +271,58 @@ typedef struct ot_loss_out {
 } ot_loss_out;
 int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step_out, const float* target_logits_or_null,
                     const ot_loss_config* cfg, ot_loss_out* out);
+
+/* The values of ot_distill_loss (same arguments, same outputs), and the gradient of grad_loss * totals[4] with respect to the
+ * drafter's logits: grad, DEVICE [K, V_d] in cfg.dtype, written whole (zeros in the rows of draft tokens without a term).
+ * grad_loss: DEVICE, one float, or NULL for 1.  p, the weights lambda and the translation are constants; q' depends on the draft
+ * logits as Eq. 1 and Eq. 2 say, so with OT_NGRAM_TERM_APPROX_KL the logits of all of an n-gram's sub-tokens get a gradient.
+ * An id that the drafter's logits mask (-inf) gets zero.  Where a term is infinite (the target gives 0 to a token that the drafter
+ * proposes with q' > 0), its rows' gradients are not finite either.                                              */
+int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step_out, const float* target_logits_or_null,
+                         const ot_loss_config* cfg, ot_loss_out* out, const float* grad_loss_or_null, void* grad);
+
+/* ---- log-probabilities of given tokens, entropy, most likely alternatives ------------------------------------ */
+/* Of every row of logits, with p(v) = softmax(z / T)(v): ln p of the given tokens, the entropy -sum p ln p, and the n_top most
+ * likely ids with their ln p, by descending logit, of equal ones the lowest id first.  For the tokens that a step emitted: logits
+ * of ot_verify_workspace (or the caller's own), tokens = out_tokens, n_tok = 1, row_off and temperature of the step, given_rows_only.
+ *   - Ids masked with -inf have probability 0 and are no alternatives; places of top_ids that remain free hold -1 (top_logprobs -inf).
+ *   - A row without any logit above -inf has no distribution: logprob -inf, entropy 0, no alternatives, zero gradients.
+ *   - A row that holds a NaN or +inf: logprob and entropy NaN, no alternatives, NaN gradients.
+ *   - A temperature that is not above 0 (a greedy sequence) counts as 1, one below 2^-126 as that.
+ *   - A token of -1 is none: logprob 0, no gradient.  A token outside [-1, V): logprob NaN, no gradient.
+ *   - given_rows_only != 0: rows all of whose tokens are -1 are not read (entropy 0, no alternatives, zero gradients).
+ * Work is enqueued on the context's stream; calls on one context share its workspace.  The logits may be any on the context's
+ * device: of the target, the drafter or another model.                                                          */
+#define OT_MAX_TOP 64                 /* n_top at most                                                          */
+typedef struct ot_logprob_in {
+  int32_t        M, V;                /* rows; ids per row                                                      */
+  int32_t        dtype;               /* OT_BF16 or OT_F32: type of the logits                                  */
+  int32_t        n_tok, n_top;        /* given tokens per row (0: none); alternatives per row, 0..OT_MAX_TOP    */
+  int32_t        given_rows_only;
+  int32_t        B;                   /* sequences, with row_off                                                */
+  int32_t        reserved;            /* must be 0                                                              */
+  int64_t        ld;                  /* elements from a row of logits to the next, at least V                  */
+  const void*    logits;              /* DEVICE, row m at logits + m * ld elements, any alignment of its type   */
+  const int32_t* tokens;              /* DEVICE [M, n_tok]                                                      */
+  const float*   temperature;         /* DEVICE [M], or [B] with row_off, or NULL: 1                            */
+  const int32_t* row_off;             /* DEVICE [B+1] first rows of the sequences that the temperatures belong to, or NULL */
+} ot_logprob_in;
+/* DEVICE.  logprob [M, n_tok] is required with n_tok > 0, top_ids and top_logprobs [M, n_top] with n_top > 0; entropy [M] may be
+ * NULL.  row_max and row_sumexp [M] (the largest logit, NaNs aside; sum_v exp((z_v - row_max) / T)) are what the gradient needs; both or none. */
+typedef struct ot_logprob_out {
+  float   *logprob, *entropy, *row_max, *row_sumexp, *top_logprobs;
+  int32_t *top_ids;
+} ot_logprob_out;
+int ot_token_logprobs(ot_ctx* ctx, const ot_logprob_in* in, ot_logprob_out* out);
+
+/* Gradient of sum grad_logprob * logprob + sum grad_entropy * entropy with respect to the logits, in the logits' type:
+ *   dz_v = (1/T) [ sum over tokens of v of grad_logprob - p_v (sum of grad_logprob + grad_entropy (ln p_v + entropy)) ],
+ * and 0 for ids masked with -inf.
+ * `in` and `forward` are those of ot_token_logprobs, whose row_max, row_sumexp and (with grad_entropy) entropy are read.
+ * grad_logprob DEVICE [M, n_tok], grad_entropy DEVICE [M]: either may be NULL (zero).  grad: DEVICE, row m at grad + m * ld_grad
+ * elements, ld_grad >= V, written whole up to V; it may be the logits themselves (with the same ld).               */
+int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logprob_out* forward, const float* grad_logprob_or_null,
+                           const float* grad_entropy_or_null, void* grad, int64_t ld_grad);
 
 /* ---- adaptive drafting: stop rule and the acceptance head's loss value -------------------------------- */
 /* Section "Online Adaptive Drafting": a head f_phi gives, for proposed token i, the logit of

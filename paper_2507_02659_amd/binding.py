@@ -17,10 +17,11 @@ LIB_PATH = os.path.join(_PKG, "libotverify.so")
 OT_OK = 0
 OT_ERR_NULL, OT_ERR_SHAPE, OT_ERR_DTYPE, OT_ERR_MAP = -1, -2, -3, -4
 OT_ERR_NGRAM, OT_ERR_CTX_MISMATCH, OT_ERR_HIP, OT_ERR_NOMEM = -5, -6, -7, -8
-OT_BF16, OT_F32 = 0, 1
+OT_BF16, OT_F32, OT_F16 = 0, 1, 2
 OT_FLAG_UNMAPPABLE, OT_FLAG_RESID_ZERO, OT_FLAG_BAD_ID = 1, 2, 4
 OT_MAX_NGRAM_LEN, OT_MAX_K = 8, 63
 OT_STATIC_MAX_BATCH = 4096
+OT_MAX_TOP = 64
 OT_N_STAGES = 4
 STAGE_NAMES = ("lm_head", "softmax_stats", "translate_accept", "residual_draw")
 
@@ -31,9 +32,10 @@ OT_LAMBDA_FIXED, OT_LAMBDA_TARGET_PROB = 0, 1
 OT_NGRAM_TERM_NLL, OT_NGRAM_TERM_APPROX_KL = 0, 1
 
 EXPORTS = (
-    "ot_verify_init", "ot_verify_destroy", "ot_ngram_cache_build", "ot_ngram_cache_create", "ot_ngram_cache_insert",
+    "ot_verify_init", "ot_verify_init_quantized", "ot_verify_destroy", "ot_lm_head", "ot_ngram_cache_build", "ot_ngram_cache_create", "ot_ngram_cache_insert",
     "ot_ngram_cache_size", "ot_ngram_cache_export", "ot_ngram_cache_import", "ot_ngram_cache_destroy", "ot_verify_step",
-    "ot_verify_step_from_logits", "ot_distill_loss", "ot_adaptive_drafting", "ot_adaptive_drafting_static", "ot_verify_workspace", "ot_verify_structure",
+    "ot_verify_step_from_logits", "ot_distill_loss", "ot_distill_loss_grad", "ot_token_logprobs", "ot_token_logprobs_grad",
+    "ot_adaptive_drafting", "ot_adaptive_drafting_static", "ot_verify_workspace", "ot_verify_structure",
     "ot_verify_profile",
     "ot_verify_profile_read", "ot_last_error", "ot_version",
 )
@@ -52,6 +54,10 @@ class ot_verify_config(C.Structure):
         ("dtype", C.c_int32), ("max_ngram_len", C.c_int32), ("draft_side", C.c_int32),
         ("W", C.c_void_p), ("direct_map", C.c_void_p), ("stream", C.c_void_p),
     ]
+
+
+class ot_quant_weights(C.Structure):
+    _fields_ = [("group", C.c_int32), ("scale_dtype", C.c_int32), ("codes", C.c_void_p), ("scales", C.c_void_p), ("zeros", C.c_void_p)]
 
 
 class ot_step_in(C.Structure):
@@ -81,6 +87,19 @@ LOSS_OUT = ("kind", "kl", "nll", "weight", "totals", "qprime")
 
 class ot_loss_out(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in LOSS_OUT]
+
+
+class ot_logprob_in(C.Structure):
+    _fields_ = [("M", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("n_tok", C.c_int32), ("n_top", C.c_int32),
+                ("given_rows_only", C.c_int32), ("B", C.c_int32), ("reserved", C.c_int32), ("ld", C.c_int64),
+                ("logits", C.c_void_p), ("tokens", C.c_void_p), ("temperature", C.c_void_p), ("row_off", C.c_void_p)]
+
+
+LOGPROB_OUT = ("logprob", "entropy", "row_max", "row_sumexp", "top_logprobs", "top_ids")
+
+
+class ot_logprob_out(C.Structure):
+    _fields_ = [(n, C.c_void_p) for n in LOGPROB_OUT]
 
 
 class ot_adapt_in(C.Structure):
@@ -115,6 +134,10 @@ def load_library() -> C.CDLL:
     lib = C.CDLL(LIB_PATH)
     lib.ot_verify_init.argtypes = [C.POINTER(ot_verify_config), C.POINTER(C.c_void_p)]
     lib.ot_verify_init.restype = C.c_int
+    lib.ot_verify_init_quantized.argtypes = [C.POINTER(ot_verify_config), C.POINTER(ot_quant_weights), C.POINTER(C.c_void_p)]
+    lib.ot_verify_init_quantized.restype = C.c_int
+    lib.ot_lm_head.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_int64]
+    lib.ot_lm_head.restype = C.c_int
     lib.ot_verify_destroy.argtypes = [C.c_void_p]
     lib.ot_verify_destroy.restype = None
     lib.ot_ngram_cache_build.argtypes = [C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.POINTER(C.c_void_p)]
@@ -139,6 +162,13 @@ def load_library() -> C.CDLL:
     lib.ot_distill_loss.argtypes = [C.c_void_p, C.POINTER(ot_step_in), C.POINTER(ot_step_out), C.c_void_p,
                                     C.POINTER(ot_loss_config), C.POINTER(ot_loss_out)]
     lib.ot_distill_loss.restype = C.c_int
+    lib.ot_distill_loss_grad.argtypes = lib.ot_distill_loss.argtypes + [C.c_void_p, C.c_void_p]
+    lib.ot_distill_loss_grad.restype = C.c_int
+    lib.ot_token_logprobs.argtypes = [C.c_void_p, C.POINTER(ot_logprob_in), C.POINTER(ot_logprob_out)]
+    lib.ot_token_logprobs.restype = C.c_int
+    lib.ot_token_logprobs_grad.argtypes = [C.c_void_p, C.POINTER(ot_logprob_in), C.POINTER(ot_logprob_out), C.c_void_p, C.c_void_p,
+                                           C.c_void_p, C.c_int64]
+    lib.ot_token_logprobs_grad.restype = C.c_int
     lib.ot_adaptive_drafting.argtypes = [C.c_void_p, C.POINTER(ot_adapt_in), C.POINTER(ot_adapt_out)]
     lib.ot_adaptive_drafting.restype = C.c_int
     lib.ot_adaptive_drafting_static.argtypes = [C.POINTER(ot_adapt_in), C.POINTER(ot_adapt_out), C.c_void_p]
@@ -199,6 +229,22 @@ def ot_verify_init(*, d, V_t, V_d, max_batch, max_k, dtype, max_ngram_len, W, di
     ctx = C.c_void_p()
     _check(load_library().ot_verify_init(C.byref(cfg), C.byref(ctx)))
     return ctx
+
+
+def ot_verify_init_quantized(*, d, V_t, V_d, max_batch, max_k, max_ngram_len, codes, scales, zeros, group, scale_dtype, direct_map, stream=None,
+                             draft_side=0, dtype=OT_BF16):
+    """codes [d / 2, V_t], scales and (or None) zeros [ceil(d / group), V_t]: device tensors or addresses.  Returns the context handle."""
+    dm = None if direct_map is None else np.ascontiguousarray(direct_map, dtype=np.int32)
+    cfg = ot_verify_config(d, V_t, V_d, max_batch, max_k, dtype, max_ngram_len, int(draft_side), None, _ptr(dm), _ptr(stream))
+    w = ot_quant_weights(int(group), int(scale_dtype), _ptr(codes), _ptr(scales), _ptr(zeros))
+    ctx = C.c_void_p()
+    _check(load_library().ot_verify_init_quantized(C.byref(cfg), C.byref(w), C.byref(ctx)))
+    return ctx
+
+
+def ot_lm_head(ctx, M: int, hidden, logits, ld: int):
+    """logits: device tensor or address; rows may be ld elements apart (a tensor that is not contiguous: pass its address)."""
+    _check(load_library().ot_lm_head(ctx, M, _ptr(hidden), _ptr(logits), ld))
 
 
 def ot_verify_destroy(ctx):
@@ -292,6 +338,34 @@ def ot_distill_loss(ctx, step_in: ot_step_in, step_out: ot_step_out, target_logi
     out = ot_loss_out(*[_ptr(buffers.get(n)) for n in LOSS_OUT])
     _check(load_library().ot_distill_loss(ctx, C.byref(step_in), C.byref(step_out), _ptr(target_logits), C.byref(cfg),
                                           C.byref(out)))
+
+
+def ot_distill_loss_grad(ctx, step_in: ot_step_in, step_out: ot_step_out, target_logits, *, lam: float, lambda_mode: int,
+                         ngram_term: int, accepted_only: bool, buffers: dict, grad_loss, grad):
+    """ot_distill_loss and the gradient of grad_loss[0] * loss (None: of the loss) with respect to the draft logits, [K, V_d]."""
+    cfg = ot_loss_config(float(lam), int(lambda_mode), int(ngram_term), 1 if accepted_only else 0)
+    out = ot_loss_out(*[_ptr(buffers.get(n)) for n in LOSS_OUT])
+    _check(load_library().ot_distill_loss_grad(ctx, C.byref(step_in), C.byref(step_out), _ptr(target_logits), C.byref(cfg), C.byref(out),
+                                               _ptr(grad_loss), _ptr(grad)))
+
+
+def make_logprob_in(*, M, V, dtype, logits, ld, tokens, n_tok, n_top=0, temperature=None, row_off=None, B=0, given_rows_only=False,
+                    reserved=0) -> ot_logprob_in:
+    return ot_logprob_in(M, V, dtype, n_tok, n_top, 1 if given_rows_only else 0, B, reserved, ld, _ptr(logits), _ptr(tokens), _ptr(temperature),
+                         _ptr(row_off))
+
+
+def make_logprob_out(buffers: dict) -> ot_logprob_out:
+    """buffers: name -> device tensor/address for the fields of ot_logprob_out (those not wanted may be absent)."""
+    return ot_logprob_out(*[_ptr(buffers.get(n)) for n in LOGPROB_OUT])
+
+
+def ot_token_logprobs(ctx, given: ot_logprob_in, out: ot_logprob_out):
+    _check(load_library().ot_token_logprobs(ctx, C.byref(given), C.byref(out)))
+
+
+def ot_token_logprobs_grad(ctx, given: ot_logprob_in, forward: ot_logprob_out, grad_logprob, grad_entropy, grad, ld_grad: int):
+    _check(load_library().ot_token_logprobs_grad(ctx, C.byref(given), C.byref(forward), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(grad), ld_grad))
 
 
 def ot_adaptive_drafting(ctx, *, B, gamma, w_accept=1.0, w_reject=1.0, row_off, row_off_host, head_logits, labels=None,

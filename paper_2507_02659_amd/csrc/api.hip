@@ -31,6 +31,14 @@ int ot_fail(int code, const char* fmt, ...) {
 
 int ot_fail_hip(hipError_t e, const char* what) { return ot_fail(OT_ERR_HIP, "%s: %s", what, hipGetErrorString(e)); }
 
+int ot_check_device(const ot_ctx* ctx, const char* who) {
+  int device = -1;
+  const hipError_t e = hipGetDevice(&device);
+  if (e != hipSuccess) return ot_fail_hip(e, who);
+  if (device != ctx->device) return ot_fail(OT_ERR_CTX_MISMATCH, "%s: device %d is current, the context is on device %d", who, device, ctx->device);
+  return OT_OK;
+}
+
 #define fail ot_fail
 #define fail_hip ot_fail_hip
 
@@ -62,10 +70,10 @@ extern "C" {
 const char* ot_last_error(void) { return g_err; }
 const char* ot_version(void) { return "otverify 0.1 (gfx950)"; }
 
-int ot_verify_init(const ot_verify_config* cfg, ot_ctx** out) {
-  if (out) *out = nullptr;
+// qw: the 4-bit weights of a quantized head (already checked), or NULL: cfg->W.
+static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot_ctx** out) {
   if (!cfg || !out) return fail(OT_ERR_NULL, "ot_verify_init: cfg and out must not be NULL");
-  if (!cfg->W || !cfg->direct_map) return fail(OT_ERR_NULL, "ot_verify_init: W and direct_map must not be NULL");
+  if ((!qw && !cfg->W) || !cfg->direct_map) return fail(OT_ERR_NULL, "ot_verify_init: W and direct_map must not be NULL");
   if (cfg->dtype != OT_BF16 && cfg->dtype != OT_F32) return fail(OT_ERR_DTYPE, "ot_verify_init: unknown dtype %d", cfg->dtype);
   if (cfg->d <= 0 || cfg->V_t <= 0 || cfg->V_d <= 0) return fail(OT_ERR_SHAPE, "ot_verify_init: d, V_t, V_d must be positive");
   if (cfg->dtype == OT_BF16 && cfg->d % 8 != 0) return fail(OT_ERR_SHAPE, "ot_verify_init: bf16 needs d %% 8 == 0 (d = %d)", cfg->d);
@@ -129,7 +137,15 @@ int ot_verify_init(const ot_verify_config* cfg, ot_ctx** out) {
 
   const size_t R = (size_t)c->max_rows, KQ = (size_t)c->max_K, Bm = (size_t)c->max_batch;
   bool ok = true;
-  if (c->dtype == OT_BF16) ok = ok && dev_alloc(c, &c->Wp, (size_t)(c->Vp / 64) * (size_t)packed_tile_units(c->Kp / 32) * 8) && dev_alloc(c, &c->zeros, 32);
+  uint4* q_codes = nullptr;
+  uint32_t* q_recs = nullptr;
+  if (qw) {
+    c->quantized = true;
+    c->q.tiles = ceil_div(c->V_t, 16); c->q.blocks = ceil_div(c->d, 128); c->q.steps = qw->group / 32;
+    const size_t n = (size_t)c->q.tiles * c->q.blocks;
+    ok = ok && dev_alloc(c, &q_codes, n * 64) && dev_alloc(c, &q_recs, n * 16 * (4 / c->q.steps));
+    c->q.codes = q_codes; c->q.recs = q_recs;
+  } else if (c->dtype == OT_BF16) ok = ok && dev_alloc(c, &c->Wp, (size_t)(c->Vp / 64) * (size_t)packed_tile_units(c->Kp / 32) * 8) && dev_alloc(c, &c->zeros, 32);
   else ok = ok && dev_alloc(c, &c->Wf, (size_t)ceil_div(c->V_t, 64) * (size_t)packed_f32_tile_units(ceil_div(c->d, 16)) * 4);
   ok = ok && dev_alloc(c, &c->dmap, (size_t)c->V_d) && dev_alloc(c, &c->tmap, tmap_h.size());
   ok = ok && dev_alloc(c, &c->Z, R * (size_t)c->V_t);
@@ -162,7 +178,9 @@ int ot_verify_init(const ot_verify_config* cfg, ot_ctx** out) {
   c->n_pairs = (int32_t)n_pairs;
   c->local_pairs = 2 * n_near >= n_pairs;
   if (e == hipSuccess) {
-    if (c->dtype == OT_BF16)
+    if (qw)
+      e = launch_pack_quant(qw->codes, qw->scales, qw->scale_dtype == OT_F16, qw->zeros, qw->group, c->d, c->V_t, c->q, q_codes, q_recs, c->stream);
+    else if (c->dtype == OT_BF16)
       e = launch_pack_w_bf16(static_cast<const uint16_t*>(cfg->W), c->d, c->V_t, c->Wp, c->Kp, c->Vp, c->stream);
     else
       e = launch_pack_w_f32(static_cast<const float*>(cfg->W), c->d, c->V_t, c->Wf, c->stream);
@@ -171,6 +189,21 @@ int ot_verify_init(const ot_verify_config* cfg, ot_ctx** out) {
   if (e != hipSuccess) { free_ctx(c); return fail_hip(e, "ot_verify_init"); }
   *out = c;
   return OT_OK;
+}
+
+int ot_verify_init(const ot_verify_config* cfg, ot_ctx** out) {
+  if (out) *out = nullptr;
+  return init_impl(cfg, nullptr, out);
+}
+
+int ot_verify_init_quantized(const ot_verify_config* cfg, const ot_quant_weights* qw, ot_ctx** out) {
+  if (out) *out = nullptr;
+  if (!cfg || !qw) return fail(OT_ERR_NULL, "ot_verify_init_quantized: cfg and weights must not be NULL");
+  if (!qw->codes || !qw->scales) return fail(OT_ERR_NULL, "ot_verify_init_quantized: codes and scales must not be NULL");
+  if (qw->group != 32 && qw->group != 64 && qw->group != 128) return fail(OT_ERR_SHAPE, "ot_verify_init_quantized: group must be 32, 64 or 128 (%d)", qw->group);
+  if (qw->scale_dtype != OT_BF16 && qw->scale_dtype != OT_F16) return fail(OT_ERR_DTYPE, "ot_verify_init_quantized: scales are OT_BF16 or OT_F16 (%d)", qw->scale_dtype);
+  if (cfg->dtype != OT_BF16) return fail(OT_ERR_DTYPE, "ot_verify_init_quantized: cfg->dtype must be OT_BF16 (%d)", cfg->dtype);
+  return init_impl(cfg, qw, out);
 }
 
 void ot_verify_destroy(ot_ctx* ctx) {
@@ -188,7 +221,7 @@ static HeadPlan head_plan(const ot_ctx* ctx, int B, int M) {
   const int K = M - B, n_cu = ctx->n_cu;
   const bool bf16 = ctx->dtype == OT_BF16;
   HeadPlan p{kHostsNothing, 0, 0};
-  if (B > kFusedMaxB || K < 1 || ctx->draft_side == OT_DRAFT_SIDE_SEPARATE) return p;
+  if (ctx->quantized || B > kFusedMaxB || K < 1 || ctx->draft_side == OT_DRAFT_SIDE_SEPARATE) return p;
   if (ctx->draft_side == OT_DRAFT_SIDE_IN_LM_HEAD) p.hosted = kHostsAll;
   else if (bf16) p.hosted = lmhead_bf16_hosts(M, ctx->d, ctx->Vp, B, K, ctx->V_d, n_cu);
   else p.hosted = lmhead_f32_hosts_draft_side(M, ctx->d, ctx->V_t, B, K, ctx->V_d, n_cu) ? kHostsAll : kHostsNothing;
@@ -213,6 +246,8 @@ static int step_impl(ot_ctx* ctx, ot_ngram_cache* cache, const ot_step_in* in, c
   }
   const int M = in->row_off_host[in->B], K = M - in->B;
   if (from_logits ? !ext_logits : !in->hidden) return fail(OT_ERR_NULL, "ot_verify_step: %s must not be NULL", from_logits ? "target_logits" : "hidden");
+  if (ctx->quantized && !from_logits && reinterpret_cast<uintptr_t>(in->hidden) % 16)
+    return fail(OT_ERR_SHAPE, "ot_verify_step: a quantized head's hidden rows start at a multiple of 16 bytes");
   if (K > 0 && (!in->draft_logits || !in->draft_ids)) return fail(OT_ERR_NULL, "ot_verify_step: draft_logits and draft_ids must not be NULL");
   if (!o->n_mapped || !o->n_accept || !o->n_accept_draft || !o->n_emit || !o->hits_proposed || !o->hits_accepted ||
       !o->flags || !o->out_tokens || !o->mapped_ids || !o->span_start || !o->span_len || !o->p_tok || !o->q_tok || !o->ratio)
@@ -268,7 +303,9 @@ static int step_impl(ot_ctx* ctx, ot_ngram_cache* cache, const ot_step_in* in, c
       a.plan = make_piece_plan(plan.workers, K);
     }
     const StepArgs* draft_side = a.hosted == kHostsAll ? &a : nullptr;
-    if (ctx->dtype == OT_BF16)
+    if (ctx->quantized)
+      e = launch_qhead(static_cast<const uint16_t*>(in->hidden), M, ctx->d, ctx->q, ctx->Z, ctx->V_t, a.ldz, ctx->n_cu, st);
+    else if (ctx->dtype == OT_BF16)
       e = launch_lmhead_bf16(static_cast<const uint16_t*>(in->hidden), M, ctx->d, ctx->Wp, ctx->Kp, ctx->Vp, ctx->Z,
                              ctx->V_t, a.ldz, ctx->zeros, &a.fused, draft_side, ctx->n_cu, st);
     else
@@ -296,6 +333,26 @@ int ot_verify_step(ot_ctx* ctx, ot_ngram_cache* cache, const ot_step_in* in, ot_
 int ot_verify_step_from_logits(ot_ctx* ctx, ot_ngram_cache* cache, const ot_step_in* in,
                                const float* target_logits, ot_step_out* out) {
   return step_impl(ctx, cache, in, target_logits, true, out);
+}
+
+int ot_lm_head(ot_ctx* ctx, int32_t M, const void* hidden, float* logits, int64_t ld) {
+  if (!ctx) return fail(OT_ERR_NULL, "ot_lm_head: ctx must not be NULL");
+  if (M < 0 || M > ctx->max_rows) return fail(OT_ERR_SHAPE, "ot_lm_head: M = %d exceeds the context's %d rows", M, ctx->max_rows);
+  if (ld < ctx->V_t) return fail(OT_ERR_SHAPE, "ot_lm_head: ld = %lld is below V_t = %d", (long long)ld, ctx->V_t);
+  if (M == 0) return OT_OK;
+  if (!hidden || !logits) return fail(OT_ERR_NULL, "ot_lm_head: hidden and logits must not be NULL");
+  if (reinterpret_cast<uintptr_t>(hidden) % (ctx->dtype == OT_BF16 ? 16 : 4) || reinterpret_cast<uintptr_t>(logits) % 4)
+    return fail(OT_ERR_SHAPE, "ot_lm_head: hidden rows start at a multiple of 16 bytes (OT_F32: 4), logits of 4");
+  if (const int bad = ot_check_device(ctx, "ot_lm_head")) return bad;
+  hipError_t e;
+  if (ctx->quantized)
+    e = launch_qhead(static_cast<const uint16_t*>(hidden), M, ctx->d, ctx->q, logits, ctx->V_t, ld, ctx->n_cu, ctx->stream);
+  else if (ctx->dtype == OT_BF16)
+    e = launch_lmhead_bf16(static_cast<const uint16_t*>(hidden), M, ctx->d, ctx->Wp, ctx->Kp, ctx->Vp, logits, ctx->V_t, ld, ctx->zeros, nullptr,
+                           nullptr, ctx->n_cu, ctx->stream);
+  else
+    e = launch_lmhead_f32(static_cast<const float*>(hidden), M, ctx->d, ctx->Wf, logits, ctx->V_t, ld, nullptr, nullptr, ctx->n_cu, ctx->stream);
+  return e == hipSuccess ? OT_OK : fail_hip(e, "ot_lm_head: launch");
 }
 
 int ot_verify_workspace(ot_ctx* ctx, ot_workspace_view* v) {

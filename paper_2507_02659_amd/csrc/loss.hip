@@ -385,8 +385,8 @@ using namespace otv;
 #pragma GCC visibility push(default)
 extern "C" {
 
-int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
-                    const ot_loss_config* cfg, ot_loss_out* out) {
+static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
+                     const ot_loss_config* cfg, ot_loss_out* out) {
   if (!ctx || !in || !step || !cfg || !out) return ot_fail(OT_ERR_NULL, "ot_distill_loss: ctx, in, step_out, cfg and out must not be NULL");
   if (cfg->lambda_mode != OT_LAMBDA_FIXED && cfg->lambda_mode != OT_LAMBDA_TARGET_PROB)
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: unknown lambda_mode %d", cfg->lambda_mode);
@@ -443,6 +443,35 @@ int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, 
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return ot_fail_hip(e, "ot_distill_loss: launch");
   return OT_OK;
+}
+
+int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
+                    const ot_loss_config* cfg, ot_loss_out* out) {
+  return loss_impl(ctx, in, step, target_logits, cfg, out);
+}
+
+int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
+                         const ot_loss_config* cfg, ot_loss_out* out, const float* grad_loss, void* grad) {
+  if (ctx)
+    if (const int bad = ot_check_device(ctx, "ot_distill_loss_grad")) return bad;
+  if (in && in->B > 0 && in->row_off_host && in->row_off_host[in->B] > in->B && !grad)
+    return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
+  if (ctx && reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
+    return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad is not aligned to its type");
+  const int bad = loss_impl(ctx, in, step, target_logits, cfg, out);
+  if (bad != OT_OK || in->B == 0) return bad;
+  LossGradArgs a{};
+  a.B = in->B; a.K = in->row_off_host[in->B] - in->B; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
+  a.approx_kl = cfg->ngram_term == OT_NGRAM_TERM_APPROX_KL;
+  a.row_off = in->row_off; a.temperature = in->temperature; a.draft_temperature = in->draft_temperature;
+  a.draft_logits = in->draft_logits; a.draft_ids = in->draft_ids; a.dmap = ctx->dmap; a.tmap = ctx->tmap;
+  a.Z = target_logits ? target_logits : ctx->Z; a.ldz = ctx->V_t;
+  a.row_max = ctx->row_max; a.row_sum = ctx->row_sum; a.drow_max = ctx->drow_max; a.drow_sum = ctx->drow_sum;
+  a.n_mapped = step->n_mapped; a.mapped_ids = step->mapped_ids; a.span_start = step->span_start; a.span_len = step->span_len;
+  a.kind = out->kind; a.kl = out->kl; a.weight = out->weight; a.totals = out->totals;
+  a.grad_loss = grad_loss; a.grad = grad;
+  const hipError_t e = launch_loss_grad(a, ctx->stream);
+  return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_distill_loss_grad: launch");
 }
 
 }  // extern "C"

@@ -11,6 +11,8 @@ int ot_fail(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3))
 int ot_fail_hip(hipError_t e, const char* what);
 // Looks up, for the current device, the address of the static scratch array of ot_adaptive_drafting_static.
 int ot_static_scratch_prepare();
+// OT_OK if the context's device is the current one, else OT_ERR_CTX_MISMATCH with a message that names `who`.
+int ot_check_device(const struct ot_ctx* ctx, const char* who);
 
 struct ot_ctx {
   int32_t d = 0, V_t = 0, V_d = 0, max_batch = 0, max_k = 0, dtype = 0, max_ngram_len = 0, draft_side = 0;
@@ -21,6 +23,8 @@ struct ot_ctx {
   uint16_t* Wp = nullptr;
   uint16_t* zeros = nullptr;          // 64 zero bytes: source of the K tail in the LM-head's hidden slices
   float* Wf = nullptr;
+  bool quantized = false;             // the head is the 4-bit one below, and Wp and Wf are not there
+  otv::QuantHead q{};
   int32_t *dmap = nullptr, *tmap = nullptr;
   const int2* pairs = nullptr;        // [n_pairs] (target id, draft id) of the direct map in ascending target id, behind tmap
   int32_t n_pairs = 0;

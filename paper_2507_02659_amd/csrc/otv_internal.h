@@ -132,6 +132,15 @@ inline PiecePlan make_piece_plan(int workers, int K) {
   return p;
 }
 
+// A head of 4-bit weights in the order its kernels read it (qhead.hip): per tile of 16 columns and block of 128 hidden indices, the
+// codes as one uint4 per lane and the scales with their zero points as one word per column and group.
+struct QuantHead {
+  const uint4* codes;      // [tiles][blocks][64]
+  const uint32_t* recs;    // [tiles][blocks][16][4 / steps]
+  int32_t tiles, blocks;   // of 16 columns, of 128 hidden indices
+  int32_t steps;           // 32-deep steps that share a scale: 1, 2 or 4
+};
+
 // What of a step's statistics the LM-head launch takes.
 enum { kHostsNothing = OT_STRUCTURE_SEPARATE, kHostsAll = OT_STRUCTURE_HOSTED, kHostsPartials = OT_STRUCTURE_PARTIALS };
 
@@ -174,6 +183,27 @@ struct StepArgs {
   ot_step_out out;
 };
 
+// What the distillation loss's gradient reads and writes (loss_grad.hip): the step's inputs, statistics and translation, and the values
+// that the loss launch in front of it left.
+struct LossGradArgs {
+  int32_t B, K, V_t, V_d, dtype, approx_kl;
+  const int32_t* row_off;
+  const float* temperature;
+  const float* draft_temperature;
+  const void* draft_logits;
+  const int32_t* draft_ids;
+  const int32_t* dmap;
+  const int32_t* tmap;
+  const float* Z;
+  int64_t ldz;
+  const float* row_max; const double* row_sum;
+  const float* drow_max; const double* drow_sum;
+  const int32_t* n_mapped; const int32_t* mapped_ids; const int32_t* span_start; const int32_t* span_len;
+  const int32_t* kind; const double* kl; const double* weight; const double* totals;
+  const float* grad_loss;   // or nullptr: 1
+  void* grad;               // [K, V_d]
+};
+
 // ------------------------------------------------------------------------------------------------ launchers
 // Each returns the hipError_t of its launch.  All work goes to `stream`.
 hipError_t launch_pack_w_bf16(const uint16_t* W, int d, int V_t, uint16_t* Wp, int Kp, int Vp, hipStream_t stream);
@@ -198,6 +228,11 @@ hipError_t launch_lmhead_f32(const float* H, int M, int d, const float* Wp, floa
                              const FusedStats* fused, const StepArgs* draft_side, int n_cu, hipStream_t stream);
 int lmhead_f32_draft_workers(int M, int d, int V_t, int B, int K, int n_cu);
 bool lmhead_f32_hosts_draft_side(int M, int d, int V_t, int B, int K, int V_d, int n_cu);
+// Logits of M hidden rows through a 4-bit head (qhead.hip).
+hipError_t launch_qhead(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream);
+hipError_t launch_pack_quant(const uint8_t* codes, const void* scales, int scale_f16, const uint8_t* zeros, int group, int d, int V_t, const QuantHead& q,
+                             uint4* packed, uint32_t* recs, hipStream_t stream);
+hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream);
 hipError_t launch_softmax_stats(const StepArgs& a, hipStream_t stream);
 // translation, acceptance test and the draw of the final tokens
 hipError_t launch_final_draw(const StepArgs& a, const int32_t* row_off_host, int n_cu, hipStream_t stream);

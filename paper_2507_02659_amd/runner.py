@@ -6,6 +6,7 @@ verification path happens here; every stage runs in libotverify's kernels.
 from __future__ import annotations
 
 import ctypes as C
+from dataclasses import dataclass
 from typing import Optional
 
 import numpy as np
@@ -34,6 +35,25 @@ def read_device(ptr: int, count: int, np_dtype) -> np.ndarray:
     return out
 
 
+@dataclass
+class QuantWeights:
+    """A target head of 4-bit weights as device tensors: W[k, v] = scales[k // group, v] * (code[k, v] - zeros[k // group, v])."""
+
+    codes: torch.Tensor                             # uint8 [d / 2, V_t]: hidden index 2 i in the low four bits of row i, 2 i + 1 in the high ones
+    scales: torch.Tensor                            # bfloat16 or float16 [ceil(d / group), V_t]
+    zeros: Optional[torch.Tensor] = None            # uint8 [ceil(d / group), V_t], 0..15; None: 8
+    group: int = 128
+
+    def check(self):
+        (half, V_t), n = self.codes.shape, -(-2 * self.codes.shape[0] // self.group)
+        if self.codes.dtype != torch.uint8 or self.scales.dtype not in (torch.bfloat16, torch.float16):
+            raise TypeError("codes are uint8, scales bfloat16 or float16")
+        if tuple(self.scales.shape) != (n, V_t) or (self.zeros is not None and tuple(self.zeros.shape) != (n, V_t)):
+            raise ValueError(f"scales and zeros of {2 * half} x {V_t} weights in groups of {self.group} are [{n}, {V_t}]")
+        if self.zeros is not None and self.zeros.dtype != torch.uint8:
+            raise TypeError("zeros are uint8")
+
+
 class Verifier:
     """One library context plus (optionally) one n-gram cache, for batches of a fixed model shape."""
 
@@ -46,14 +66,22 @@ class Verifier:
         self.d, self.V_t, self.V_d = d, V_t, V_d
         self.stream = stream
         torch.cuda.set_device(self.device)
-        W_dev = W if isinstance(W, torch.Tensor) else _to_device(W, dtype, self.device)
-        assert tuple(W_dev.shape) == (d, V_t)
-        torch.cuda.synchronize(self.device)
-        self.ctx = ot.ot_verify_init(d=d, V_t=V_t, V_d=V_d, max_batch=max_batch, max_k=max_k,
-                                     dtype=ot.OT_BF16 if dtype == "bf16" else ot.OT_F32, max_ngram_len=max_ngram_len,
-                                     W=W_dev, direct_map=direct_map,
-                                     stream=None if stream is None else stream.cuda_stream, draft_side=draft_side)
-        del W_dev                                   # init keeps a private re-tiled copy
+        common = dict(d=d, V_t=V_t, V_d=V_d, max_batch=max_batch, max_k=max_k, max_ngram_len=max_ngram_len, direct_map=direct_map,
+                      dtype=ot.OT_BF16 if dtype == "bf16" else ot.OT_F32, stream=None if stream is None else stream.cuda_stream,
+                      draft_side=draft_side)
+        self.ctx = None
+        if isinstance(W, QuantWeights):
+            W.check()
+            assert tuple(W.codes.shape) == (d // 2, V_t)
+            torch.cuda.synchronize(self.device)
+            self.ctx = ot.ot_verify_init_quantized(codes=W.codes, scales=W.scales, zeros=W.zeros, group=W.group,
+                                                   scale_dtype=ot.OT_F16 if W.scales.dtype == torch.float16 else ot.OT_BF16, **common)
+        else:
+            W_dev = W if isinstance(W, torch.Tensor) else _to_device(W, dtype, self.device)
+            assert tuple(W_dev.shape) == (d, V_t)
+            torch.cuda.synchronize(self.device)
+            self.ctx = ot.ot_verify_init(W=W_dev, **common)
+            del W_dev                               # init keeps a private re-tiled copy
         self.cache = None
         self._keep = None
 
@@ -68,6 +96,12 @@ class Verifier:
         v = cls(d=case.d, V_t=case.V_t, V_d=case.V_d, dtype=case.dtype, W=W, direct_map=case.direct_map, **kw)
         v.set_cache(case.ngram_key_off, case.ngram_key_ids, case.ngram_target_ids)
         return v
+
+    @classmethod
+    def quantized(cls, weights: QuantWeights, **kw) -> "Verifier":
+        """A verifier whose target head has 4-bit weights; the other arguments are the constructor's."""
+        half, V_t = weights.codes.shape
+        return cls(d=2 * half, V_t=V_t, dtype="bf16", W=weights, **kw)
 
     def set_cache(self, key_off, key_ids, target_ids):
         if self.cache is not None:
@@ -133,17 +167,7 @@ class Verifier:
                      ngram_term: int = ot.OT_NGRAM_TERM_NLL, accepted_only: bool = False, with_qprime: bool = False,
                      sync: bool = True) -> Optional[dict]:
         """Enqueues ot_distill_loss after a step on `inp`; with sync, waits and returns its outputs as numpy arrays."""
-        dev = self.device
-        M = max(inp["M"], 1)
-        key = ("loss_buffers", M, with_qprime)
-        buf = inp.get(key)
-        if buf is None:
-            buf = {"kind": torch.full((M,), -7, dtype=torch.int32, device=dev),
-                   "totals": torch.full((5,), -7.0, dtype=torch.float64, device=dev)}
-            buf.update({n: torch.full((M,), -7.0, dtype=torch.float64, device=dev) for n in ("kl", "nll", "weight")})
-            if with_qprime:
-                buf["qprime"] = torch.full((M, self.V_t), -7.0, dtype=torch.float32, device=dev)
-            inp[key] = buf
+        buf = self._loss_buffers(inp, with_qprime)
         sin = ot.make_step_in(B=inp["B"], step=inp["step"], row_off=inp["row_off"], row_off_host=inp["row_off_host"],
                               hidden=inp["hidden"], draft_logits=inp["draft_logits"], draft_ids=inp["draft_ids"],
                               temperature=inp["temperature"], draft_temperature=inp["draft_temperature"],
@@ -158,6 +182,119 @@ class Verifier:
         res.update(loss_dm=float(totals[0]), loss_ngram=float(totals[1]), n_dm=int(totals[2]), n_ngram_tokens=int(totals[3]),
                    loss=float(totals[4]))
         return res
+
+    def _loss_buffers(self, inp: dict, with_qprime: bool) -> dict:
+        dev = self.device
+        M = max(inp["M"], 1)
+        key = ("loss_buffers", M, with_qprime)
+        buf = inp.get(key)
+        if buf is None:
+            buf = {"kind": torch.full((M,), -7, dtype=torch.int32, device=dev),
+                   "totals": torch.full((5,), -7.0, dtype=torch.float64, device=dev)}
+            buf.update({n: torch.full((M,), -7.0, dtype=torch.float64, device=dev) for n in ("kl", "nll", "weight")})
+            if with_qprime:
+                buf["qprime"] = torch.full((M, self.V_t), -7.0, dtype=torch.float32, device=dev)
+            inp[key] = buf
+        return buf
+
+    def distill_loss_grad(self, inp: dict, *, from_logits: bool = False, lam: float = 0.2, lambda_mode: int = ot.OT_LAMBDA_FIXED,
+                          ngram_term: int = ot.OT_NGRAM_TERM_NLL, accepted_only: bool = False, with_qprime: bool = False,
+                          grad_loss: Optional[torch.Tensor] = None) -> dict:
+        """Enqueues ot_distill_loss_grad after a step on `inp`.  Returns device tensors: "grad", the gradient of grad_loss * loss (a float32
+        tensor of one element; None: 1) with respect to the draft logits [K, V_d], and the loss's outputs (the same buffers every call)."""
+        buf = self._loss_buffers(inp, with_qprime)
+        if grad_loss is not None and (grad_loss.dtype != torch.float32 or grad_loss.numel() != 1):
+            raise ValueError("grad_loss is one float32")
+        grad = self._empty((inp["K"], self.V_d), inp["draft_logits"].dtype)
+        sin = ot.make_step_in(B=inp["B"], step=inp["step"], row_off=inp["row_off"], row_off_host=inp["row_off_host"],
+                              hidden=inp["hidden"], draft_logits=inp["draft_logits"], draft_ids=inp["draft_ids"],
+                              temperature=inp["temperature"], draft_temperature=inp["draft_temperature"],
+                              seq_id=inp["seq_id"], seed=inp["seed"])
+        ot.ot_distill_loss_grad(self.ctx, sin, ot.make_step_out(inp["out"]), inp["target_logits"] if from_logits else None, lam=lam,
+                                lambda_mode=lambda_mode, ngram_term=ngram_term, accepted_only=accepted_only, buffers=buf,
+                                grad_loss=grad_loss, grad=grad)
+        return dict(buf, grad=grad)
+
+    # ------------------------------------------------------------------ logits and log-probabilities
+    def _empty(self, shape, dtype) -> torch.Tensor:
+        """Memory for outputs that work on the verifier's stream writes."""
+        if self.stream is None:
+            return torch.empty(shape, dtype=dtype, device=self.device)
+        with torch.cuda.stream(self.stream):
+            return torch.empty(shape, dtype=dtype, device=self.device)
+
+    def lm_head(self, hidden: torch.Tensor) -> torch.Tensor:
+        """Logits [M, V_t] (float32) of hidden rows [M, d] through the verifier's head (ot_lm_head)."""
+        if hidden.dtype != (torch.bfloat16 if self.dtype == "bf16" else torch.float32) or hidden.dim() != 2 or hidden.shape[1] != self.d:
+            raise ValueError(f"hidden rows are [M, {self.d}] of the verifier's type, not {tuple(hidden.shape)} {hidden.dtype}")
+        M = hidden.shape[0]
+        logits = self._empty((M, self.V_t), torch.float32)
+        ot.ot_lm_head(self.ctx, M, hidden, logits, self.V_t)
+        return logits
+
+    @staticmethod
+    def _logprob_in(logits, tokens, temperature, row_off, n_top, given_rows_only):
+        M, V = logits.shape
+        if logits.dtype not in (torch.bfloat16, torch.float32) or (V > 1 and logits.stride(1) != 1):
+            raise ValueError("logits are [M, V] bfloat16 or float32 with neighbouring ids next to each other")
+        n_tok = 0
+        if tokens is not None:
+            if tokens.dtype != torch.int32 or tokens.shape[0] != M or tokens.dim() > 2:
+                raise ValueError(f"tokens are int32 [{M}] or [{M}, n]")
+            n_tok = 1 if tokens.dim() == 1 else tokens.shape[1]
+        B = M if row_off is None else row_off.numel() - 1
+        if temperature is not None and (temperature.dtype != torch.float32 or temperature.numel() != B):
+            raise ValueError(f"temperatures are {B} float32")
+        if row_off is not None and row_off.dtype != torch.int32:
+            raise ValueError("row_off is int32")
+        # rows may lie further apart than V, and overlap nothing: one row alone may have any stride
+        return ot.make_logprob_in(M=M, V=V, dtype=ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, logits=logits.data_ptr(),
+                                  ld=logits.stride(0) if M > 1 else V, tokens=tokens, n_tok=n_tok, n_top=n_top, temperature=temperature,
+                                  row_off=row_off, B=B, given_rows_only=given_rows_only)
+
+    def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, temperature: Optional[torch.Tensor] = None,
+                       row_off: Optional[torch.Tensor] = None, n_top: int = 0, given_rows_only: bool = False) -> dict:
+        """Log-probabilities of the given tokens (int32 [M] or [M, n], -1: none), entropy and the n_top most likely ids of every row of logits
+        [M, V] (ot_token_logprobs).  Returns device tensors: logprob (shaped like tokens), entropy, row_max, row_sumexp and, with n_top,
+        top_ids and top_logprobs.  temperature: one per row, or per sequence of row_off."""
+        given = self._logprob_in(logits, tokens, temperature, row_off, n_top, given_rows_only)
+        return self._token_logprobs(given, tokens)
+
+    def _token_logprobs(self, given, tokens) -> dict:
+        M, n_top = given.M, given.n_top
+        rows = self._empty((3, M), torch.float32)
+        out = {"entropy": rows[0], "row_max": rows[1], "row_sumexp": rows[2]}
+        if tokens is not None:
+            out["logprob"] = self._empty(tokens.shape, torch.float32)
+        if n_top:
+            out["top_ids"] = self._empty((M, n_top), torch.int32)
+            out["top_logprobs"] = self._empty((M, n_top), torch.float32)
+        ot.ot_token_logprobs(self.ctx, given, ot.make_logprob_out(out))
+        return out
+
+    def token_logprobs_grad(self, logits: torch.Tensor, tokens: Optional[torch.Tensor], forward: dict, *, grad_logprob: Optional[torch.Tensor] = None,
+                            grad_entropy: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
+                            row_off: Optional[torch.Tensor] = None, given_rows_only: bool = False) -> torch.Tensor:
+        """Gradient of sum grad_logprob * logprob + sum grad_entropy * entropy with respect to the logits, in their type
+        (ot_token_logprobs_grad).  forward: what token_logprobs returned for the same arguments."""
+        given = self._logprob_in(logits, tokens, temperature, row_off, 0, given_rows_only)
+        for name, g, shape in (("grad_logprob", grad_logprob, None if tokens is None else tokens.shape), ("grad_entropy", grad_entropy, logits.shape[:1])):
+            if g is not None and (g.dtype != torch.float32 or g.shape != shape):
+                raise ValueError(f"{name} is float32 {shape}")
+        grad = self._empty(logits.shape, logits.dtype)
+        ot.ot_token_logprobs_grad(self.ctx, given, ot.make_logprob_out(forward), grad_logprob, grad_entropy, grad, logits.shape[1])
+        return grad
+
+    def step_logprobs(self, inp: dict, *, from_logits: bool = False, n_top: int = 0, at_temperature: bool = True) -> dict:
+        """Log-probabilities of the tokens that the last step on `inp` emitted, with entropy and alternatives, from the logits it left
+        (from_logits: those it was given).  Rows without an emitted token hold 0, no alternatives.  at_temperature: under the step's
+        temperatures (greedy sequences at 1), else at 1."""
+        M, tokens = inp["M"], inp["out"]["out_tokens"]
+        w = ot.ot_verify_workspace(self.ctx)
+        given = ot.make_logprob_in(M=M, V=self.V_t, dtype=ot.OT_F32, logits=inp["target_logits"] if from_logits else w.logits, ld=self.V_t if from_logits else w.ld_logits,
+                                   tokens=tokens, n_tok=1, n_top=n_top, temperature=inp["temperature"] if at_temperature else None,
+                                   row_off=inp["row_off"] if at_temperature else None, B=inp["B"], given_rows_only=True)
+        return self._token_logprobs(given, tokens[:M])
 
     def synchronize(self):
         if self.stream is not None:

@@ -1,0 +1,330 @@
+"""Token log-probabilities, entropy and alternatives, and their gradient, against oracle/logprobs.py."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import logprobs as ol
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+
+
+@pytest.fixture(scope="module")
+def v():
+    from paper_2507_02659_amd.runner import Verifier
+    ver = Verifier(d=8, V_t=16, V_d=1, dtype="bf16", W=torch.zeros(8, 16, dtype=torch.bfloat16, device=DEV), direct_map=np.zeros(1, np.int32),
+                   max_batch=1, max_k=0)
+    yield ver
+    ver.close()
+
+
+def _tolerances(want, T):
+    """Per row, absolute, on ln S and on the entropy, derived from the row's own distribution.  An exponential's base-2 argument t takes three
+    roundings of 2^-24 |t|, the instruction and the sums in front of 64 bits six more half-steps: e is off by at most (3 |t| + 6) 2^-24, S by the
+    mean of that, E = sum e |t| by the mean of |t| times as much and one step more.  The results are rounded to float32 once."""
+    lp = want["lp"]
+    with np.errstate(invalid="ignore"):
+        t = np.where(lp > -np.inf, np.abs(lp - lp.max(1, keepdims=True)) / np.log(2), 0.0)
+        p = np.where(lp > -np.inf, np.exp(lp), 0.0)
+    each = (3 * t + 6) * 2.0 ** -24
+    tol_S = (p * each).sum(1) + 2.0 ** -24
+    tol_H = tol_S + (p * t * (each + 2.0 ** -23)).sum(1) * np.log(2) + (p * t).sum(1) * tol_S
+    return tol_S, tol_H, p, t
+
+
+def _near(got, want, tol):
+    got, want = np.asarray(got, np.float64), np.asarray(want, np.float64)
+    assert got.shape == want.shape
+    np.testing.assert_array_equal(np.isnan(got), np.isnan(want))
+    fine = np.isfinite(want) & (np.abs(want) < 3e38)
+    np.testing.assert_array_equal(np.where(fine | np.isnan(want), 0, got), np.where(fine | np.isnan(want), 0, np.float32(want)))
+    off = np.abs(got - want)[fine] - (np.broadcast_to(tol, want.shape) + 2.0 ** -24 * np.abs(want))[fine]
+    assert off.size == 0 or off.max() <= 0, off.max()
+
+
+def _check(v, z, tokens=None, T=None, n_top=0, given=False, grads=True, row_off=None, temps=None, seed=0):
+    """z: a device tensor [M, V].  T: per-row temperatures of the oracle; temps and row_off: how the call gets them."""
+    M, V = z.shape
+    Z = z.double().cpu().numpy()
+    T_rows = np.ones(M) if T is None else np.asarray(T, np.float64)
+    if T is not None and temps is None:
+        temps = torch.from_numpy(np.asarray(T, np.float32)).to(DEV)
+        T_rows = temps.double().cpu().numpy()
+    tok = None if tokens is None else torch.from_numpy(np.asarray(tokens, np.int32)).to(DEV)
+    print(f"logprobs M={M} V={V} {z.dtype} stride={z.stride()} at {z.data_ptr() % 16} n_top={n_top} tokens={None if tok is None else tuple(tok.shape)}", flush=True)
+    got = v.token_logprobs(z, tok, temperature=temps, row_off=row_off, n_top=n_top, given_rows_only=given)
+    host = {n: t.cpu().numpy() for n, t in got.items()}
+    want = ol.token_logprobs(Z, tokens, T_rows, n_top, given)
+    tol_S, tol_H, p, t = _tolerances(want, T_rows)
+    np.testing.assert_array_equal(host["row_max"], want["row_max"].astype(np.float32))
+    _near(host["row_sumexp"], want["row_sumexp"], np.where(want["row_sumexp"] > 0, want["row_sumexp"], 1) * tol_S)
+    _near(host["entropy"], want["entropy"], tol_H)
+    if tokens is not None:
+        _near(host["logprob"].reshape(M, -1), want["logprob"], tol_S[:, None])
+    if n_top:
+        np.testing.assert_array_equal(host["top_ids"], want["top_ids"])
+        _near(host["top_logprobs"], want["top_logprobs"], tol_S[:, None])
+    if not grads:
+        return got
+    rng = np.random.default_rng(seed)
+    g = None if tokens is None else rng.standard_normal(np.asarray(tokens).shape).astype(np.float32)
+    gH = rng.standard_normal(M).astype(np.float32)
+    put = lambda a: None if a is None else torch.from_numpy(a).to(DEV)  # noqa: E731
+    for g_use, gH_use in ((g, gH), (g, None), (None, gH)):
+        if g_use is None and gH_use is None:
+            continue
+        dz = v.token_logprobs_grad(z, tok, got, grad_logprob=put(g_use), grad_entropy=put(gH_use), temperature=temps, row_off=row_off, given_rows_only=given)
+        assert dz.dtype == z.dtype and dz.shape == z.shape
+        ref = ol.token_logprobs_grad(Z, tokens, T_rows, g_use, gH_use, given)
+        Tm = np.where(T_rows > 0, np.maximum(T_rows, 2.0 ** -126), 1.0)[:, None]
+        with np.errstate(invalid="ignore"):
+            lp, H = np.where(want["lp"] > -np.inf, want["lp"], 0.0), want["entropy"][:, None]
+            G = np.zeros((M, 1)) if g_use is None else np.abs(g_use.reshape(M, -1)).sum(1, keepdims=True)
+            h = np.zeros((M, 1)) if gH_use is None else np.abs(gH_use[:, None]).astype(np.float64)
+            # p as above and the two statistics' roundings; the sums of G and of ln p + entropy; four roundings of the result
+            u = G + h * np.abs(lp + H)
+            tol = p / Tm * (u * ((3 * t + 12) * 2.0 ** -24 + tol_S[:, None]) + G * (np.asarray(tok.shape)[-1] if g_use is not None else 0) * 2.0 ** -24
+                            + h * (tol_S + tol_H)[:, None] + h * (np.abs(lp) + H + t) * 2.0 ** -22)
+            tol = tol + 4 * 2.0 ** -24 * (np.abs(ref) + (p / Tm) * u) + 1e-37
+            # an element that tokens name is a sum of -p u and their g, which may cancel: every addition rounds by at most 2^-24 of the
+            # partial sum, itself at most p u + sum |g|
+            if g_use is not None:
+                at = np.zeros_like(ref)
+                for i, row in enumerate(np.asarray(tokens).reshape(M, -1)):
+                    ok = (row >= 0) & (row < V)
+                    np.add.at(at[i], row[ok], np.abs(g_use.reshape(M, -1)[i][ok]))
+                tol = tol + np.where(at > 0, (tok.numel() // M + 1) * 2.0 ** -24 * (at + p * u) / Tm, 0.0)
+            # the instruction flushes exponentials below 2^-126: p is off by as much at most, whatever 1 / T makes of it
+            tol = tol + 2.0 ** -126 * (u + h) / Tm
+            if z.dtype == torch.bfloat16:
+                tol = tol * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(ref)
+        out = dz.double().cpu().numpy()
+        np.testing.assert_array_equal(np.isnan(out), np.isnan(ref))
+        off = np.where(np.isnan(ref), 0, np.abs(out - ref) - tol)
+        assert off.max() <= 0, (off.max(), np.unravel_index(off.argmax(), off.shape))
+    return got
+
+
+def _logits(rng, M, V, dtype=torch.float32, sigma=2.0):
+    return torch.from_numpy((sigma * rng.standard_normal((M, V))).astype(np.float32)).to(dtype).to(DEV)
+
+
+@pytest.mark.parametrize("V", [1, 2, 3, 5, 63, 64, 65, 127, 255, 257, 1000, 1023, 4097, 8191, 8193, 16384, 20001, 40003, 130001])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_lengths(v, V, dtype):
+    rng = np.random.default_rng(V)
+    M = 3 if V > 5000 else 7
+    _check(v, _logits(rng, M, V, dtype), rng.integers(0, V, M), 0.3 + rng.random(M), n_top=min(20, 64))
+
+
+@pytest.mark.parametrize("M,V", [(1, 32000), (2, 300), (64, 1000), (257, 700), (600, 513), (2000, 100), (5000, 3)])
+def test_numbers_of_rows(v, M, V):
+    rng = np.random.default_rng(M)
+    _check(v, _logits(rng, M, V, torch.bfloat16 if M % 2 else torch.float32), rng.integers(0, V, (M, 2)), 0.5 + rng.random(M), n_top=5)
+
+
+@pytest.mark.parametrize("n_top", [0, 1, 2, 31, 32, 33, 63, 64])
+def test_alternatives(v, n_top):
+    """More alternatives than ids; ties everywhere; ascending and descending rows, whose every logit is a new best."""
+    rng = np.random.default_rng(n_top)
+    for V in (1, 40, 64, 5000):
+        _check(v, _logits(rng, 2, V), rng.integers(0, V, 2), n_top=n_top, grads=False)
+        _check(v, torch.from_numpy(rng.integers(-3, 3, (3, V)).astype(np.float32)).to(DEV), n_top=n_top, grads=False)
+    up = torch.linspace(-20, 20, 30011, device=DEV).repeat(3, 1)
+    up[1] = up[1].flip(0)
+    up[2] = 1.5
+    _check(v, up, n_top=n_top, grads=False)
+    _check(v, up.bfloat16(), n_top=n_top, grads=False)
+    signed = torch.zeros(2, 3000, device=DEV)
+    signed[:, ::3] = -0.0                                 # equal to 0: the lowest id wins whatever its sign
+    _check(v, signed, n_top=n_top, grads=False)
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+@pytest.mark.parametrize("V", [50, 9000, 40003])
+def test_masks(v, V, dtype):
+    rng = np.random.default_rng(V)
+    z = _logits(rng, 12, V, dtype)
+    low = torch.finfo(dtype).min
+    z[0] = -float("inf")                                  # nothing is left
+    z[1, 1:] = -float("inf")                              # one id is
+    z[2, :-1] = -float("inf")
+    z[3, torch.from_numpy(rng.random(V) < 0.9).to(DEV)] = -float("inf")
+    z[4] = low                                            # all at the type's lowest value: uniform
+    z[5, torch.from_numpy(rng.random(V) < 0.9).to(DEV)] = low
+    z[6, V // 2] = float("nan")
+    z[7, V - 1] = float("inf")
+    z[8] = float("nan")
+    z[9] = -float("inf")
+    z[9, 7] = float("nan")
+    z[10] = 1e30
+    z[11, :V // 2] = -float("inf")
+    z[11, 0] = -1e30
+    tokens = rng.integers(0, V, (12, 3))
+    tokens[:, 1] = [0, 0, V - 1, 3, 5, 6, V // 2, V - 1, 1, 7, 2, 0]
+    for T in (None, np.full(12, 0.01), np.full(12, 1e-42), np.full(12, 100.0), [0.0, -1.0, 1.0, 0.5] * 3):
+        _check(v, z, tokens, T, n_top=20)
+
+
+def test_tokens(v):
+    """None, out of range, the same one twice, hundreds in one row."""
+    rng = np.random.default_rng(2)
+    z = _logits(rng, 6, 777)
+    _check(v, z, np.array([[-1, 3], [3, 3], [776, 777], [-2, 0], [2 ** 31 - 1, 5], [-1, -1]]), n_top=3)
+    _check(v, z, np.array([[-1, 3], [3, 3], [776, 777], [-2, 0], [2 ** 31 - 1, 5], [-1, -1]]), n_top=3, given=True)
+    _check(v, z, np.array([-1, 3, -1, 5, 776, -1]), given=True)
+    _check(v, z, rng.integers(-1, 777, (6, 400)), np.full(6, 0.5))
+    _check(v, z, None, n_top=4)
+    _check(v, z.bfloat16(), np.full((6, 300), 11))
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_strides_and_alignment(v, dtype):
+    """Rows apart from each other, from any element on, also where every row starts at another alignment."""
+    rng = np.random.default_rng(9)
+    for V, ld, at in ((1003, 1003, 1), (1003, 1003, 3), (1000, 1024, 5), (8192, 8200, 7), (8200, 8201, 0), (17, 40, 2)):
+        flat = _logits(rng, 1, at + 5 * ld + 16, dtype)[0]
+        flat[:at] = float("nan")                          # what lies around the rows is not theirs
+        z = flat[at:at + 5 * ld].view(5, ld)[:, :V]
+        z.as_strided((5, ld - V), (ld, 1), at + V).fill_(float("nan")) if ld > V else None
+        _check(v, z, rng.integers(0, V, 5), n_top=7)
+    _check(v, _logits(rng, 9, 515, dtype)[::2], rng.integers(0, 515, 5), n_top=7)
+    _check(v, _logits(rng, 9, 515, dtype)[3:4, 5:], [2], n_top=7)
+
+
+def test_gradient_in_place_and_around(v):
+    from paper_2507_02659_amd import binding as ot
+    rng = np.random.default_rng(3)
+    for dtype in (torch.float32, torch.bfloat16):
+        z = _logits(rng, 4, 1003, dtype)
+        tok = torch.from_numpy(rng.integers(0, 1003, 4).astype(np.int32)).to(DEV)
+        g = torch.ones(4, device=DEV)
+        fwd = v.token_logprobs(z, tok)
+        want = v.token_logprobs_grad(z, tok, fwd, grad_logprob=g)
+        code = ot.OT_F32 if dtype == torch.float32 else ot.OT_BF16
+        given = ot.make_logprob_in(M=4, V=1003, dtype=code, logits=z, ld=1003, tokens=tok, n_tok=1)
+        wide = torch.full((5, 1031), -7.0, dtype=dtype, device=DEV)
+        ot.ot_token_logprobs_grad(v.ctx, given, ot.make_logprob_out(fwd), g, None, wide, 1031)
+        assert torch.equal(wide[:4, :1003], want) and (wide[:, 1003:] == -7).all() and (wide[4] == -7).all()
+        ot.ot_token_logprobs_grad(v.ctx, given, ot.make_logprob_out(fwd), g, None, z, 1003)
+        assert torch.equal(z, want)
+
+
+def test_rows_behind_the_last_stay_as_they_were(v):
+    from paper_2507_02659_amd import binding as ot
+    z = _logits(np.random.default_rng(1), 3, 100)
+    out = {n: torch.full((5, 2) if n in ("top_logprobs", "logprob") else (5,), -7.0, device=DEV) for n in ot.LOGPROB_OUT[:-1]}
+    out["top_ids"] = torch.full((5, 2), -7, dtype=torch.int32, device=DEV)
+    tok = torch.zeros(3, 2, dtype=torch.int32, device=DEV)
+    ot.ot_token_logprobs(v.ctx, ot.make_logprob_in(M=3, V=100, dtype=ot.OT_F32, logits=z, ld=100, tokens=tok, n_tok=2, n_top=2), ot.make_logprob_out(out))
+    for n, x in out.items():
+        assert (x[3:] == -7).all() and (x[:3] != -7).all(), n
+    # no output but the alternatives; no rows at all
+    few = {"top_ids": out["top_ids"], "top_logprobs": out["top_logprobs"]}
+    ot.ot_token_logprobs(v.ctx, ot.make_logprob_in(M=3, V=100, dtype=ot.OT_F32, logits=z, ld=100, tokens=None, n_tok=0, n_top=2), ot.make_logprob_out(few))
+    ot.ot_token_logprobs(v.ctx, ot.make_logprob_in(M=0, V=100, dtype=ot.OT_F32, logits=None, ld=100, tokens=None, n_tok=0, n_top=2), ot.make_logprob_out({}))
+
+
+def test_temperatures_by_sequence(v):
+    rng = np.random.default_rng(5)
+    row_off = np.array([0, 3, 4, 9, 10], np.int32)
+    T = np.array([1.0, 0.0, 0.4, 2.0], np.float32)
+    _check(v, _logits(rng, 10, 900), rng.integers(0, 900, 10), np.repeat(T, np.diff(row_off)), n_top=3, row_off=torch.from_numpy(row_off).to(DEV),
+           temps=torch.from_numpy(T).to(DEV))
+
+
+def test_offsets_past_32_bits(v):
+    """Rows whose elements lie past 2^31 of the first."""
+    M, V, ld = 5, 1500, 600_000_000
+    flat = torch.zeros((M - 1) * ld + V, dtype=torch.bfloat16, device=DEV)
+    z = flat.as_strided((M, V), (ld, 1))
+    rng = np.random.default_rng(0)
+    z.copy_(_logits(rng, M, V, torch.bfloat16))
+    _check(v, z, rng.integers(0, V, M), n_top=5)
+
+
+def test_gradient_of_a_vast_tensor(v):
+    """More than 2^31 elements in a contiguous gradient: its last rows."""
+    M, V = 17000, 131072
+    z = torch.zeros(M, V, dtype=torch.bfloat16, device=DEV)
+    rng = np.random.default_rng(0)
+    z[-2:] = _logits(rng, 2, V, torch.bfloat16)
+    tok = torch.full((M,), 5, dtype=torch.int32, device=DEV)
+    got = v.token_logprobs(z, tok, n_top=3)
+    dz = v.token_logprobs_grad(z, tok, got, grad_logprob=torch.ones(M, device=DEV))
+    want = ol.token_logprobs(z[-2:].double().cpu().numpy(), [5, 5], [1.0, 1.0], 3)
+    assert np.array_equal(got["top_ids"][-2:].cpu().numpy(), want["top_ids"])
+    np.testing.assert_allclose(got["logprob"][-2:].cpu().numpy(), want["logprob"][:, 0], rtol=1e-6)
+    ref = ol.token_logprobs_grad(z[-2:].double().cpu().numpy(), [5, 5], [1.0, 1.0], [1.0, 1.0])
+    np.testing.assert_allclose(dz[-2:].double().cpu().numpy(), ref, rtol=2.0 ** -8 + 1e-5, atol=1e-30)
+
+
+def test_same_results_every_time_and_from_graphs():
+    """Two captured graphs that share the context's workspace, replayed in turn with eager calls between them."""
+    from paper_2507_02659_amd.runner import Verifier
+    rng = np.random.default_rng(6)
+    stream = torch.cuda.Stream()
+    ver = Verifier(d=8, V_t=16, V_d=1, dtype="bf16", W=torch.zeros(8, 16, dtype=torch.bfloat16, device=DEV), direct_map=np.zeros(1, np.int32),
+                   max_batch=1, max_k=0, stream=stream)
+    with torch.cuda.stream(stream):
+        def call(z, tok, n_top):
+            got = ver.token_logprobs(z, tok, n_top=n_top)
+            return dict(got, grad=ver.token_logprobs_grad(z, tok, got, grad_logprob=ones[:z.shape[0]], grad_entropy=ones[:z.shape[0]]))
+        ones = torch.ones(40, device=DEV)
+        made = []
+        for M, V, n_top in ((1, 50001, 20), (40, 9000, 64)):
+            inputs = [(_logits(rng, M, V), torch.from_numpy(rng.integers(0, V, M).astype(np.int32)).to(DEV)) for _ in range(3)]
+            eager = [{n: x.clone() for n, x in call(z, t, n_top).items()} for z, t in inputs]
+            z, t = (x.clone() for x in inputs[0])
+            stream.synchronize()
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph, stream=stream):
+                out = call(z, t, n_top)
+            made.append((inputs, eager, z, t, graph, out, n_top))
+        for turn in range(3):
+            for inputs, eager, z, t, graph, out, n_top in made:
+                z.copy_(inputs[turn][0])
+                t.copy_(inputs[turn][1])
+                graph.replay()
+                again = call(*inputs[turn], n_top)
+                stream.synchronize()
+                for n, want in eager[turn].items():
+                    assert torch.equal(out[n], want) and torch.equal(again[n], want), n
+    ver.close()
+
+
+def test_refusals(v):
+    from paper_2507_02659_amd import binding as ot
+    z, tok = torch.zeros(4, 100, device=DEV), torch.zeros(4, dtype=torch.int32, device=DEV)
+    lp = torch.zeros(4, device=DEV)
+    base = dict(M=4, V=100, dtype=ot.OT_F32, logits=z, ld=100, tokens=tok, n_tok=1)
+
+    def code(out=None, **kw):
+        with pytest.raises(ot.OtError) as e:
+            ot.ot_token_logprobs(v.ctx, ot.make_logprob_in(**dict(base, **kw)), ot.make_logprob_out(dict({"logprob": lp}, **(out or {}))))
+        return e.value.code
+
+    assert code(M=-1) == ot.OT_ERR_SHAPE and code(V=0) == ot.OT_ERR_SHAPE and code(ld=99) == ot.OT_ERR_SHAPE and code(n_tok=-1) == ot.OT_ERR_SHAPE
+    assert code(n_top=-1) == ot.OT_ERR_SHAPE and code(n_top=65) == ot.OT_ERR_SHAPE and code(reserved=1) == ot.OT_ERR_SHAPE
+    assert code(dtype=ot.OT_F16) == ot.OT_ERR_DTYPE and code(dtype=9) == ot.OT_ERR_DTYPE
+    assert code(logits=None) == ot.OT_ERR_NULL and code(tokens=None) == ot.OT_ERR_NULL and code(out={"logprob": None}) == ot.OT_ERR_NULL
+    assert code(n_top=3) == ot.OT_ERR_NULL and code(out={"row_max": lp}) == ot.OT_ERR_NULL and code(out={"row_sumexp": lp}) == ot.OT_ERR_NULL
+    assert code(n_tok=0, tokens=None, given_rows_only=True) == ot.OT_ERR_SHAPE
+    assert code(row_off=tok, B=0, temperature=lp) == ot.OT_ERR_SHAPE and code(row_off=tok, B=3) == ot.OT_ERR_SHAPE
+    assert code(logits=z.data_ptr() + 2) == ot.OT_ERR_SHAPE
+
+    fwd = {"row_max": lp, "row_sumexp": lp, "entropy": lp}
+
+    def gcode(fwd=fwd, grad=z, ld=100, gH=None, **kw):
+        with pytest.raises(ot.OtError) as e:
+            ot.ot_token_logprobs_grad(v.ctx, ot.make_logprob_in(**dict(base, **kw)), ot.make_logprob_out(fwd), lp, gH, grad, ld)
+        return e.value.code
+
+    wide = torch.zeros(4, 200, device=DEV)
+    assert gcode(grad=None) == ot.OT_ERR_NULL and gcode(fwd={"row_max": lp}) == ot.OT_ERR_NULL and gcode(ld=99) == ot.OT_ERR_SHAPE
+    assert gcode(fwd={"row_max": lp, "row_sumexp": lp}, gH=lp) == ot.OT_ERR_NULL and gcode(grad=wide.data_ptr() + 2, ld=200) == ot.OT_ERR_SHAPE
+    assert gcode(grad=z, ld=101) == ot.OT_ERR_SHAPE and gcode(dtype=3) == ot.OT_ERR_DTYPE
+    for bad in (dict(logits=z.half()), dict(logits=z.t()), dict(logits=z[:1].expand(4, 100)), dict(tokens=tok.long()), dict(tokens=tok[:3]),
+                dict(temperature=lp[:3]), dict(temperature=lp.double())):
+        with pytest.raises((ValueError, ot.OtError)):
+            v.token_logprobs(bad.pop("logits", z), bad.pop("tokens", tok), **bad)

@@ -1,0 +1,55 @@
+"""A program's iteration: a step through a 4-bit head, the emitted tokens' log-probabilities with alternatives, the drafter's loss and its
+gradient, and the log-probabilities of given tokens under the same head."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import distill_grad as og
+from oracle import logprobs as ol
+from oracle import quant_head as oq
+from oracle import verify as ov
+from test_gpu_quant_head import _weights
+from workloads import CaseSpec, make_case
+
+pytestmark = pytest.mark.gpu
+
+
+def test_an_iteration():
+    from paper_2507_02659_amd.runner import Verifier
+    rng = np.random.default_rng(3)
+    case = make_case(CaseSpec(name="iteration", dtype="bf16", d=512, V_t=5003, V_d=2001, k=[5, 0, 8, 3, 6], temperature=[1.0, 1.0, 0.7, 0.0, 1.0], n_direct=1500,
+                              n_ngram=300, ngram_len=(2, 4), plant_cover=0.4, data_seed=3, philox_seed=4))
+    w, given = _weights(rng, 512, 5003, 128, "f16", True)
+    v = Verifier.quantized(w, V_d=2001, direct_map=case.direct_map, max_batch=5, max_k=8, max_ngram_len=case.max_ngram_len)
+    v.set_cache(case.ngram_key_off, case.ngram_key_ids, case.ngram_target_ids)
+    inp = v.upload(case)
+    for step in range(2):
+        v.step(inp, step=step)
+        emitted = v.step_logprobs(inp, n_top=5)
+        plain = v.step_logprobs(inp, n_top=5, at_temperature=False)
+        loss = v.distill_loss_grad(inp)
+        scored = v.token_logprobs(v.lm_head(inp["hidden"]), inp["out"]["mapped_ids"], n_top=2)
+        res, Z = v.results(inp), v.workspace(case.M, case.K, with_logits=True)["logits"]
+        want_Z = oq.logits(ov.widen(case.hidden, "bf16"), *given)
+        np.testing.assert_allclose(Z, want_Z, atol=1e-5 * np.abs(want_Z).max())
+        T = np.repeat(case.temperature, case.k + 1)
+        for got, temps in ((emitted, T), (plain, np.ones(case.M))):
+            want = ol.token_logprobs(Z, res["out_tokens"], temps, 5, True)
+            assert np.array_equal(got["top_ids"].cpu().numpy(), want["top_ids"])
+            for n in ("logprob", "entropy", "top_logprobs"):
+                np.testing.assert_allclose(got[n].cpu().numpy().reshape(want[n].shape), want[n], rtol=2e-6, atol=2e-6, err_msg=n)
+        # the probability that the step tested with is the one reported
+        for b in range(case.B):
+            for row in range(case.row_off[b], case.row_off[b] + res["n_accept"][b]):
+                if case.temperature[b] > 0:
+                    assert float(emitted["logprob"][row]) == pytest.approx(np.log(res["p_tok"][row]), abs=1e-5)
+        want = ol.token_logprobs(Z, res["mapped_ids"], np.ones(case.M), 2)
+        assert np.array_equal(scored["top_ids"].cpu().numpy(), want["top_ids"])
+        np.testing.assert_allclose(scored["logprob"].cpu().numpy(), want["logprob"][:, 0], rtol=2e-6, atol=2e-6)
+        case_z = dict(row_off=case.row_off, draft_ids=case.draft_ids, draft_logits=case.draft_logits, direct_map=case.direct_map, V_t=case.V_t,
+                      cache=ov.build_cache(case.ngram_key_off, case.ngram_key_ids, case.ngram_target_ids), max_ngram_len=case.max_ngram_len,
+                      temperature=case.temperature, target_logits=Z, dtype="bf16")
+        want, scale, _ = og.hybrid_loss_grad(**case_z)
+        grad = loss["grad"].double().cpu().numpy()
+        assert (np.abs(grad - want) <= 8e-6 * scale * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want) + 1e-37).all()
+    v.close()
