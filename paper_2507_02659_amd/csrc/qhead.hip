@@ -6,6 +6,8 @@
 // then the group's scale multiplies 16 rows x 16 columns in four instructions.  Products of a bf16 number and 16 + c are exact in
 // fp32, so what is rounded is the sums alone; they are at most 31 / |c - zp| times as large as with the centred codes, which
 // costs less than the fp32 rounding of a group's scaled sum in the total over the groups.
+#include <algorithm>
+
 #include "device_math.h"
 #include "otv_internal.h"
 
@@ -69,40 +71,252 @@ __global__ void pack_scales_kernel(const void* __restrict__ scales, int f16, con
   recs[i] = r;
 }
 
-// One wavefront per 16 columns and 16 rows.
-template <int kSteps>
-__global__ __launch_bounds__(256) void qhead_kernel(const uint16_t* __restrict__ H, int M, int d, QuantHead q, float* __restrict__ Z, int V_t, int64_t ldz) {
-  constexpr int kGroups = 4 / kSteps;
-  const int lane = threadIdx.x & 63, tile = blockIdx.x * 4 + uniform((int)threadIdx.x >> 6), row0 = blockIdx.y * 16;
-  if (tile >= q.tiles) return;
-  const uint16_t* h = H + (int64_t)min(row0 + (lane & 15), M - 1) * d;
-  const u32x4* codes = reinterpret_cast<const u32x4*>(q.codes) + (int64_t)tile * q.blocks * 64 + lane;
-  const uint32_t* recs = q.recs + (int64_t)tile * q.blocks * 16 * kGroups + (lane & 15) * kGroups;
-  f32x4 total = {};
-  for (int b = 0; b < q.blocks; ++b) {
-    const u32x4 w = codes[(int64_t)b * 64];
+// What a wavefront reads of the weights: the codes of S tiles of 16 columns and a block of 128 hidden indices, with the scales.
+// Addresses are a base that the wavefront shares and 32 bits of the lane's own.
+template <int S, int kGroups>
+struct Weights {
+  u32x4 w[S];
+  uint32_t rec[S][kGroups];
+};
+template <typename T>
+__device__ inline T load_at(const void* base, uint32_t bytes) { return *reinterpret_cast<const T*>(static_cast<const char*>(base) + bytes); }
+template <int S, int kGroups, bool kOnce>
+__device__ inline void load_weights(const QuantHead& q, const int* tile, int b, int lane, Weights<S, kGroups>* out) {
+  typedef uint32_t recs_t __attribute__((ext_vector_type(kGroups == 1 ? 2 : kGroups)));
 #pragma unroll
-    for (int g = 0; g < kGroups; ++g) {
-      const uint32_t rec = recs[(int64_t)b * 16 * kGroups + g];
-      f32x4 acc = {}, sum = {};
+  for (int s = 0; s < S; ++s) {
+    const int64_t at = (int64_t)tile[s] * q.blocks + b;
+    const char* codes = reinterpret_cast<const char*>(q.codes) + at * 1024;
+    if (kOnce) out->w[s] = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(codes + (uint32_t)lane * 16));
+    else out->w[s] = load_at<u32x4>(codes, (uint32_t)lane * 16);
+    const char* recs = reinterpret_cast<const char*>(q.recs) + at * (64 * kGroups);
+    if constexpr (kGroups == 1) {
+      out->rec[s][0] = load_at<uint32_t>(recs, (uint32_t)(lane & 15) * 4);
+    } else {
+      const recs_t r = load_at<recs_t>(recs, (uint32_t)(lane & 15) * (4 * kGroups));
 #pragma unroll
-      for (int s = 0; s < kSteps; ++s) {
-        const int ks = g * kSteps + s, k = b * 128 + ks * 32 + (lane >> 4) * 8;
-        const u32x4 x = k < d ? *reinterpret_cast<const u32x4*>(h + k) : u32x4{};
-        acc = mfma(x, codes_to_bf16(w[ks]), acc);
-        sum = mfma(x, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, sum);
-      }
-      const float s = rec_scale(rec), zero = rec_zero(rec);
-#pragma unroll
-      for (int i = 0; i < 4; ++i) total[i] = fmaf(s, fmaf(-zero, sum[i], acc[i]), total[i]);
+      for (int g = 0; g < kGroups; ++g) out->rec[s][g] = r[g];
     }
   }
-  const int v = tile * 16 + (lane & 15);
+}
+// The operands of block b of 16 hidden rows; h: the rows' first element, `at`: the lane's row and its 8 indices within a step, in bytes.
+__device__ inline void load_hidden(const uint16_t* h, uint32_t at, int b, int d, int lane, u32x4* x) {
+  if ((b + 1) * 128 <= d) {
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const int row = row0 + 4 * (lane >> 4) + i;
-    if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = total[i];
+    for (int ks = 0; ks < 4; ++ks) x[ks] = load_at<u32x4>(h + b * 128, at + ks * 64);
+  } else {
+#pragma unroll
+    for (int ks = 0; ks < 4; ++ks) x[ks] = b * 128 + ks * 32 + (lane >> 4) * 8 < d ? load_at<u32x4>(h + b * 128, at + ks * 64) : u32x4{};
   }
+}
+
+// Up to 16 rows.  The hidden rows lie in LDS in the order of the matrix instruction's operand, [32-deep step][lane], all of the hidden
+// dimension where it fits (chunk_steps steps); behind that every wavefront goes its own way: S tiles of 16 columns and one of `parts`
+// parts of the hidden dimension, its weights asked for kAhead blocks ahead.  No barrier until the parts are joined.
+template <int S, int kSteps, int kAhead>
+__global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __restrict__ H, int M, int d, QuantHead q, float* __restrict__ Z, int V_t,
+                                                            int64_t ldz, int chunk_blocks, int parts) {
+  constexpr int kGroups = 4 / kSteps;
+  extern __shared__ u32x4 s_x[];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n_waves = blockDim.x >> 6;
+  const int part = wave % parts, first = ((int)blockIdx.x * (n_waves / parts) + wave / parts) * S;
+  int tile[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) tile[s] = min(first + s, q.tiles - 1);
+  const uint32_t h_at = (uint32_t)(min(lane & 15, M - 1) * d + (lane >> 4) * 8) * 2;
+  f32x4 total[S] = {};
+  for (int c0 = 0; c0 < q.blocks; c0 += chunk_blocks) {
+    const int c1 = min(c0 + chunk_blocks, q.blocks), len = (c1 - c0 + parts - 1) / parts;
+    const int b0 = min(c0 + part * len, c1), b1 = min(b0 + len, c1);
+    Weights<S, kGroups> ring[kAhead];
+    if (b0 < b1) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) load_weights<S, kGroups, true>(q, tile, min(b0 + i, b1 - 1), lane, &ring[i]);
+    }
+    if (c0 > 0) __syncthreads();
+    for (int b = c0 + wave; b < c1; b += n_waves) {
+      u32x4 x[4];
+      load_hidden(H, h_at, b, d, lane, x);
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) s_x[((b - c0) * 4 + ks) * 64 + lane] = x[ks];
+    }
+    __syncthreads();
+    for (int b = b0; b < b1; b += kAhead) {
+#pragma unroll
+      for (int i = 0; i < kAhead; ++i) {
+        if (b + i < b1) {
+          const u32x4* x = s_x + (b + i - c0) * 256 + lane;
+#pragma unroll
+          for (int g = 0; g < kGroups; ++g) {
+            f32x4 acc[S] = {}, sum = {};
+#pragma unroll
+            for (int t = 0; t < kSteps; ++t) {
+              const int ks = g * kSteps + t;
+              const u32x4 xf = x[ks * 64];
+              sum = mfma(xf, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, sum);
+#pragma unroll
+              for (int s = 0; s < S; ++s) acc[s] = mfma(xf, codes_to_bf16(ring[i].w[s][ks]), acc[s]);
+            }
+#pragma unroll
+            for (int s = 0; s < S; ++s) {
+              const float scale = rec_scale(ring[i].rec[s][g]), zero = rec_zero(ring[i].rec[s][g]);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) total[s][e] = fmaf(scale, fmaf(-zero, sum[e], acc[s][e]), total[s][e]);
+            }
+          }
+          load_weights<S, kGroups, true>(q, tile, min(b + i + kAhead, b1 - 1), lane, &ring[i]);
+        }
+      }
+    }
+  }
+  if (parts > 1) {                                       // joined in ascending order by the wavefront of part 0
+    __syncthreads();
+    f32x4* red = reinterpret_cast<f32x4*>(s_x);
+    if (part > 0) {
+#pragma unroll
+      for (int s = 0; s < S; ++s) red[(wave * S + s) * 64 + lane] = total[s];
+    }
+    __syncthreads();
+    if (part > 0) return;
+    for (int p = 1; p < parts; ++p) {
+#pragma unroll
+      for (int s = 0; s < S; ++s) total[s] += red[((wave + p) * S + s) * 64 + lane];
+    }
+  }
+#pragma unroll
+  for (int s = 0; s < S; ++s) {
+    const int v = (first + s) * 16 + (lane & 15);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int row = 4 * (lane >> 4) + e;
+      if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = total[s][e];
+    }
+  }
+}
+
+// More than 16 rows: blocks of RT tiles of 16 rows.  A wavefront owns S tiles of 16 columns over the whole hidden dimension; the block's
+// hidden rows come through LDS in chunks of kBlocks * 128 hidden indices, two buffers, one barrier per chunk.  A wavefront stages whole
+// (row tile, block) units, in the order of the matrix instruction's operand, and forms their groups' sums on the way (a product with ones).
+constexpr int kTallWaves = 8;
+constexpr int tall_blocks(int RT) { return RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }
+template <int RT, int S, int kSteps, int kAhead>
+__global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint16_t* __restrict__ H, int M, int d, QuantHead q, float* __restrict__ Z,
+                                                                     int V_t, int64_t ldz, int m_blocks) {
+  constexpr int kGroups = 4 / kSteps, kBlocks = tall_blocks(RT), kUnits = kBlocks * RT;
+  constexpr int kStage = (kUnits + kTallWaves - 3) / (kTallWaves - 2);   // units per wavefront of six at least
+  __shared__ u32x4 s_x[2][kUnits][4][64];
+  __shared__ f32x4 s_sum[2][kUnits][kGroups][4];
+  const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n_waves = blockDim.x >> 6;
+  const int slot = (int)blockIdx.x >> 3, row0 = slot % m_blocks * (RT * 16), ct = slot / m_blocks * 8 + ((int)blockIdx.x & 7);
+  const int first = (ct * n_waves + wave) * S;
+  if (ct * n_waves * S >= q.tiles) return;               // padding of the id space
+  int tile[S];
+#pragma unroll
+  for (int s = 0; s < S; ++s) tile[s] = min(first + s, q.tiles - 1);
+  u32x4 stage[kStage][4];
+  auto fetch = [&](int c) {                              // this wavefront's units of chunk c
+#pragma unroll
+    for (int j = 0; j < kStage; ++j) {
+      const int u = wave + j * n_waves;
+      if (u < kUnits) {
+        const int row = min(u % RT * 16 + (lane & 15), M - 1 - row0);
+        load_hidden(H + (int64_t)row0 * d, (uint32_t)(row * d + (lane >> 4) * 8) * 2, c * kBlocks + u / RT, d, lane, stage[j]);
+      }
+    }
+  };
+  auto put = [&](int buf) {
+#pragma unroll
+    for (int j = 0; j < kStage; ++j) {
+      const int u = wave + j * n_waves;
+      if (u < kUnits) {
+#pragma unroll
+        for (int g = 0; g < kGroups; ++g) {
+          f32x4 sum = {};
+#pragma unroll
+          for (int t = 0; t < kSteps; ++t) {
+            const u32x4 x = stage[j][g * kSteps + t];
+            s_x[buf][u][g * kSteps + t][lane] = x;
+            sum = mfma(x, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, sum);
+          }
+          if ((lane & 15) == 0) s_sum[buf][u][g][lane >> 4] = sum;
+        }
+      }
+    }
+  };
+  Weights<S, kGroups> ring[kAhead];
+#pragma unroll
+  for (int i = 0; i < kAhead; ++i) load_weights<S, kGroups, false>(q, tile, min(i, q.blocks - 1), lane, &ring[i]);
+  fetch(0);
+  put(0);
+  f32x4 total[RT][S] = {};
+  const int chunks = (q.blocks + kBlocks - 1) / kBlocks;
+  auto block = [&](int buf, int j, Weights<S, kGroups>& W) {
+    u32x4 w[S][4];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) w[s][ks] = codes_to_bf16(W.w[s][ks]);
+    float scale[S][kGroups], zero[S][kGroups];
+#pragma unroll
+    for (int s = 0; s < S; ++s)
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) { scale[s][g] = rec_scale(W.rec[s][g]); zero[s][g] = -rec_zero(W.rec[s][g]); }
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const int u = j * RT + rt;
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) {
+        const f32x4 sum = s_sum[buf][u][g][lane >> 4];
+        f32x4 acc[S];
+#pragma unroll
+        for (int s = 0; s < S; ++s) acc[s] = sum * zero[s][g];
+#pragma unroll
+        for (int t = 0; t < kSteps; ++t) {
+          const u32x4 x = s_x[buf][u][g * kSteps + t][lane];
+#pragma unroll
+          for (int s = 0; s < S; ++s) acc[s] = mfma(x, w[s][g * kSteps + t], acc[s]);
+        }
+#pragma unroll
+        for (int s = 0; s < S; ++s)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) total[rt][s][e] = fmaf(scale[s][g], acc[s][e], total[rt][s][e]);
+      }
+      // a row tile's sums are formed before the next tile's reads: left to itself the compiler reads first and multiplies last, and spills
+#pragma unroll
+      for (int s = 0; s < S; ++s) asm volatile("" : "+v"(total[rt][s]));
+    }
+  };
+  constexpr int kTurn = kAhead / kBlocks;                // chunks per trip: the ring's places and, if even, the buffers are constants
+  static_assert(kAhead % kBlocks == 0, "a chunk's blocks have places of their own in the ring");
+  // chunks are padded to whole trips: past the last block the hidden rows are staged as zeros, and the last block's weights are used again
+  for (int c0 = 0; c0 < chunks; c0 += kTurn) {
+#pragma unroll
+    for (int cc = 0; cc < kTurn; ++cc) {
+      const int c = c0 + cc, buf = kTurn % 2 == 0 ? cc & 1 : c & 1;
+      __syncthreads();
+      fetch(c + 1);
+#pragma unroll
+      for (int j = 0; j < kBlocks; ++j) {
+        const int b = c * kBlocks + j;
+        if (kBlocks == 1 || b < q.blocks) {
+          block(buf, j, ring[cc * kBlocks + j]);
+          load_weights<S, kGroups, false>(q, tile, min(b + kAhead, q.blocks - 1), lane, &ring[cc * kBlocks + j]);
+        }
+      }
+      put(buf ^ 1);
+    }
+  }
+#pragma unroll
+  for (int rt = 0; rt < RT; ++rt)
+#pragma unroll
+    for (int s = 0; s < S; ++s) {
+      const int v = (first + s) * 16 + (lane & 15);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = row0 + rt * 16 + 4 * (lane >> 4) + e;
+        if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = total[rt][s][e];
+      }
+    }
 }
 
 }  // namespace
@@ -119,14 +333,67 @@ hipError_t launch_pack_quant(const uint8_t* codes, const void* scales, int scale
   return hipGetLastError();
 }
 
-hipError_t launch_qhead(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
-  (void)n_cu;
-  if (M == 0) return hipSuccess;
-  const dim3 grid((unsigned)ceil_div(q.tiles, 4), (unsigned)ceil_div(M, 16)), block(256);
-  if (grid.y > 65535) return hipErrorInvalidValue;
-  const auto kernel = q.steps == 4 ? qhead_kernel<4> : q.steps == 2 ? qhead_kernel<2> : qhead_kernel<1>;
-  hipLaunchKernelGGL(kernel, grid, block, 0, stream, H, M, d, q, Z, V_t, ldz);
+namespace {
+
+constexpr int kChunkBlocks = 38;      // blocks of 16 hidden rows in LDS at most: 4 KB each
+
+template <int S, int kSteps>
+hipError_t launch_rows16(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int columns, int parts, hipStream_t stream) {
+  constexpr int kAhead = S == 1 ? 8 : S == 2 ? 4 : S == 3 ? 3 : 2;
+  const int chunks = ceil_div(q.blocks, kChunkBlocks), chunk_blocks = ceil_div(q.blocks, chunks), waves = columns * parts;
+  const size_t lds = (size_t)1024 * std::max(4 * chunk_blocks, parts > 1 ? waves * S : 0);
+  hipLaunchKernelGGL((qhead_rows16_kernel<S, kSteps, kAhead>), dim3((unsigned)ceil_div(q.tiles, columns * S)), dim3(64 * waves), lds, stream, H, M, d, q, Z,
+                     V_t, ldz, chunk_blocks, parts);
   return hipGetLastError();
+}
+
+template <int kSteps>
+hipError_t launch_up_to_16(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
+  const int rounds = ceil_div(q.tiles, 64 * n_cu), per_cu = ceil_div(q.tiles, rounds * n_cu);
+  const int S = ceil_div(per_cu, 16), columns = ceil_div(per_cu, S), parts = std::max(1, std::min(16 / columns, q.blocks));
+  switch (S) {
+    case 1: return launch_rows16<1, kSteps>(H, M, d, q, Z, V_t, ldz, columns, parts, stream);
+    case 2: return launch_rows16<2, kSteps>(H, M, d, q, Z, V_t, ldz, columns, parts, stream);
+    case 3: return launch_rows16<3, kSteps>(H, M, d, q, Z, V_t, ldz, columns, parts, stream);
+    default: return launch_rows16<4, kSteps>(H, M, d, q, Z, V_t, ldz, columns, parts, stream);
+  }
+}
+
+template <int RT, int S, int kSteps>
+hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int m_blocks, int waves, hipStream_t stream) {
+  constexpr int kAhead = RT <= 4 ? 4 : 2;
+  const int64_t grid = (int64_t)ceil_div(ceil_div(q.tiles, waves * S), 8) * 8 * m_blocks;
+  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  hipLaunchKernelGGL((qhead_tall_kernel<RT, S, kSteps, kAhead>), dim3((unsigned)grid), dim3(64 * waves), 0, stream, H, M, d, q, Z, V_t, ldz, m_blocks);
+  return hipGetLastError();
+}
+
+template <int kSteps>
+hipError_t launch_above_16(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
+  const int m_blocks = ceil_div(M, 9 * 16), RT = ceil_div(M, 16 * m_blocks);
+  const int most = RT <= 2 ? 4 : 2;
+  int S = 1, waves = 8;
+  int64_t best = INT64_MAX;
+  for (int s = 1; s <= most; s *= 2)
+    for (int w = 8; w >= 6; --w) {
+      const int64_t cost = (int64_t)ceil_div((int64_t)ceil_div(q.tiles, s * w) * m_blocks, n_cu) * s * w;
+      if (cost < best || (cost == best && s > S)) { best = cost; S = s; waves = w; }
+    }
+#define OT_TALL(rt, s) if (RT == rt && S == s) return launch_tall<rt, s, kSteps>(H, M, d, q, Z, V_t, ldz, m_blocks, waves, stream)
+  OT_TALL(2, 1); OT_TALL(2, 2); OT_TALL(2, 4);
+  OT_TALL(3, 1); OT_TALL(3, 2); OT_TALL(4, 1); OT_TALL(4, 2); OT_TALL(5, 1); OT_TALL(5, 2); OT_TALL(6, 1); OT_TALL(6, 2);
+  OT_TALL(7, 1); OT_TALL(7, 2); OT_TALL(8, 1); OT_TALL(8, 2); OT_TALL(9, 1); OT_TALL(9, 2);
+#undef OT_TALL
+  return hipErrorInvalidValue;
+}
+
+}  // namespace
+
+hipError_t launch_qhead(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
+  if (M == 0) return hipSuccess;
+  if (q.steps == 4) return M <= 16 ? launch_up_to_16<4>(H, M, d, q, Z, V_t, ldz, n_cu, stream) : launch_above_16<4>(H, M, d, q, Z, V_t, ldz, n_cu, stream);
+  if (q.steps == 2) return M <= 16 ? launch_up_to_16<2>(H, M, d, q, Z, V_t, ldz, n_cu, stream) : launch_above_16<2>(H, M, d, q, Z, V_t, ldz, n_cu, stream);
+  return M <= 16 ? launch_up_to_16<1>(H, M, d, q, Z, V_t, ldz, n_cu, stream) : launch_above_16<1>(H, M, d, q, Z, V_t, ldz, n_cu, stream);
 }
 
 }  // namespace otv
