@@ -25,9 +25,12 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 // Eight codes of one packed word as bf16 numbers 16 + c, in ascending hidden index.  The word is the one whose nibble j holds code 2 j
 // and whose nibble j + 4 code 2 j + 1 (j < 4), rotated left by 3: a pair's mantissa bits are then a shift and a mask away.
 __device__ inline u32x4 codes_to_bf16(uint32_t w) {
-  constexpr uint32_t kMask = 0x00780078u, kSixteen = 0x41804180u;
-  return u32x4{(w & kMask) | kSixteen, (w >> 4 & kMask) | kSixteen, (w >> 8 & kMask) | kSixteen,
-               (__builtin_amdgcn_alignbit(w, w, 12) & kMask) | kSixteen};
+  auto bits = [](uint32_t x) {                           // (x & mask) | 16: one instruction, which takes no literals, so from registers
+    uint32_t r;
+    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(0x00780078u), "v"(0x41804180u));
+    return r;
+  };
+  return u32x4{bits(w), bits(w >> 4), bits(w >> 8), bits(__builtin_amdgcn_alignbit(w, w, 12))};
 }
 // A group's scale and 16 + zero point of one column: the scale's fp32 bits, of which a bf16 or fp16 scale leaves the low 13 free.
 __device__ inline float rec_scale(uint32_t r) { return __uint_as_float(r & 0xFFFFE000u); }
@@ -99,15 +102,17 @@ __device__ inline void load_weights(const QuantHead& q, const int* tile, int b, 
     }
   }
 }
-// The operands of block b of 16 hidden rows; h: the rows' first element, `at`: the lane's row and its 8 indices within a step, in bytes.
-__device__ inline void load_hidden(const uint16_t* h, uint32_t at, int b, int d, int lane, u32x4* x) {
-  if ((b + 1) * 128 <= d) {
+// The operands of block b of 16 hidden rows; h: the rows' first element, row_at: the lane's row, in bytes.  Indices past d are read from the
+// row's end, without a branch (which would make the compiler wait for whatever else is on its way), and zeroed by clear_tail.
+__device__ inline void load_hidden(const uint16_t* h, uint32_t row_at, int b, int d, int lane, u32x4* x) {
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) x[ks] = load_at<u32x4>(h + b * 128, at + ks * 64);
-  } else {
+  for (int ks = 0; ks < 4; ++ks) x[ks] = load_at<u32x4>(h, row_at + 2u * min(b * 128 + ks * 32 + (lane >> 4) * 8, d - 8));
+}
+__device__ inline void clear_tail(int b, int d, int lane, u32x4* x) {
+  if ((b + 1) * 128 <= d) return;
 #pragma unroll
-    for (int ks = 0; ks < 4; ++ks) x[ks] = b * 128 + ks * 32 + (lane >> 4) * 8 < d ? load_at<u32x4>(h + b * 128, at + ks * 64) : u32x4{};
-  }
+  for (int ks = 0; ks < 4; ++ks)
+    if (b * 128 + ks * 32 + (lane >> 4) * 8 >= d) x[ks] = u32x4{};
 }
 
 // Up to 16 rows.  The hidden rows lie in LDS in the order of the matrix instruction's operand, [32-deep step][lane], all of the hidden
@@ -123,7 +128,7 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
   int tile[S];
 #pragma unroll
   for (int s = 0; s < S; ++s) tile[s] = min(first + s, q.tiles - 1);
-  const uint32_t h_at = (uint32_t)(min(lane & 15, M - 1) * d + (lane >> 4) * 8) * 2;
+  const uint32_t h_at = 2u * (uint32_t)(min(lane & 15, M - 1) * d);
   f32x4 total[S] = {};
   for (int c0 = 0; c0 < q.blocks; c0 += chunk_blocks) {
     const int c1 = min(c0 + chunk_blocks, q.blocks), len = (c1 - c0 + parts - 1) / parts;
@@ -137,6 +142,7 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
     for (int b = c0 + wave; b < c1; b += n_waves) {
       u32x4 x[4];
       load_hidden(H, h_at, b, d, lane, x);
+      clear_tail(b, d, lane, x);
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) s_x[((b - c0) * 4 + ks) * 64 + lane] = x[ks];
     }
@@ -198,11 +204,11 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
 // hidden rows come through LDS in chunks of kBlocks * 128 hidden indices, two buffers, one barrier per chunk.  A wavefront stages whole
 // (row tile, block) units, in the order of the matrix instruction's operand, and forms their groups' sums on the way (a product with ones).
 constexpr int kTallWaves = 8;
-constexpr int tall_blocks(int RT) { return RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }
+constexpr int tall_blocks(int RT, int S) { return S > 2 ? (RT <= 2 ? 2 : 1) : RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }
 template <int RT, int S, int kSteps, int kAhead>
 __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint16_t* __restrict__ H, int M, int d, QuantHead q, float* __restrict__ Z,
                                                                      int V_t, int64_t ldz, int m_blocks) {
-  constexpr int kGroups = 4 / kSteps, kBlocks = tall_blocks(RT), kUnits = kBlocks * RT;
+  constexpr int kGroups = 4 / kSteps, kBlocks = tall_blocks(RT, S), kUnits = kBlocks * RT;
   constexpr int kStage = (kUnits + kTallWaves - 3) / (kTallWaves - 2);   // units per wavefront of six at least
   __shared__ u32x4 s_x[2][kUnits][4][64];
   __shared__ f32x4 s_sum[2][kUnits][kGroups][4];
@@ -218,17 +224,18 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
       const int u = wave + j * n_waves;
-      if (u < kUnits) {
-        const int row = min(u % RT * 16 + (lane & 15), M - 1 - row0);
-        load_hidden(H + (int64_t)row0 * d, (uint32_t)(row * d + (lane >> 4) * 8) * 2, c * kBlocks + u / RT, d, lane, stage[j]);
+      if (j == 0 || u < kUnits) {
+        const int row = min(min(u, kUnits - 1) % RT * 16 + (lane & 15), M - 1 - row0);
+        load_hidden(H + (int64_t)row0 * d, 2u * (uint32_t)(row * d), c * kBlocks + min(u, kUnits - 1) / RT, d, lane, stage[j]);
       }
     }
   };
-  auto put = [&](int buf) {
+  auto put = [&](int c, int buf) {
 #pragma unroll
     for (int j = 0; j < kStage; ++j) {
       const int u = wave + j * n_waves;
       if (u < kUnits) {
+        clear_tail(c * kBlocks + u / RT, d, lane, stage[j]);
 #pragma unroll
         for (int g = 0; g < kGroups; ++g) {
           f32x4 sum = {};
@@ -247,7 +254,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
   for (int i = 0; i < kAhead; ++i) load_weights<S, kGroups, false>(q, tile, min(i, q.blocks - 1), lane, &ring[i]);
   fetch(0);
-  put(0);
+  put(0, 0);
   f32x4 total[RT][S] = {};
   const int chunks = (q.blocks + kBlocks - 1) / kBlocks;
   auto block = [&](int buf, int j, Weights<S, kGroups>& W) {
@@ -261,27 +268,36 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
     for (int s = 0; s < S; ++s)
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) { scale[s][g] = rec_scale(W.rec[s][g]); zero[s][g] = -rec_zero(W.rec[s][g]); }
+    // a row tile's operands are read while the tile in front of it is multiplied
+    u32x4 x[2][4];
+    f32x4 sum[2][kGroups];
+    auto read = [&](int rt) {
+#pragma unroll
+      for (int g = 0; g < kGroups; ++g) sum[rt & 1][g] = s_sum[buf][j * RT + rt][g][lane >> 4];
+#pragma unroll
+      for (int ks = 0; ks < 4; ++ks) x[rt & 1][ks] = s_x[buf][j * RT + rt][ks][lane];
+    };
+    read(0);
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
-      const int u = j * RT + rt;
+      if (rt + 1 < RT) read(rt + 1);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        const f32x4 sum = s_sum[buf][u][g][lane >> 4];
         f32x4 acc[S];
 #pragma unroll
-        for (int s = 0; s < S; ++s) acc[s] = sum * zero[s][g];
+        for (int s = 0; s < S; ++s) acc[s] = sum[rt & 1][g] * zero[s][g];
 #pragma unroll
         for (int t = 0; t < kSteps; ++t) {
-          const u32x4 x = s_x[buf][u][g * kSteps + t][lane];
 #pragma unroll
-          for (int s = 0; s < S; ++s) acc[s] = mfma(x, w[s][g * kSteps + t], acc[s]);
+          for (int s = 0; s < S; ++s) acc[s] = mfma(x[rt & 1][g * kSteps + t], w[s][g * kSteps + t], acc[s]);
         }
 #pragma unroll
         for (int s = 0; s < S; ++s)
 #pragma unroll
           for (int e = 0; e < 4; ++e) total[rt][s][e] = fmaf(scale[s][g], acc[s][e], total[rt][s][e]);
       }
-      // a row tile's sums are formed before the next tile's reads: left to itself the compiler reads first and multiplies last, and spills
+      // a row tile's sums are formed before the tile after the next one is read: left to itself the compiler reads first and multiplies
+      // last, and spills
 #pragma unroll
       for (int s = 0; s < S; ++s) asm volatile("" : "+v"(total[rt][s]));
     }
@@ -303,7 +319,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
           load_weights<S, kGroups, false>(q, tile, min(b + kAhead, q.blocks - 1), lane, &ring[cc * kBlocks + j]);
         }
       }
-      put(buf ^ 1);
+      put(c + 1, buf ^ 1);
     }
   }
 #pragma unroll
@@ -361,7 +377,7 @@ hipError_t launch_up_to_16(const uint16_t* H, int M, int d, const QuantHead& q, 
 
 template <int RT, int S, int kSteps>
 hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int m_blocks, int waves, hipStream_t stream) {
-  constexpr int kAhead = RT <= 4 ? 4 : 2;
+  constexpr int kAhead = S > 2 ? 2 : RT <= 4 ? 4 : 2;
   const int64_t grid = (int64_t)ceil_div(ceil_div(q.tiles, waves * S), 8) * 8 * m_blocks;
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   hipLaunchKernelGGL((qhead_tall_kernel<RT, S, kSteps, kAhead>), dim3((unsigned)grid), dim3(64 * waves), 0, stream, H, M, d, q, Z, V_t, ldz, m_blocks);
@@ -371,7 +387,7 @@ hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, floa
 template <int kSteps>
 hipError_t launch_above_16(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
   const int m_blocks = ceil_div(M, 9 * 16), RT = ceil_div(M, 16 * m_blocks);
-  const int most = RT <= 2 ? 4 : 2;
+  const int most = kSteps == 4 && RT <= 5 ? 4 : 2;
   int S = 1, waves = 8;
   int64_t best = INT64_MAX;
   for (int s = 1; s <= most; s *= 2)
@@ -380,9 +396,9 @@ hipError_t launch_above_16(const uint16_t* H, int M, int d, const QuantHead& q, 
       if (cost < best || (cost == best && s > S)) { best = cost; S = s; waves = w; }
     }
 #define OT_TALL(rt, s) if (RT == rt && S == s) return launch_tall<rt, s, kSteps>(H, M, d, q, Z, V_t, ldz, m_blocks, waves, stream)
-  OT_TALL(2, 1); OT_TALL(2, 2); OT_TALL(2, 4);
-  OT_TALL(3, 1); OT_TALL(3, 2); OT_TALL(4, 1); OT_TALL(4, 2); OT_TALL(5, 1); OT_TALL(5, 2); OT_TALL(6, 1); OT_TALL(6, 2);
-  OT_TALL(7, 1); OT_TALL(7, 2); OT_TALL(8, 1); OT_TALL(8, 2); OT_TALL(9, 1); OT_TALL(9, 2);
+  if constexpr (kSteps == 4) { OT_TALL(2, 4); OT_TALL(3, 4); OT_TALL(4, 4); OT_TALL(5, 4); }
+  OT_TALL(2, 1); OT_TALL(2, 2); OT_TALL(3, 1); OT_TALL(3, 2); OT_TALL(4, 1); OT_TALL(4, 2); OT_TALL(5, 1); OT_TALL(5, 2);
+  OT_TALL(6, 1); OT_TALL(6, 2); OT_TALL(7, 1); OT_TALL(7, 2); OT_TALL(8, 1); OT_TALL(8, 2); OT_TALL(9, 1); OT_TALL(9, 2);
 #undef OT_TALL
   return hipErrorInvalidValue;
 }
