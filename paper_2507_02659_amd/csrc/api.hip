@@ -163,7 +163,10 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   ok = ok && dev_alloc(c, &c->loss_part, R * kLossGroups);
   ok = ok && dev_alloc(c, &c->adapt_part, 2 * Bm);
   ok = ok && dev_alloc(c, &c->unit_mass, Bm * c->max_units);
-  const size_t n_counters = 1 + (R + 1);                 // of adaptive drafting, of the loss
+  uint8_t* lp_part = nullptr;
+  ok = ok && dev_alloc(c, &lp_part, kLogprobSegments * logprob_segment_bytes());
+  c->lp_part = lp_part;
+  const size_t n_counters = 1 + (R + 1) + kLogprobSegments;   // of adaptive drafting, of the loss, of the log-probabilities
   ok = ok && dev_alloc(c, &c->counters, n_counters);
   if (!ok) { free_ctx(c); return fail(OT_ERR_NOMEM, "ot_verify_init: device allocation failed"); }
 
@@ -172,6 +175,7 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   if (e == hipSuccess) e = hipMemsetAsync(c->unit_mass, 0xFF, sizeof(double) * Bm * c->max_units, c->stream);
   c->adapt_count = c->counters;
   c->loss_count = c->adapt_count + 1;
+  c->lp_count = c->loss_count + R + 1;
   if (e == hipSuccess) e = hipMemcpyAsync(c->dmap, cfg->direct_map, sizeof(int32_t) * c->V_d, hipMemcpyHostToDevice, c->stream);
   if (e == hipSuccess) e = hipMemcpyAsync(c->tmap, tmap_h.data(), sizeof(int32_t) * tmap_h.size(), hipMemcpyHostToDevice, c->stream);
   c->pairs = reinterpret_cast<const int2*>(c->tmap + pairs_at);

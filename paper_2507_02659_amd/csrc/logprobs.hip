@@ -5,6 +5,8 @@
 //   dz_v = (1/T) [ sum over tokens of v of g - p_v (G + gH (ln p_v + entropy)) ],   G = sum of the row's g.
 #include <math.h>
 
+#include <algorithm>
+
 #include "device_math.h"
 #include "otv_host.h"
 
@@ -37,83 +39,297 @@ __device__ inline bool any_given(const ot_logprob_in& in, int64_t row) {
   return false;
 }
 
+// ------------------------------------------------------------------------------------------------ alternatives
 // Order of alternatives as one number: by descending logit (-0 and 0 alike), of equal ones the lowest id first; 0 is none.
-__device__ inline unsigned long long order_key(float z, int v) {
+typedef unsigned long long key_t;
+__device__ inline key_t order_key(float z, int v) {
   const uint32_t u = __float_as_uint(z + 0.f), up = u & 0x80000000u ? ~u : u | 0x80000000u;
-  return z > -INFINITY ? (unsigned long long)up << 32 | (0xFFFFFFFFu - (uint32_t)v) : 0ull;
+  return z > -INFINITY ? (key_t)up << 32 | (0xFFFFFFFFu - (uint32_t)v) : 0ull;
 }
-__device__ inline unsigned long long wave_max(unsigned long long k) {
-  for (int o = 32; o > 0; o >>= 1) {
-    const unsigned long long other = __shfl_xor(k, o);
-    k = other > k ? other : k;
-  }
-  return k;
+__device__ inline int key_id(key_t k) { return (int)(0xFFFFFFFFu - (uint32_t)k); }
+__device__ inline float key_logit(key_t k) {
+  const uint32_t up = (uint32_t)(k >> 32);
+  return k ? __uint_as_float(up & 0x80000000u ? up ^ 0x80000000u : ~up) : -INFINITY;
+}
+__device__ inline key_t lane_key(key_t k, int l) {
+  return (key_t)(uint32_t)__builtin_amdgcn_readlane((int)(k >> 32), l) << 32 | (uint32_t)__builtin_amdgcn_readlane((int)k, l);
+}
+// The partner's key, lanes apart by exclusive or with kMask: data-parallel moves within a row of 16 lanes, else through the LDS network.
+template <int kCtrl>
+__device__ inline key_t dpp_key(key_t k) {
+  const int hi = (int)(k >> 32), lo = (int)k;
+  return (key_t)(uint32_t)__builtin_amdgcn_update_dpp(hi, hi, kCtrl, 0xF, 0xF, false) << 32 |
+         (uint32_t)__builtin_amdgcn_update_dpp(lo, lo, kCtrl, 0xF, 0xF, false);
+}
+template <int kMask>
+__device__ inline key_t partner(key_t k) {
+  if constexpr (kMask == 1) return dpp_key<0xB1>(k);
+  else if constexpr (kMask == 2) return dpp_key<0x4E>(k);
+  else if constexpr (kMask == 3) return dpp_key<0x1B>(k);
+  else if constexpr (kMask == 4) return dpp_key<0x1B>(dpp_key<0x141>(k));
+  else if constexpr (kMask == 7) return dpp_key<0x141>(k);
+  else if constexpr (kMask == 8) return dpp_key<0x128>(k);
+  else if constexpr (kMask == 15) return dpp_key<0x140>(k);
+  else return __shfl_xor(k, kMask);
+}
+// The larger of the two partners' keys into the lower lane.
+template <int kMask>
+__device__ inline key_t exchange(key_t k, int lane) {
+  const key_t other = partner<kMask>(k);
+  constexpr int kHighest = kMask >= 32 ? 32 : kMask >= 16 ? 16 : kMask >= 8 ? 8 : kMask >= 4 ? 4 : kMask >= 2 ? 2 : 1;
+  return (other > k) != ((lane & kHighest) != 0) ? other : k;
+}
+// Sorts 64 keys over the lanes, the largest into lane 0: merges of 2, 4, ... lanes whose first step meets the mirrored lane, so that every
+// step has the same direction.
+__device__ inline key_t sort_keys(key_t k, int lane) {
+  k = exchange<1>(k, lane);
+  k = exchange<3>(k, lane); k = exchange<1>(k, lane);
+  k = exchange<7>(k, lane); k = exchange<2>(k, lane); k = exchange<1>(k, lane);
+  k = exchange<15>(k, lane); k = exchange<4>(k, lane); k = exchange<2>(k, lane); k = exchange<1>(k, lane);
+  k = exchange<31>(k, lane); k = exchange<8>(k, lane); k = exchange<4>(k, lane); k = exchange<2>(k, lane); k = exchange<1>(k, lane);
+  k = exchange<63>(k, lane); k = exchange<16>(k, lane); k = exchange<8>(k, lane); k = exchange<4>(k, lane); k = exchange<2>(k, lane);
+  return exchange<1>(k, lane);
+}
+// The 64 largest of a sorted list and of one whose lane i holds the (63 - i)-th.
+__device__ inline key_t merge_keys(key_t k, key_t mirrored, int lane) {
+  k = mirrored > k ? mirrored : k;
+  k = exchange<32>(k, lane); k = exchange<16>(k, lane); k = exchange<8>(k, lane); k = exchange<4>(k, lane); k = exchange<2>(k, lane);
+  return exchange<1>(k, lane);
+}
+// Puts a key (the same in every lane) into a sorted list.
+__device__ inline key_t insert_key(key_t list, key_t k, int lane) {
+  const int at = __popcll(__ballot(list > k));
+  const key_t below = __shfl_up(list, 1);
+  return lane < at ? list : lane == at ? k : below;
 }
 
-// One workgroup per row.
-__global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a) {
-  const ot_logprob_in& in = a.in;
-  const int row = blockIdx.x, tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  __shared__ float s_f[4];
-  __shared__ double s_d[2][4];
-  __shared__ unsigned long long s_k[4];
-  const void* z = row_of(in, row);
-  const float T = row_temperature(in, row, lane);
-  const float scale = kLog2e / T;
-  const bool skip = in.given_rows_only && !any_given(in, row);
-  const int V = skip ? 0 : in.V;
-  float mx = -INFINITY;
-  for (int v = tid; v < V; v += 256) mx = fmaxf(mx, logit(z, in.dtype, v));
-  mx = otv::wave_max(mx);
-  if (lane == 0) s_f[wave] = mx;
-  __syncthreads();
-  mx = fmaxf(fmaxf(s_f[0], s_f[1]), fmaxf(s_f[2], s_f[3]));
-  const float top = mx == -INFINITY ? 0.f : mx;
-  double S = 0.0, E = 0.0;
-  for (int v = tid; v < V; v += 256) {
-    const float t = (logit(z, in.dtype, v) - top) * scale, e = __builtin_amdgcn_exp2f(t);
-    S += e;
-    E -= e * fmaxf(t, -200.f);
+// ------------------------------------------------------------------------------------------------ a row's sums
+// Per lane: maximum, sum of 2^t and of 2^t |t|, t = (z - mx) * scale.
+struct Sums {
+  float mx;
+  double S, E;
+};
+__device__ inline float reference(float mx) { return mx == -INFINITY ? 0.f : mx; }
+__device__ inline Sums rescaled(Sums a, float mx, float scale) {      // to a maximum that is no smaller
+  const double d = fmax((double)((reference(a.mx) - reference(mx)) * scale), -2000.0);
+  if (a.mx == -INFINITY || a.mx == mx) { a.mx = mx; return a; }
+  const double f = exp_neg_fast(d * 0.6931471805599453);
+  a.E = f * (a.E - d * a.S);
+  a.S = f * a.S;
+  a.mx = mx;
+  return a;
+}
+__device__ inline Sums wave_sums(Sums a, float scale) {
+  a = rescaled(a, wave_max(a.mx), scale);
+  a.S = wave_sum(a.S);
+  a.E = wave_sum(a.E);
+  return a;
+}
+
+// What the workgroups of a row hand to the last of them.
+struct Segment {
+  double S, E;
+  float mx, pad;
+  key_t top[OT_MAX_TOP];
+};
+
+template <typename T> struct Vec;
+template <> struct Vec<float> {
+  static constexpr int kElems = 4;
+  typedef float Raw __attribute__((ext_vector_type(4)));
+  __device__ static void unpack(const Raw& x, float* v) { v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; }
+  __device__ static float one(const float* p) { return *p; }
+};
+template <> struct Vec<uint16_t> {
+  static constexpr int kElems = 8;
+  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
+  __device__ static void unpack(const Raw& x, float* v) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(x[i] << 16);
+      v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
+    }
   }
-  S = wave_sum(S); E = wave_sum(E);
-  if (lane == 0) { s_d[0][wave] = S; s_d[1][wave] = E; }
+  __device__ static float one(const uint16_t* p) { return bf16_to_f32(*p); }
+};
+
+// Sum of n values, the deepest of them log2 n additions deep.
+template <int n>
+__device__ inline float tree_sum(const float* x) {
+  if constexpr (n == 1) return x[0];
+  else return tree_sum<n / 2>(x) + tree_sum<n - n / 2>(x + n / 2);
+}
+
+// kPer logits per lane into the running sums and the sorted list of the best.  id0 + id_of(e): the id of the lane's element e, ascending in e.
+// masked: elements may be -inf because they are past the row's end.
+template <int kPer, bool kTop, typename IdFn>
+__device__ __forceinline__ void take(const float* v, float scale, int n_top, int lane, int lowest_id, IdFn id_of, Sums* a, key_t* list) {
+  float mx = v[0];
+#pragma unroll
+  for (int e = 1; e < kPer; ++e) mx = fmaxf(mx, v[e]);
+  if (__any(mx > a->mx)) *a = rescaled(*a, fmaxf(mx, a->mx), scale);
+  const float ref = reference(a->mx);
+  constexpr int kBatch = kPer < 16 ? kPer : 16;
+#pragma unroll
+  for (int e0 = 0; e0 < kPer; e0 += kBatch) {
+    float ex[kBatch], en[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int e = 0; e < kBatch; ++e) {
+      const float t = (v[e0 + e] - ref) * scale;
+      ex[e] = __builtin_amdgcn_exp2f(t);
+      en[e & 3] = fmaf(ex[e], fmaxf(t, -200.f), en[e & 3]);
+    }
+    a->S += (double)tree_sum<kBatch>(ex);
+    a->E -= (double)((en[0] + en[1]) + (en[2] + en[3]));
+  }
+  if constexpr (kTop) {
+    key_t last = lane_key(*list, n_top - 1);
+    float bar = key_logit(last);
+    // Ids in front of the last of the list win where the logits are equal.
+    const bool earlier = last != 0 && lowest_id < key_id(last);
+    const unsigned long long hit = __ballot(earlier ? mx >= bar : mx > bar);
+    if (hit == 0) return;
+    int taken = -1;
+    if (__popcll(hit) > 6) {                             // many: every lane's best at once
+      int at = 0;
+#pragma unroll
+      for (int e = kPer - 1; e >= 0; --e) at = v[e] == mx ? e : at;
+      taken = at;
+      *list = merge_keys(*list, __shfl(sort_keys(order_key(mx, id_of(at)), lane), 63 - lane), lane);
+      last = lane_key(*list, n_top - 1);
+      bar = key_logit(last);
+    }
+    const float least = earlier || taken >= 0 ? bar : nextafterf(bar, INFINITY);
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {                     // and what else is above the bar, one by one
+      unsigned long long more = __ballot(v[e] >= least && v[e] > -INFINITY && e != taken);
+      while (more) {
+        const int l = (int)__builtin_ctzll(more);
+        more &= more - 1;
+        const key_t k = lane_key(order_key(v[e], id_of(e)), l);
+        if (k > last) {
+          *list = insert_key(*list, k, lane);
+          last = lane_key(*list, n_top - 1);
+        }
+      }
+    }
+  }
+}
+
+// Grid = segments x rows; a wavefront takes whole tiles of 64 * kPer logits of its segment, one after the other.  Rows start at any element:
+// the tiles are laid out from the first 16-byte boundary on, and the elements in front of it and behind the last whole vector go, one a
+// lane, with the first wavefront of the first segment.
+template <typename T, int kPer, bool kTop>
+__global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a, int segments, int tiles_per_wave, Segment* part, int32_t* count) {
+  typedef typename Vec<T>::Raw Raw;
+  constexpr int kVec = Vec<T>::kElems, kLoads = kPer / kVec;
+  const ot_logprob_in& in = a.in;
+  const int row = (int)(blockIdx.x / (unsigned)segments), seg = (int)(blockIdx.x % (unsigned)segments);
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  __shared__ Sums s_sums[4];
+  __shared__ key_t s_list[3][64];
+  const T* z = static_cast<const T*>(row_of(in, row));
+  const bool skip = in.given_rows_only && !any_given(in, row);
+  if (skip && seg > 0) return;                           // such a row's first workgroup writes what is left
+  const int V = skip ? 0 : in.V;
+  const int head = min(V, (int)((kVec - ((reinterpret_cast<uintptr_t>(z) / sizeof(T)) & (kVec - 1))) & (kVec - 1)));
+  const int vecs = (V - head) / kVec, tail = V - head - vecs * kVec;
+  const Raw* zv = reinterpret_cast<const Raw*>(z + head);
+  Sums own{-INFINITY, 0.0, 0.0};
+  key_t list = 0;
+  const float scale = kLog2e / row_temperature(in, row, lane);
+  int tile = (seg * 4 + wave) * tiles_per_wave;
+  const int end = min(tile + tiles_per_wave, (vecs + 64 * kLoads - 1) / (64 * kLoads));
+  if (seg == 0 && wave == 0 && head + tail > 0) {
+    const int id = lane < head ? lane : V - tail + lane - head;
+    const float v = lane < head + tail ? Vec<T>::one(z + id) : -INFINITY;
+    take<1, kTop>(&v, scale, in.n_top, lane, 0, [&](int) { return id; }, &own, &list);
+  }
+  for (; tile < end; ++tile) {
+    const int first = tile * 64 * kLoads + lane;
+    Raw raw[kLoads];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) raw[i] = __builtin_nontemporal_load(zv + min(first + i * 64, vecs - 1));
+    float v[kPer];
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) Vec<T>::unpack(raw[i], v + i * kVec);
+    if ((tile + 1) * 64 * kLoads > vecs) {
+#pragma unroll
+      for (int i = 0; i < kLoads; ++i)
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) v[i * kVec + e] = first + i * 64 < vecs ? v[i * kVec + e] : -INFINITY;
+    }
+    take<kPer, kTop>(v, scale, in.n_top, lane, head + tile * 64 * kLoads * kVec,
+                     [&](int e) { return head + (first + e / kVec * 64) * kVec + e % kVec; }, &own, &list);
+  }
+  own = wave_sums(own, scale);
+  if (lane == 0) s_sums[wave] = own;
+  if (kTop && wave > 0) s_list[wave - 1][63 - lane] = list;
   __syncthreads();
-  S = s_d[0][0] + s_d[0][1] + s_d[0][2] + s_d[0][3];
-  E = s_d[1][0] + s_d[1][1] + s_d[1][2] + s_d[1][3];
-  const double lnS = log(S);
+  if (wave != 0) return;
+  Sums all = lane < 4 ? s_sums[lane] : Sums{-INFINITY, 0.0, 0.0};
+  all = wave_sums(all, scale);
+  if constexpr (kTop) {
+#pragma unroll
+    for (int w = 0; w < 3; ++w) list = merge_keys(list, s_list[w][lane], lane);
+  }
+  if (segments > 1 && !skip) {
+    Segment* mine = part + (int64_t)row * segments + seg;
+    if (lane == 0) {
+      publish(&mine->S, all.S);
+      publish(&mine->E, all.E);
+      publish(reinterpret_cast<int32_t*>(&mine->mx), (int32_t)__float_as_int(all.mx));
+    }
+    if (kTop && lane < in.n_top) publish(reinterpret_cast<double*>(&mine->top[lane]), __longlong_as_double((long long)list));
+    stores_done();
+    int last = 0;
+    if (lane == 0) last = arrive(count + row, segments);
+    if (!uniform(last)) return;
+    Segment* others = part + (int64_t)row * segments;
+    all = Sums{-INFINITY, 0.0, 0.0};
+    for (int s0 = 0; s0 < segments; s0 += 64) {
+      Sums x{-INFINITY, 0.0, 0.0};
+      if (s0 + lane < segments) {
+        x.mx = __int_as_float(observe(reinterpret_cast<int32_t*>(&others[s0 + lane].mx)));
+        x.S = observe(&others[s0 + lane].S);
+        x.E = observe(&others[s0 + lane].E);
+      }
+      x = wave_sums(x, scale);
+      const float mx = fmaxf(all.mx, x.mx);
+      all = rescaled(all, mx, scale);
+      x = rescaled(x, mx, scale);
+      all.S += x.S;
+      all.E += x.E;
+    }
+    if constexpr (kTop) {
+      list = 0;
+      const int mirrored = 63 - lane;
+      for (int s = 0; s < segments; ++s) {
+        key_t other = 0;
+        if (mirrored < in.n_top) other = (key_t)__double_as_longlong(observe(reinterpret_cast<double*>(&others[s].top[mirrored])));
+        list = merge_keys(list, other, lane);
+      }
+    }
+  }
+  // the row's results, by one wavefront
+  const double S = all.S, lnS = log(S), mx = (double)all.mx, temp = (double)row_temperature(in, row, lane);
   const float invalid = S == 0.0 ? -INFINITY : kNan;      // of a row without a distribution
   const bool valid = S > 0.0 && S < 1e300;
-  if (tid == 0) {
-    if (a.out.entropy) a.out.entropy[row] = valid ? (float)(lnS + E / S * 0.6931471805599453) : S == 0.0 ? 0.f : kNan;
-    if (a.out.row_max) { a.out.row_max[row] = mx; a.out.row_sumexp[row] = valid || S == 0.0 ? (float)S : kNan; }
+  if (lane == 0) {
+    if (a.out.entropy) a.out.entropy[row] = valid ? (float)(lnS + all.E / S * 0.6931471805599453) : S == 0.0 ? 0.f : kNan;
+    if (a.out.row_max) { a.out.row_max[row] = all.mx; a.out.row_sumexp[row] = valid || S == 0.0 ? (float)S : kNan; }
   }
-  for (int i = tid; i < in.n_tok; i += 256) {
+  for (int i = lane; i < in.n_tok; i += 64) {
     const int t = in.tokens[(int64_t)row * in.n_tok + i];
     float lp = 0.f;
     if (t < -1 || t >= in.V) lp = kNan;
-    else if (t >= 0) lp = valid ? (float)(((double)logit(z, in.dtype, t) - (double)mx) / (double)T - lnS) : invalid;
+    else if (t >= 0) lp = valid ? (float)(((double)Vec<T>::one(z + t) - mx) / temp - lnS) : invalid;
     a.out.logprob[(int64_t)row * in.n_tok + i] = lp;
   }
-  unsigned long long below = ~0ull;
-  for (int n = 0; n < in.n_top; ++n) {
-    unsigned long long best = 0;
-    if (valid)
-      for (int v = tid; v < V; v += 256) {
-        const unsigned long long k = order_key(logit(z, in.dtype, v), v);
-        if (k < below && k > best) best = k;
-      }
-    best = wave_max(best);
-    __syncthreads();
-    if (lane == 0) s_k[wave] = best;
-    __syncthreads();
-    for (int w = 0; w < 4; ++w) best = s_k[w] > best ? s_k[w] : best;
-    if (tid == 0) {
-      const int id = best ? (int)(0xFFFFFFFFu - (uint32_t)best) : -1;
-      a.out.top_ids[(int64_t)row * in.n_top + n] = id;
-      a.out.top_logprobs[(int64_t)row * in.n_top + n] =
-          best ? (float)(((double)logit(z, in.dtype, id) - (double)mx) / (double)T - lnS) : -INFINITY;
-    }
-    below = best ? best : 0;
+  if (kTop && lane < in.n_top) {
+    const bool some = valid && list != 0;
+    a.out.top_ids[(int64_t)row * in.n_top + lane] = some ? key_id(list) : -1;
+    a.out.top_logprobs[(int64_t)row * in.n_top + lane] = some ? (float)(((double)key_logit(list) - mx) / temp - lnS) : -INFINITY;
   }
 }
 
@@ -159,6 +375,22 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradArgs a, in
   }
 }
 
+// Segments of a row: as many workgroups as the chip holds at a time, each wavefront of them with one tile at least; of the rows whose
+// workgroups meet in memory there are at most kLogprobSegments segments.
+template <typename T, int kPer>
+hipError_t launch_logprobs(const ot_ctx* ctx, const LogprobArgs& a, hipStream_t stream) {
+  const int tiles = std::max(1, ceil_div(a.in.V, 64 * kPer)), want = ceil_div(4 * ctx->n_cu, a.in.M);
+  int segments = std::max(1, std::min({want, ceil_div(tiles, 4), kLogprobSegments / a.in.M}));
+  const int tiles_per_wave = ceil_div(tiles, 4 * segments);
+  segments = ceil_div(tiles, 4 * tiles_per_wave);
+  const dim3 grid((unsigned)segments * (unsigned)a.in.M);
+  if (a.in.n_top > 0)
+    hipLaunchKernelGGL((logprob_kernel<T, kPer, true>), grid, dim3(256), 0, stream, a, segments, tiles_per_wave, static_cast<Segment*>(ctx->lp_part), ctx->lp_count);
+  else
+    hipLaunchKernelGGL((logprob_kernel<T, kPer, false>), grid, dim3(256), 0, stream, a, segments, tiles_per_wave, static_cast<Segment*>(ctx->lp_part), ctx->lp_count);
+  return hipGetLastError();
+}
+
 int check_in(const ot_ctx* ctx, const ot_logprob_in* in, const char* who) {
   if (in->dtype != OT_BF16 && in->dtype != OT_F32) return ot_fail(OT_ERR_DTYPE, "%s: logits are OT_BF16 or OT_F32 (%d)", who, in->dtype);
   if (in->M < 0 || in->V < 1 || in->n_tok < 0 || in->ld < in->V)
@@ -173,6 +405,9 @@ int check_in(const ot_ctx* ctx, const ot_logprob_in* in, const char* who) {
 }
 
 }  // namespace
+
+size_t logprob_segment_bytes() { return sizeof(Segment); }
+
 }  // namespace otv
 
 using namespace otv;
@@ -187,8 +422,11 @@ int ot_token_logprobs(ot_ctx* ctx, const ot_logprob_in* in, ot_logprob_out* out)
   if ((in->n_tok > 0 && !out->logprob) || (in->n_top > 0 && (!out->top_ids || !out->top_logprobs)))
     return ot_fail(OT_ERR_NULL, "ot_token_logprobs: logprob, top_ids and top_logprobs are required where they have entries");
   if (!out->row_max != !out->row_sumexp) return ot_fail(OT_ERR_NULL, "ot_token_logprobs: row_max and row_sumexp come together");
-  hipLaunchKernelGGL(logprob_kernel, dim3((unsigned)in->M), dim3(256), 0, ctx->stream, LogprobArgs{*in, *out});
-  const hipError_t e = hipGetLastError();
+  const LogprobArgs a{*in, *out};
+  const bool few = (int64_t)in->M * in->V < (int64_t)ctx->n_cu * 8192;
+  hipError_t e;
+  if (in->dtype == OT_BF16) e = few ? launch_logprobs<uint16_t, 16>(ctx, a, ctx->stream) : launch_logprobs<uint16_t, 64>(ctx, a, ctx->stream);
+  else e = few ? launch_logprobs<float, 16>(ctx, a, ctx->stream) : launch_logprobs<float, 64>(ctx, a, ctx->stream);
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_token_logprobs: launch");
 }
 

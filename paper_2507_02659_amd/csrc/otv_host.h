@@ -45,6 +45,8 @@ struct ot_ctx {
   int32_t* loss_count = nullptr;      // [max_rows + 1] arrival counters of the loss launch, 0 between launches
   int32_t* adapt_count = nullptr;     // arrival counter of the adaptive-drafting launch, 0 between launches
   double* adapt_part = nullptr;       // [max_batch, 2] per-sequence partials of the acceptance head's loss
+  void* lp_part = nullptr;            // [kLogprobSegments] what the workgroups of a row of log-probabilities hand to the last of them
+  int32_t* lp_count = nullptr;        // [kLogprobSegments] their arrival counters, 0 between launches
   // profiling
   bool profiling = false;
   std::vector<hipEvent_t> events;   // OT_N_STAGES + 1 per pending step

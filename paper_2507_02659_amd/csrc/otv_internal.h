@@ -26,6 +26,8 @@ constexpr int64_t packed_tile_units(int nks) { return (int64_t)nks * 256 + kGemm
 constexpr int64_t packed_f32_tile_units(int nkb) { return (int64_t)nkb * 256 + kGemmTileGapUnits; }
 constexpr int kLossGroups = 64;      // workgroups per row of the distillation loss at most: a wavefront adds their sums
 
+constexpr int kLogprobSegments = 4096;  // workgroups of the log-probabilities' rows that are split, at most
+
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ------------------------------------------------------------------------------------------------ n-gram table
@@ -232,6 +234,7 @@ bool lmhead_f32_hosts_draft_side(int M, int d, int V_t, int B, int K, int V_d, i
 hipError_t launch_qhead(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream);
 hipError_t launch_pack_quant(const uint8_t* codes, const void* scales, int scale_f16, const uint8_t* zeros, int group, int d, int V_t, const QuantHead& q,
                              uint4* packed, uint32_t* recs, hipStream_t stream);
+size_t logprob_segment_bytes();       // of one of ot_ctx::lp_part (logprobs.hip)
 hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream);
 hipError_t launch_softmax_stats(const StepArgs& a, hipStream_t stream);
 // translation, acceptance test and the draw of the final tokens
