@@ -21,9 +21,6 @@ struct LogprobArgs {
   ot_logprob_out out;
 };
 
-__device__ inline float logit(const void* row, int dtype, int64_t v) {
-  return dtype == OT_BF16 ? bf16_to_f32(static_cast<const uint16_t*>(row)[v]) : static_cast<const float*>(row)[v];
-}
 __device__ inline const void* row_of(const ot_logprob_in& in, int64_t row) {
   return static_cast<const char*>(in.logits) + row * in.ld * (in.dtype == OT_BF16 ? 2 : 4);
 }
@@ -104,13 +101,13 @@ __device__ inline key_t insert_key(key_t list, key_t k, int lane) {
 }
 
 // ------------------------------------------------------------------------------------------------ a row's sums
-// Per lane: maximum, sum of 2^t and of 2^t |t|, t = (z - mx) * scale.
+// Sums of 2^t and of -2^t t, t = (z - mx) * scale, with a reference mx near the largest logit (-inf: of none).
 struct Sums {
   float mx;
   double S, E;
 };
 __device__ inline float reference(float mx) { return mx == -INFINITY ? 0.f : mx; }
-__device__ inline Sums rescaled(Sums a, float mx, float scale) {      // to a maximum that is no smaller
+__device__ inline Sums rescaled(Sums a, float mx, float scale) {      // to another reference
   const double d = fmax((double)((reference(a.mx) - reference(mx)) * scale), -2000.0);
   if (a.mx == -INFINITY || a.mx == mx) { a.mx = mx; return a; }
   const double f = exp_neg_fast(d * 0.6931471805599453);
@@ -160,14 +157,15 @@ __device__ inline float tree_sum(const float* x) {
   else return tree_sum<n / 2>(x) + tree_sum<n - n / 2>(x + n / 2);
 }
 
-// kPer logits per lane into the running sums and the sorted list of the best.  id0 + id_of(e): the id of the lane's element e, ascending in e.
-// masked: elements may be -inf because they are past the row's end.
-template <int kPer, bool kTop, typename IdFn>
-__device__ __forceinline__ void take(const float* v, float scale, int n_top, int lane, int lowest_id, IdFn id_of, Sums* a, key_t* list) {
+// kPer logits per lane into the lane's running sums (-inf: none); returns the largest.  The sums' reference is one for the wavefront and
+// moves, in 64 bits, only when a logit is more than 4 above it in the exponent: with a lane's own maximum for it nearly every tile moved one
+// (144 rows x 128256 ids 17.2 us, 2000 x 32003 in bf16 30.5).
+template <int kPer>
+__device__ __forceinline__ float add_logits(const float* v, float scale, Sums* a) {
   float mx = v[0];
 #pragma unroll
   for (int e = 1; e < kPer; ++e) mx = fmaxf(mx, v[e]);
-  if (__any(mx > a->mx)) *a = rescaled(*a, fmaxf(mx, a->mx), scale);
+  if (__any((mx - a->mx) * scale > 4.f)) *a = rescaled(*a, fmaxf(wave_max(mx), a->mx), scale);
   const float ref = reference(a->mx);
   constexpr int kBatch = kPer < 16 ? kPer : 16;
 #pragma unroll
@@ -182,117 +180,187 @@ __device__ __forceinline__ void take(const float* v, float scale, int n_top, int
     a->S += (double)tree_sum<kBatch>(ex);
     a->E -= (double)((en[0] + en[1]) + (en[2] + en[3]));
   }
-  if constexpr (kTop) {
-    key_t last = lane_key(*list, n_top - 1);
-    float bar = key_logit(last);
-    // Ids in front of the last of the list win where the logits are equal.
-    const bool earlier = last != 0 && lowest_id < key_id(last);
-    const unsigned long long hit = __ballot(earlier ? mx >= bar : mx > bar);
-    if (hit == 0) return;
-    int taken = -1;
-    if (__popcll(hit) > 6) {                             // many: every lane's best at once
-      int at = 0;
+  return mx;
+}
+
+// kPer values per lane, by a whole wavefront, into the sorted list whose first n count (-inf: none).  id_of(e): the id of the lane's value e,
+// ascending in e; ids of different lanes and calls come in any order.  n values of the row, at least, are known not to be below `least`.
+template <int kPer, typename IdFn>
+__device__ __forceinline__ void select(const float* v, int n, float least, int lane, IdFn id_of, key_t* list) {
+  float mx = v[0];
 #pragma unroll
-      for (int e = kPer - 1; e >= 0; --e) at = v[e] == mx ? e : at;
-      taken = at;
-      *list = merge_keys(*list, __shfl(sort_keys(order_key(mx, id_of(at)), lane), 63 - lane), lane);
-      last = lane_key(*list, n_top - 1);
-      bar = key_logit(last);
-    }
-    const float least = earlier || taken >= 0 ? bar : nextafterf(bar, INFINITY);
+  for (int e = 1; e < kPer; ++e) mx = fmaxf(mx, v[e]);
+  key_t last = lane_key(*list, n - 1);
+  least = fmaxf(least, -3.402823466e38f);
+  float bar = fmaxf(key_logit(last), least);             // below it, or at it with a higher id, nothing changes the first n
+  const unsigned long long hit = __ballot(mx >= bar);
+  if (hit == 0) return;
+  int taken = -1;
+  if (__popcll(hit) > 6) {                               // many: every lane's best at once
+    int at = 0;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {                     // and what else is above the bar, one by one
-      unsigned long long more = __ballot(v[e] >= least && v[e] > -INFINITY && e != taken);
-      while (more) {
-        const int l = (int)__builtin_ctzll(more);
-        more &= more - 1;
-        const key_t k = lane_key(order_key(v[e], id_of(e)), l);
-        if (k > last) {
-          *list = insert_key(*list, k, lane);
-          last = lane_key(*list, n_top - 1);
-        }
+    for (int e = kPer - 1; e >= 0; --e) at = v[e] == mx ? e : at;
+    taken = at;
+    const key_t best = sort_keys(order_key(mx, id_of(at)), lane);
+    *list = last == 0 && lane_key(*list, 0) == 0 ? best : merge_keys(*list, __shfl(best, 63 - lane), lane);
+    last = lane_key(*list, n - 1);
+    bar = fmaxf(key_logit(last), least);
+  }
+#pragma unroll
+  for (int e = 0; e < kPer; ++e) {                       // and what else is not below the bar, one by one
+    unsigned long long more = __ballot(v[e] >= bar && e != taken);
+    while (more) {
+      const int l = (int)__builtin_ctzll(more);
+      more &= more - 1;
+      const key_t k = lane_key(order_key(v[e], id_of(e)), l);
+      if (k > last) {
+        *list = insert_key(*list, k, lane);
+        last = lane_key(*list, n - 1);
       }
     }
   }
 }
+// The lists of a workgroup's wavefronts joined, two by two, in the first one; all of them call it.
+template <int kWaves>
+__device__ inline key_t join_lists(key_t list, key_t (*s_list)[64], int wave, int lane) {
+#pragma unroll
+  for (int step = 1; step < kWaves; step *= 2) {
+    if (wave % step == 0) s_list[wave][lane] = list;
+    __syncthreads();
+    if (wave % (2 * step) == 0) list = merge_keys(list, s_list[wave + step][63 - lane], lane);
+  }
+  return list;
+}
 
 // Grid = segments x rows; a wavefront takes whole tiles of 64 * kPer logits of its segment, one after the other.  Rows start at any element:
 // the tiles are laid out from the first 16-byte boundary on, and the elements in front of it and behind the last whole vector go, one a
-// lane, with the first wavefront of the first segment.
-template <typename T, int kPer, bool kTop>
-__global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a, int segments, int tiles_per_wave, Segment* part, int32_t* count) {
+// lane, with the first wavefront of the first segment.  The workgroup of a row that ends last joins the sums.
+//
+// The alternatives cost the pass nothing but the largest logit of every lane, which it has for the sums.  The n best of these maxima are n
+// logits of the segment, so its n best logits are not below the n-th of them, and only the lanes that reach it can hold any: the workgroup
+// selects those and reads what they have read once more, from a cache.
+template <typename T, int kPer, int kWaves, bool kTop>
+__global__ __launch_bounds__(64 * kWaves) void logprob_kernel(LogprobArgs a, int segments, int tiles_per_wave, Segment* part, int32_t* count) {
   typedef typename Vec<T>::Raw Raw;
   constexpr int kVec = Vec<T>::kElems, kLoads = kPer / kVec;
   const ot_logprob_in& in = a.in;
   const int row = (int)(blockIdx.x / (unsigned)segments), seg = (int)(blockIdx.x % (unsigned)segments);
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
-  __shared__ Sums s_sums[4];
-  __shared__ key_t s_list[3][64];
+  __shared__ Sums s_sums[kWaves];
+  __shared__ key_t s_list[kTop ? kWaves : 1][64];
+  __shared__ int s_last;
   const T* z = static_cast<const T*>(row_of(in, row));
   const bool skip = in.given_rows_only && !any_given(in, row);
   if (skip && seg > 0) return;                           // such a row's first workgroup writes what is left
   const int V = skip ? 0 : in.V;
   const int head = min(V, (int)((kVec - ((reinterpret_cast<uintptr_t>(z) / sizeof(T)) & (kVec - 1))) & (kVec - 1)));
-  const int vecs = (V - head) / kVec, tail = V - head - vecs * kVec;
+  const int vecs = (V - head) / kVec, tail = V - head - vecs * kVec, tiles = (vecs + 64 * kLoads - 1) / (64 * kLoads);
   const Raw* zv = reinterpret_cast<const Raw*>(z + head);
+  const int edge_id = lane < head ? lane : V - tail + lane - head;
+  const float temperature = row_temperature(in, row, lane), scale = kLog2e / temperature;
   Sums own{-INFINITY, 0.0, 0.0};
-  key_t list = 0;
-  const float scale = kLog2e / row_temperature(in, row, lane);
-  int tile = (seg * 4 + wave) * tiles_per_wave;
-  const int end = min(tile + tiles_per_wave, (vecs + 64 * kLoads - 1) / (64 * kLoads));
-  if (seg == 0 && wave == 0 && head + tail > 0) {
-    const int id = lane < head ? lane : V - tail + lane - head;
-    const float v = lane < head + tail ? Vec<T>::one(z + id) : -INFINITY;
-    take<1, kTop>(&v, scale, in.n_top, lane, 0, [&](int) { return id; }, &own, &list);
-  }
-  for (; tile < end; ++tile) {
-    const int first = tile * 64 * kLoads + lane;
-    Raw raw[kLoads];
+  const int tile0 = seg * kWaves * tiles_per_wave;        // of the segment: wavefront w takes tile0 + w, tile0 + kWaves + w, ...
+  int tile = tile0 + wave;
+  const int end = min(tile0 + kWaves * tiles_per_wave, tiles);
+  Raw raw[kLoads];
+  auto load = [&](int t, int l) {
 #pragma unroll
-    for (int i = 0; i < kLoads; ++i) raw[i] = __builtin_nontemporal_load(zv + min(first + i * 64, vecs - 1));
-    float v[kPer];
+    for (int i = 0; i < kLoads; ++i) raw[i] = zv[min(t * 64 * kLoads + l + i * 64, vecs - 1)];
+  };
+  auto unpack = [&](int t, int l, float* v) {            // -inf past the end
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) Vec<T>::unpack(raw[i], v + i * kVec);
-    if ((tile + 1) * 64 * kLoads > vecs) {
+    if ((t + 1) * 64 * kLoads > vecs) {
 #pragma unroll
       for (int i = 0; i < kLoads; ++i)
 #pragma unroll
-        for (int e = 0; e < kVec; ++e) v[i * kVec + e] = first + i * 64 < vecs ? v[i * kVec + e] : -INFINITY;
+        for (int e = 0; e < kVec; ++e) v[i * kVec + e] = t * 64 * kLoads + l + i * 64 < vecs ? v[i * kVec + e] : -INFINITY;
     }
-    take<kPer, kTop>(v, scale, in.n_top, lane, head + tile * 64 * kLoads * kVec,
-                     [&](int e) { return head + (first + e / kVec * 64) * kVec + e % kVec; }, &own, &list);
+  };
+  auto tile_id = [&](int t, int l, int e) { return head + (t * 64 * kLoads + l + e / kVec * 64) * kVec + e % kVec; };
+  if (tile < end) load(tile, lane);
+  // the given tokens' logits, which the last workgroup of the row needs at its end
+  int token = -1;
+  float token_logit = 0.f;
+  if (wave == 0 && lane < in.n_tok && V > 0) {
+    token = in.tokens[(int64_t)row * in.n_tok + lane];
+    if (token >= 0 && token < V) token_logit = Vec<T>::one(z + token);
   }
-  own = wave_sums(own, scale);
+  const bool edges = seg == 0 && wave == 0 && head + tail > 0;
+  float edge = -INFINITY, lane_max = -INFINITY;
+  if (edges) {
+    if (lane < head + tail) edge = Vec<T>::one(z + edge_id);
+    lane_max = add_logits<1>(&edge, scale, &own);
+  }
+  for (; tile < end; tile += kWaves) {
+    float v[kPer];
+    unpack(tile, lane, v);
+    if (tile + kWaves < end) load(tile + kWaves, lane);  // on its way while this one is taken
+    lane_max = fmaxf(lane_max, add_logits<kPer>(v, scale, &own));
+  }
+  Segment* parts = part + (int64_t)row * segments;
+  const bool split = segments > 1 && !skip;
+  own = wave_sums(rescaled(own, wave_max(lane_max), scale), scale);   // the true maximum from here on
   if (lane == 0) s_sums[wave] = own;
-  if (kTop && wave > 0) s_list[wave - 1][63 - lane] = list;
-  __syncthreads();
-  if (wave != 0) return;
-  Sums all = lane < 4 ? s_sums[lane] : Sums{-INFINITY, 0.0, 0.0};
-  all = wave_sums(all, scale);
+  key_t list = 0;
   if constexpr (kTop) {
+    // the lanes with the largest maxima, lane l of wavefront w as 64 w + l
+    list = join_lists<kWaves>(sort_keys(order_key(lane_max, tid), lane), s_list, wave, lane);
+    if (wave == 0) s_list[0][lane] = list;
+    __syncthreads();
+    const key_t holder = s_list[0][lane];
+    const float bar = key_logit(lane_key(holder, in.n_top - 1));
+    const key_t worst = lane_key(holder, 63);
+    __syncthreads();
+    list = 0;
+    if (worst != 0 && key_logit(worst) >= bar) {         // more lanes than the list holds reach the bar (equal logits): all of them
+      for (int t = tile0 + wave; t < end; t += kWaves) {
+        float v[kPer];
+        load(t, lane);
+        unpack(t, lane, v);
+        select<kPer>(v, in.n_top, bar, lane, [&](int e) { return tile_id(t, lane, e); }, &list);
+      }
+    } else {
+      const int l = key_id(holder) & 63, w = key_id(holder) >> 6;
+      const bool reaches = holder != 0 && key_logit(holder) >= bar;
+      for (int j = wave; j < tiles_per_wave; j += kWaves) {
+        const int t = tile0 + j * kWaves + w;
+        float v[kPer];
 #pragma unroll
-    for (int w = 0; w < 3; ++w) list = merge_keys(list, s_list[w][lane], lane);
-  }
-  if (segments > 1 && !skip) {
-    Segment* mine = part + (int64_t)row * segments + seg;
-    if (lane == 0) {
-      publish(&mine->S, all.S);
-      publish(&mine->E, all.E);
-      publish(reinterpret_cast<int32_t*>(&mine->mx), (int32_t)__float_as_int(all.mx));
+        for (int e = 0; e < kPer; ++e) v[e] = -INFINITY;
+        if (reaches && t < end) {
+          load(t, l);
+          unpack(t, l, v);
+        }
+        select<kPer>(v, in.n_top, bar, lane, [&](int e) { return tile_id(t, l, e); }, &list);
+      }
     }
-    if (kTop && lane < in.n_top) publish(reinterpret_cast<double*>(&mine->top[lane]), __longlong_as_double((long long)list));
-    stores_done();
-    int last = 0;
-    if (lane == 0) last = arrive(count + row, segments);
-    if (!uniform(last)) return;
-    Segment* others = part + (int64_t)row * segments;
+    if (edges) select<1>(&edge, in.n_top, bar, lane, [&](int) { return edge_id; }, &list);
+    list = join_lists<kWaves>(list, s_list, wave, lane);
+  }
+  __syncthreads();
+  Sums all = lane < kWaves ? s_sums[lane] : Sums{-INFINITY, 0.0, 0.0};
+  all = wave_sums(all, scale);
+  if (split) {
+    if (wave == 0) {
+      if (kTop && lane < in.n_top) publish(reinterpret_cast<double*>(&parts[seg].top[lane]), __longlong_as_double((long long)list));
+      if (lane == 0) {
+        publish(&parts[seg].S, all.S);
+        publish(&parts[seg].E, all.E);
+        publish(reinterpret_cast<int32_t*>(&parts[seg].mx), (int32_t)__float_as_int(all.mx));
+      }
+      stores_done();
+      if (lane == 0) s_last = arrive(count + row, segments);
+    }
+    __syncthreads();
+    if (!s_last) return;
     all = Sums{-INFINITY, 0.0, 0.0};
-    for (int s0 = 0; s0 < segments; s0 += 64) {
+    for (int s0 = 0; s0 < segments && wave == 0; s0 += 64) {
       Sums x{-INFINITY, 0.0, 0.0};
       if (s0 + lane < segments) {
-        x.mx = __int_as_float(observe(reinterpret_cast<int32_t*>(&others[s0 + lane].mx)));
-        x.S = observe(&others[s0 + lane].S);
-        x.E = observe(&others[s0 + lane].E);
+        x.mx = __int_as_float(observe(reinterpret_cast<int32_t*>(&parts[s0 + lane].mx)));
+        x.S = observe(&parts[s0 + lane].S);
+        x.E = observe(&parts[s0 + lane].E);
       }
       x = wave_sums(x, scale);
       const float mx = fmaxf(all.mx, x.mx);
@@ -301,18 +369,25 @@ __global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a, int segment
       all.S += x.S;
       all.E += x.E;
     }
-    if constexpr (kTop) {
+    if constexpr (kTop) {                                // wavefront w joins the lists of segments w, w + kWaves, ...
       list = 0;
       const int mirrored = 63 - lane;
-      for (int s = 0; s < segments; ++s) {
-        key_t other = 0;
-        if (mirrored < in.n_top) other = (key_t)__double_as_longlong(observe(reinterpret_cast<double*>(&others[s].top[mirrored])));
-        list = merge_keys(list, other, lane);
+      for (int s0 = wave; s0 < segments; s0 += 4 * kWaves) {
+        key_t other[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          other[j] = s0 + j * kWaves < segments && mirrored < in.n_top
+                         ? (key_t)__double_as_longlong(observe(reinterpret_cast<double*>(&parts[s0 + j * kWaves].top[mirrored]))) : 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (s0 + j * kWaves < segments) list = merge_keys(list, other[j], lane);
       }
+      list = join_lists<kWaves>(list, s_list, wave, lane);
     }
   }
+  if (wave != 0) return;
   // the row's results, by one wavefront
-  const double S = all.S, lnS = log(S), mx = (double)all.mx, temp = (double)row_temperature(in, row, lane);
+  const double S = all.S, lnS = log(S), mx = (double)all.mx, temp = (double)temperature;
   const float invalid = S == 0.0 ? -INFINITY : kNan;      // of a row without a distribution
   const bool valid = S > 0.0 && S < 1e300;
   if (lane == 0) {
@@ -320,10 +395,14 @@ __global__ __launch_bounds__(256) void logprob_kernel(LogprobArgs a, int segment
     if (a.out.row_max) { a.out.row_max[row] = all.mx; a.out.row_sumexp[row] = valid || S == 0.0 ? (float)S : kNan; }
   }
   for (int i = lane; i < in.n_tok; i += 64) {
-    const int t = in.tokens[(int64_t)row * in.n_tok + i];
+    if (i >= 64) {
+      token = in.tokens[(int64_t)row * in.n_tok + i];
+      if (token >= 0 && token < in.V) token_logit = Vec<T>::one(z + token);
+    }
+    const int t = token;
     float lp = 0.f;
     if (t < -1 || t >= in.V) lp = kNan;
-    else if (t >= 0) lp = valid ? (float)(((double)Vec<T>::one(z + t) - mx) / temp - lnS) : invalid;
+    else if (t >= 0) lp = valid ? (float)(((double)token_logit - mx) / temp - lnS) : invalid;
     a.out.logprob[(int64_t)row * in.n_tok + i] = lp;
   }
   if (kTop && lane < in.n_top) {
@@ -340,54 +419,118 @@ struct LogprobGradArgs {
   int64_t ld_grad;
 };
 
-__device__ inline uint16_t f32_to_bf16(float x) {         // to nearest, ties to even; NaN stays one
-  const uint32_t u = __float_as_uint(x);
-  return x != x ? 0x7FC0 : (uint16_t)((u + 0x7FFFu + (u >> 16 & 1u)) >> 16);
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+typedef float f32x2 __attribute__((ext_vector_type(2)));
+__device__ inline void store_one(float* p, float x) { *p = x; }
+__device__ inline void store_one(uint16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }   // to nearest
+__device__ inline void store_vec(float* p, const float* x) {
+  typedef float raw_t __attribute__((ext_vector_type(4)));
+  __builtin_nontemporal_store(raw_t{x[0], x[1], x[2], x[3]}, reinterpret_cast<raw_t*>(p));
+}
+__device__ inline void store_vec(uint16_t* p, const float* x) {
+  typedef uint32_t raw_t __attribute__((ext_vector_type(4)));
+  raw_t r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
+  __builtin_nontemporal_store(r, reinterpret_cast<raw_t*>(p));
 }
 
-// Grid = chunks x rows.
-constexpr int kGradChunk = 2048;
+// Grid = chunks x rows: 32 logits per thread, all asked for at once, whole vectors where the rows of the logits and of the gradient start at
+// the same place of a 16-byte unit, else one by one.  Bound by memory: a logit is read once, a gradient written once.
+constexpr int kGradChunk = 8192;
+template <typename T>
 __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradArgs a, int chunks) {
+  constexpr int kVec = Vec<T>::kElems, kLoads = kGradChunk / 256 / kVec;
   const ot_logprob_in& in = a.in;
-  const int row = blockIdx.x / chunks, v0 = (int)(blockIdx.x % chunks) * kGradChunk, tid = threadIdx.x, lane = tid & 63;
-  const void* z = row_of(in, row);
-  const float T = row_temperature(in, row, lane), scale = kLog2e / T, invT = 1.f / T;
+  const int row = (int)(blockIdx.x / (unsigned)chunks), tid = threadIdx.x, lane = tid & 63;
+  const T* z = static_cast<const T*>(row_of(in, row));
+  T* grad = static_cast<T*>(a.grad) + (int64_t)row * a.ld_grad;
+  const int shift = (int)(reinterpret_cast<uintptr_t>(z) / sizeof(T)) & (kVec - 1);
+  const bool vectors = ((int)(reinterpret_cast<uintptr_t>(grad) / sizeof(T)) & (kVec - 1)) == shift;
+  // thread's vector i holds ids v0 + 256 i kVec ..; of the row's first one the ids below 0, of its last one those past the end are nobody's
+  const int c0 = (int)(blockIdx.x % (unsigned)chunks) * kGradChunk - shift, v0 = c0 + tid * kVec;
+  auto whole = [&](int i) { const int at = v0 + i * 256 * kVec; return vectors && at >= 0 && at + kVec <= in.V; };
+  typename Vec<T>::Raw raw[kLoads];
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i)
+    if (whole(i)) raw[i] = __builtin_nontemporal_load(reinterpret_cast<const typename Vec<T>::Raw*>(z + v0 + i * 256 * kVec));
+  const float T_row = row_temperature(in, row, lane), scale = kLog2e / T_row, invT = 1.f / T_row;
   const float mx = a.row_max[row], S = a.row_sumexp[row];
-  const float lnS = logf(S), invS = 1.f / S, gH = a.grad_entropy ? a.grad_entropy[row] : 0.f, H = a.grad_entropy ? a.entropy[row] : 0.f;
-  float G = 0.f;
-  for (int i = 0; a.grad_logprob && i < in.n_tok; ++i) {
-    const int t = in.tokens[(int64_t)row * in.n_tok + i];
-    if (t >= 0 && t < in.V) G += a.grad_logprob[(int64_t)row * in.n_tok + i];
-  }
-  for (int v = v0 + tid; v < min(v0 + kGradChunk, in.V); v += 256) {
-    float out = 0.f;
-    if (S != 0.f) {
-      const float x = logit(z, in.dtype, v), t = (x - mx) * scale, p = __builtin_amdgcn_exp2f(t) * invS;
-      const float lp = fmaxf(t, -200.f) * 0.69314718f - lnS;
-      out = -p * (G + gH * (lp + H));
-      for (int i = 0; a.grad_logprob && i < in.n_tok; ++i)
-        if (in.tokens[(int64_t)row * in.n_tok + i] == v && x > -INFINITY) out += a.grad_logprob[(int64_t)row * in.n_tok + i];
-      out *= invT;
+  const float gH = a.grad_entropy ? a.grad_entropy[row] : 0.f, H = a.grad_entropy ? a.entropy[row] : 0.f;
+  const float invS = S == 0.f ? 0.f : invT / S, HS = H - logf(S);
+  float v[kGradChunk / 256];
+  auto mine = [&](int i, int e) { return v0 + i * 256 * kVec + e; };
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    if (whole(i)) {
+      Vec<T>::unpack(raw[i], v + i * kVec);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[i * kVec + e] = mine(i, e) >= 0 && mine(i, e) < in.V ? Vec<T>::one(z + mine(i, e)) : -INFINITY;
     }
-    const int64_t at = (int64_t)row * a.ld_grad + v;
-    if (in.dtype == OT_BF16) static_cast<uint16_t*>(a.grad)[at] = f32_to_bf16(out);
-    else static_cast<float*>(a.grad)[at] = out;
+  }
+  const int n_tok = a.grad_logprob ? in.n_tok : 0;
+  double sum = 0.0;
+  for (int i = lane; i < n_tok; i += 64) {
+    const int t = in.tokens[(int64_t)row * in.n_tok + i];
+    if (t >= 0 && t < in.V) sum += a.grad_logprob[(int64_t)row * in.n_tok + i];
+  }
+  const float G = (float)wave_sum(sum);
+  float out[kGradChunk / 256];
+#pragma unroll
+  for (int i = 0; i < kGradChunk / 256; ++i) {
+    const float t = (v[i] - mx) * scale, p = __builtin_amdgcn_exp2f(t) * invS;   // over T
+    out[i] = -p * fmaf(gH, fmaf(fmaxf(t, -200.f), 0.69314718f, HS), G);
+  }
+  if (S != 0.f) {
+    for (int i0 = 0; i0 < n_tok; i0 += 64) {
+      int t = -1;
+      float g = 0.f;
+      if (i0 + lane < n_tok) {
+        t = in.tokens[(int64_t)row * in.n_tok + i0 + lane];
+        g = a.grad_logprob[(int64_t)row * in.n_tok + i0 + lane];
+      }
+      unsigned long long here = __ballot(t >= 0 && t >= c0 && t < min(c0 + kGradChunk, in.V));
+      while (here) {
+        const int l = (int)__builtin_ctzll(here);
+        here &= here - 1;
+        const int at = __builtin_amdgcn_readlane(t, l);
+        const float add = __int_as_float(__builtin_amdgcn_readlane(__float_as_int(g), l)) * invT;
+#pragma unroll
+        for (int i = 0; i < kGradChunk / 256; ++i)
+          if (mine(i / kVec, i % kVec) == at && v[i] > -INFINITY) out[i] += add;
+      }
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kGradChunk / 256; ++i) out[i] = 0.f;
+  }
+#pragma unroll
+  for (int i = 0; i < kLoads; ++i) {
+    if (whole(i)) {
+      store_vec(grad + v0 + i * 256 * kVec, out + i * kVec);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (mine(i, e) >= 0 && mine(i, e) < in.V) store_one(grad + mine(i, e), out[i * kVec + e]);
+    }
   }
 }
 
-// Segments of a row: as many workgroups as the chip holds at a time, each wavefront of them with one tile at least; of the rows whose
-// workgroups meet in memory there are at most kLogprobSegments segments.
-template <typename T, int kPer>
+// Workgroups of four wavefronts, two per compute unit where the rows are few enough to be split; a wavefront has one tile at least.  Of the
+// rows whose workgroups meet in memory there are at most kLogprobSegments segments.
+// Measured, us for 144 rows x 128256 ids with 20 alternatives / 2000 x 32003 in bf16 with 5: tiles of 16 logits per lane 24.3 / 39.5, of 32
+// 27.3 / 38.4; workgroups of 8 wavefronts 27.2 / 42.7, of 16 38.8 / 92; four per compute unit 26.6 / 39.4.
+constexpr int kPerLane = 16, kRowWaves = 4;
+template <typename T>
 hipError_t launch_logprobs(const ot_ctx* ctx, const LogprobArgs& a, hipStream_t stream) {
-  const int tiles = std::max(1, ceil_div(a.in.V, 64 * kPer)), want = ceil_div(4 * ctx->n_cu, a.in.M);
-  int segments = std::max(1, std::min({want, ceil_div(tiles, 4), kLogprobSegments / a.in.M}));
-  const int tiles_per_wave = ceil_div(tiles, 4 * segments);
-  segments = ceil_div(tiles, 4 * tiles_per_wave);
+  const int tiles = std::max(1, ceil_div(a.in.V, 64 * kPerLane)), want = ceil_div(2 * ctx->n_cu, a.in.M);
+  int segments = std::max(1, std::min({want, ceil_div(tiles, kRowWaves), kLogprobSegments / a.in.M}));
+  const int tiles_per_wave = ceil_div(tiles, kRowWaves * segments);
+  segments = ceil_div(tiles, kRowWaves * tiles_per_wave);
   const dim3 grid((unsigned)segments * (unsigned)a.in.M);
-  if (a.in.n_top > 0)
-    hipLaunchKernelGGL((logprob_kernel<T, kPer, true>), grid, dim3(256), 0, stream, a, segments, tiles_per_wave, static_cast<Segment*>(ctx->lp_part), ctx->lp_count);
-  else
-    hipLaunchKernelGGL((logprob_kernel<T, kPer, false>), grid, dim3(256), 0, stream, a, segments, tiles_per_wave, static_cast<Segment*>(ctx->lp_part), ctx->lp_count);
+  const auto kernel = a.in.n_top > 0 ? logprob_kernel<T, kPerLane, kRowWaves, true> : logprob_kernel<T, kPerLane, kRowWaves, false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(64 * kRowWaves), 0, stream, a, segments, tiles_per_wave, static_cast<Segment*>(ctx->lp_part), ctx->lp_count);
   return hipGetLastError();
 }
 
@@ -423,10 +566,7 @@ int ot_token_logprobs(ot_ctx* ctx, const ot_logprob_in* in, ot_logprob_out* out)
     return ot_fail(OT_ERR_NULL, "ot_token_logprobs: logprob, top_ids and top_logprobs are required where they have entries");
   if (!out->row_max != !out->row_sumexp) return ot_fail(OT_ERR_NULL, "ot_token_logprobs: row_max and row_sumexp come together");
   const LogprobArgs a{*in, *out};
-  const bool few = (int64_t)in->M * in->V < (int64_t)ctx->n_cu * 8192;
-  hipError_t e;
-  if (in->dtype == OT_BF16) e = few ? launch_logprobs<uint16_t, 16>(ctx, a, ctx->stream) : launch_logprobs<uint16_t, 64>(ctx, a, ctx->stream);
-  else e = few ? launch_logprobs<float, 16>(ctx, a, ctx->stream) : launch_logprobs<float, 64>(ctx, a, ctx->stream);
+  const hipError_t e = in->dtype == OT_BF16 ? launch_logprobs<uint16_t>(ctx, a, ctx->stream) : launch_logprobs<float>(ctx, a, ctx->stream);
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_token_logprobs: launch");
 }
 
@@ -441,10 +581,11 @@ int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logpro
   if (reinterpret_cast<uintptr_t>(grad) % (in->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: grad is not aligned to its type");
   if (grad == in->logits && ld_grad != in->ld) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: in place, ld_grad must be ld");
-  const int chunks = ceil_div(in->V, kGradChunk);
+  const int chunks = ceil_div((int64_t)in->V + 7, kGradChunk);   // a row starts up to 7 elements into its first vector
   if ((int64_t)chunks * in->M > 0x7FFFFFFF) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: %d rows of %d ids are too many for a launch", in->M, in->V);
   const LogprobGradArgs a{*in, fwd->row_max, fwd->row_sumexp, fwd->entropy, grad_logprob, grad_entropy, grad, ld_grad};
-  hipLaunchKernelGGL(logprob_grad_kernel, dim3((unsigned)(chunks * in->M)), dim3(256), 0, ctx->stream, a, chunks);
+  const auto kernel = in->dtype == OT_BF16 ? logprob_grad_kernel<uint16_t> : logprob_grad_kernel<float>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)chunks * (unsigned)in->M), dim3(256), 0, ctx->stream, a, chunks);
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_token_logprobs_grad: launch");
 }

@@ -261,15 +261,19 @@ class Verifier:
         return self._token_logprobs(given, tokens)
 
     def _token_logprobs(self, given, tokens) -> dict:
-        M, n_top = given.M, given.n_top
-        rows = self._empty((3, M), torch.float32)
-        out = {"entropy": rows[0], "row_max": rows[1], "row_sumexp": rows[2]}
+        # a call of one row is bound by the host: one allocation for all outputs, whose addresses are known without asking for them
+        M, n_top, n_tok = given.M, given.n_top, given.n_tok
+        at_top = (3 + n_tok) * M
+        memory = self._empty((at_top + 2 * n_top * M,), torch.float32)
+        p, one, part = memory.data_ptr(), (M,), memory.as_strided
+        out = {"entropy": part(one, (1,), 0), "row_max": part(one, (1,), M), "row_sumexp": part(one, (1,), 2 * M)}
         if tokens is not None:
-            out["logprob"] = self._empty(tokens.shape, torch.float32)
+            out["logprob"] = part(tokens.shape, (1,) if tokens.dim() == 1 else (n_tok, 1), 3 * M)
         if n_top:
-            out["top_ids"] = self._empty((M, n_top), torch.int32)
-            out["top_logprobs"] = self._empty((M, n_top), torch.float32)
-        ot.ot_token_logprobs(self.ctx, given, ot.make_logprob_out(out))
+            out["top_logprobs"] = part((M, n_top), (n_top, 1), at_top)
+            out["top_ids"] = memory.view(torch.int32).as_strided((M, n_top), (n_top, 1), at_top + n_top * M)
+        ot.ot_token_logprobs(self.ctx, given, ot.ot_logprob_out(p + 12 * M if n_tok else None, p, p + 4 * M, p + 8 * M, p + 4 * at_top if n_top else None,
+                                                                p + 4 * (at_top + n_top * M) if n_top else None))
         return out
 
     def token_logprobs_grad(self, logits: torch.Tensor, tokens: Optional[torch.Tensor], forward: dict, *, grad_logprob: Optional[torch.Tensor] = None,
