@@ -160,7 +160,7 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   ok = ok && dev_alloc(c, &c->drow_max, KQ) && dev_alloc(c, &c->drow_sum, KQ) && dev_alloc(c, &c->drow_arg, KQ);
   ok = ok && dev_alloc(c, &c->fin, Bm) && dev_alloc(c, &c->probe, Bm) &&
        dev_alloc(c, &c->dpiece, KQ * otv::kDraftPieces);
-  ok = ok && dev_alloc(c, &c->loss_part, R * kLossGroups);
+  ok = ok && dev_alloc(c, &c->loss_part, R * kLossGroups) && dev_alloc(c, &c->loss_mass_part, R * kLossGroups) && dev_alloc(c, &c->loss_mass, R);
   ok = ok && dev_alloc(c, &c->adapt_part, 2 * Bm);
   ok = ok && dev_alloc(c, &c->unit_mass, Bm * c->max_units);
   uint8_t* lp_part = nullptr;

@@ -64,6 +64,8 @@ struct LossArgs {
   float lambda; int32_t lambda_mode, ngram_term, accepted_only;
   // workspace
   double* part;          // [M, kLossGroups] sums of a row's groups
+  double* mass_part;     // the same of the mass below
+  double* mass;          // [M] for the gradient: the mass of q on the mapped draft ids, without Eq. 2's overrides
   int32_t* count;        // [M + 1] groups of a row that have delivered, and (first entry) rows that have; 0 between launches
   // outputs
   ot_loss_out out;
@@ -201,7 +203,8 @@ struct LossRowOffsets { int32_t v[kArgumentB + 1]; };
 // 0: the rows one after the other: ragged windows that would leave most places empty, and where the q' rows are wanted, which
 // every row's workgroups write (us per call, rows / places: 16 windows of 1 to 10 tokens x 50257 ids 20.2 / 20.9, 48 of them 35.2 / 36.7).
 // n_arrivals: rows, or places with a row, that are counted in.
-template <int kThreads>
+// kMass: also the sums that the gradient needs (kernels of their own: the values alone keep theirs).
+template <int kThreads, bool kMass>
 __global__ __launch_bounds__(kThreads, 4) void loss_kernel(LossArgs a, LossRowOffsets ro, int seq_rows, int n_arrivals, int groups,
                                                           int group_terms, int staged) {
   constexpr int kWaves = kThreads / 64;
@@ -277,7 +280,7 @@ __global__ __launch_bounds__(kThreads, 4) void loss_kernel(LossArgs a, LossRowOf
       }
     }
   }
-  double kl = 0.0;
+  double kl = 0.0, mass = 0.0;
   if (visit) {
     int lds_at = -1;
     if (staged && wave > 0) lds_at = stage_draft_row<kThreads - 64>(zq, a.dtype, a.V_d, tid - 64, 0);
@@ -308,6 +311,7 @@ __global__ __launch_bounds__(kThreads, 4) void loss_kernel(LossArgs a, LossRowOf
           if (kPlain || dv[e] >= 0) {
             lq = ((double)__uint_as_float(a.dtype == OT_BF16 ? xq[e] << 16 : xq[e]) - R.mxq) * R.invTd - R.lnSq;
             q = exp_neg_fast(lq);
+            if (kMass && (kPlain || (v != R.t_pre && v != R.t_ng && at + e * kThreads < i1))) mass += q;
           }
           if (!kPlain && v == R.t_pre) { q = R.q_pre; lq = R.ln_q_pre; }
           if (!kPlain && v == R.t_ng) { q = R.pi; lq = R.ln_pi; }   // the n-gram case of Eq. 2 wins when both name the same id
@@ -325,6 +329,7 @@ __global__ __launch_bounds__(kThreads, 4) void loss_kernel(LossArgs a, LossRowOf
     if (pairs && grp == 0 && tid == 0 && R.t_ng >= 0 && a.tmap[R.t_ng] < 0 && R.pi > 0.0)
       kl += R.pi * (R.ln_pi - (((double)z[R.t_ng] - R.mx) * R.invT - R.lnS));
     kl = need_kl ? block_sum<kWaves>(kl, s_term[0], wave, lane) : 0.0;
+    if (kMass && need_kl) mass = block_sum<kWaves>(mass, s_term[1], wave, lane);
   }
   if (wave == 0) {
     bool row_done = need_kl || grp == 0;
@@ -333,15 +338,18 @@ __global__ __launch_bounds__(kThreads, 4) void loss_kernel(LossArgs a, LossRowOf
       int last = 0;
       if (lane == 0) {
         publish(part + grp, kl);
+        if (kMass) publish(a.mass_part + (int64_t)row * groups + grp, mass);
         last = arrive(a.count + 1 + row, groups);
       }
       row_done = uniform(last) != 0;
       kl = row_done ? wave_sum(lane < groups ? observe(part + lane) : 0.0) : 0.0;   // a wavefront holds all groups
+      if (kMass) mass = row_done ? wave_sum(lane < groups ? observe(a.mass_part + (int64_t)row * groups + lane) : 0.0) : 0.0;
     }
     if (lane == 0) {
       s_last = 0;
       if (row_done) {
         publish(a.out.kl + row, need_kl ? kl : 0.0);
+        if (kMass) a.mass[row] = mass;
         s_last = arrive(a.count, n_arrivals);
       }
     }
@@ -386,7 +394,7 @@ using namespace otv;
 extern "C" {
 
 static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
-                     const ot_loss_config* cfg, ot_loss_out* out) {
+                     const ot_loss_config* cfg, ot_loss_out* out, bool with_mass) {
   if (!ctx || !in || !step || !cfg || !out) return ot_fail(OT_ERR_NULL, "ot_distill_loss: ctx, in, step_out, cfg and out must not be NULL");
   if (cfg->lambda_mode != OT_LAMBDA_FIXED && cfg->lambda_mode != OT_LAMBDA_TARGET_PROB)
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: unknown lambda_mode %d", cfg->lambda_mode);
@@ -418,7 +426,7 @@ static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step,
   a.n_mapped = step->n_mapped; a.n_accept = step->n_accept; a.mapped_ids = step->mapped_ids;
   a.span_start = step->span_start; a.span_len = step->span_len; a.p_tok = step->p_tok;
   a.lambda = cfg->lambda; a.lambda_mode = cfg->lambda_mode; a.ngram_term = cfg->ngram_term; a.accepted_only = cfg->accepted_only != 0;
-  a.part = ctx->loss_part; a.count = ctx->loss_count;
+  a.part = ctx->loss_part; a.mass_part = ctx->loss_mass_part; a.mass = ctx->loss_mass; a.count = ctx->loss_count;
   a.out = *out;
 
   hipStream_t st = ctx->stream;
@@ -438,7 +446,8 @@ static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step,
   const int places = seq_rows > 0 ? seq_rows * in->B : std::max(M, 1);
   const dim3 grid((unsigned)(p.groups * ceil_div(places, 8) * 8)), block(p.threads);
   const size_t lds = p.staged ? row_bytes : 16;
-  const auto kernel = p.threads == 1024 ? loss_kernel<1024> : p.threads == 512 ? loss_kernel<512> : loss_kernel<256>;
+  const auto kernel = with_mass ? (p.threads == 1024 ? loss_kernel<1024, true> : p.threads == 512 ? loss_kernel<512, true> : loss_kernel<256, true>)
+                                : (p.threads == 1024 ? loss_kernel<1024, false> : p.threads == 512 ? loss_kernel<512, false> : loss_kernel<256, false>);
   hipLaunchKernelGGL(kernel, grid, block, lds, st, a, ro, seq_rows, n_arrivals, p.groups, p.group_terms, p.staged);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return ot_fail_hip(e, "ot_distill_loss: launch");
@@ -447,7 +456,7 @@ static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step,
 
 int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
                     const ot_loss_config* cfg, ot_loss_out* out) {
-  return loss_impl(ctx, in, step, target_logits, cfg, out);
+  return loss_impl(ctx, in, step, target_logits, cfg, out, false);
 }
 
 int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
@@ -458,7 +467,7 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
     return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
   if (ctx && reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad is not aligned to its type");
-  const int bad = loss_impl(ctx, in, step, target_logits, cfg, out);
+  const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true);
   if (bad != OT_OK || in->B == 0) return bad;
   LossGradArgs a{};
   a.B = in->B; a.K = in->row_off_host[in->B] - in->B; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
@@ -468,7 +477,7 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
   a.Z = target_logits ? target_logits : ctx->Z; a.ldz = ctx->V_t;
   a.row_max = ctx->row_max; a.row_sum = ctx->row_sum; a.drow_max = ctx->drow_max; a.drow_sum = ctx->drow_sum;
   a.n_mapped = step->n_mapped; a.mapped_ids = step->mapped_ids; a.span_start = step->span_start; a.span_len = step->span_len;
-  a.kind = out->kind; a.kl = out->kl; a.weight = out->weight; a.totals = out->totals;
+  a.kind = out->kind; a.kl = out->kl; a.mass = ctx->loss_mass; a.weight = out->weight; a.totals = out->totals;
   a.grad_loss = grad_loss; a.grad = grad;
   const hipError_t e = launch_loss_grad(a, ctx->stream);
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_distill_loss_grad: launch");
