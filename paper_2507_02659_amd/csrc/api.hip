@@ -163,10 +163,12 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   ok = ok && dev_alloc(c, &c->loss_part, R * kLossGroups) && dev_alloc(c, &c->loss_mass_part, R * kLossGroups) && dev_alloc(c, &c->loss_mass, R);
   ok = ok && dev_alloc(c, &c->adapt_part, 2 * Bm);
   ok = ok && dev_alloc(c, &c->unit_mass, Bm * c->max_units);
-  uint8_t* lp_part = nullptr;
+  uint8_t *lp_part = nullptr, *grad_rows = nullptr;
+  ok = ok && dev_alloc(c, &grad_rows, KQ * loss_grad_row_bytes());
+  c->grad_rows = grad_rows;
   ok = ok && dev_alloc(c, &lp_part, kLogprobSegments * logprob_segment_bytes());
   c->lp_part = lp_part;
-  const size_t n_counters = 1 + (R + 1) + kLogprobSegments;   // of adaptive drafting, of the loss, of the log-probabilities
+  const size_t n_counters = 1 + (R + 1) + kLogprobSegments + 2;   // of adaptive drafting, the loss, the log-probabilities, the gradient
   ok = ok && dev_alloc(c, &c->counters, n_counters);
   if (!ok) { free_ctx(c); return fail(OT_ERR_NOMEM, "ot_verify_init: device allocation failed"); }
 
@@ -176,6 +178,7 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   c->adapt_count = c->counters;
   c->loss_count = c->adapt_count + 1;
   c->lp_count = c->loss_count + R + 1;
+  c->grad_count = c->lp_count + kLogprobSegments;
   if (e == hipSuccess) e = hipMemcpyAsync(c->dmap, cfg->direct_map, sizeof(int32_t) * c->V_d, hipMemcpyHostToDevice, c->stream);
   if (e == hipSuccess) e = hipMemcpyAsync(c->tmap, tmap_h.data(), sizeof(int32_t) * tmap_h.size(), hipMemcpyHostToDevice, c->stream);
   c->pairs = reinterpret_cast<const int2*>(c->tmap + pairs_at);

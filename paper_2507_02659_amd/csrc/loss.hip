@@ -394,7 +394,7 @@ using namespace otv;
 extern "C" {
 
 static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
-                     const ot_loss_config* cfg, ot_loss_out* out, bool with_mass) {
+                     const ot_loss_config* cfg, ot_loss_out* out, bool with_mass, bool check_only) {
   if (!ctx || !in || !step || !cfg || !out) return ot_fail(OT_ERR_NULL, "ot_distill_loss: ctx, in, step_out, cfg and out must not be NULL");
   if (cfg->lambda_mode != OT_LAMBDA_FIXED && cfg->lambda_mode != OT_LAMBDA_TARGET_PROB)
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: unknown lambda_mode %d", cfg->lambda_mode);
@@ -416,6 +416,8 @@ static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step,
   }
   const int M = in->B > 0 ? in->row_off_host[in->B] : 0;
   if (M - in->B > 0 && (!in->draft_logits || !in->draft_ids)) return ot_fail(OT_ERR_NULL, "ot_distill_loss: draft_logits and draft_ids must not be NULL");
+
+  if (check_only) return OT_OK;
 
   LossArgs a{};
   a.B = in->B; a.M = M; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
@@ -456,7 +458,7 @@ static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step,
 
 int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
                     const ot_loss_config* cfg, ot_loss_out* out) {
-  return loss_impl(ctx, in, step, target_logits, cfg, out, false);
+  return loss_impl(ctx, in, step, target_logits, cfg, out, false, false);
 }
 
 int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
@@ -467,7 +469,10 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
     return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
   if (ctx && reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad is not aligned to its type");
-  const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true);
+  // where the gradient's launches take rows of this size they do the loss's work as well (without the q' rows)
+  const bool in_one = ctx && in && out && in->B > 0 && in->row_off_host && !out->qprime &&
+                      loss_grad_row_fits(in->row_off_host[in->B] - in->B, ctx->V_d);
+  const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, in_one);
   if (bad != OT_OK || in->B == 0) return bad;
   LossGradArgs a{};
   a.B = in->B; a.K = in->row_off_host[in->B] - in->B; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
@@ -479,7 +484,12 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
   a.n_mapped = step->n_mapped; a.mapped_ids = step->mapped_ids; a.span_start = step->span_start; a.span_len = step->span_len;
   a.kind = out->kind; a.kl = out->kl; a.mass = ctx->loss_mass; a.weight = out->weight; a.totals = out->totals;
   a.grad_loss = grad_loss; a.grad = grad;
-  const hipError_t e = launch_loss_grad(a, ctx->stream);
+  a.M = in->row_off_host[in->B]; a.n_pairs = ctx->n_pairs; a.pairs = ctx->pairs;
+  a.lambda_mode = cfg->lambda_mode; a.lambda = cfg->lambda; a.accepted_only = cfg->accepted_only != 0;
+  a.n_accept = step->n_accept; a.p_tok = step->p_tok;
+  a.rows = ctx->grad_rows; a.count = ctx->grad_count; a.n_tokens = ctx->grad_count + 1;
+  a.out = *out;
+  const hipError_t e = in_one ? launch_loss_and_grad(a, ctx->stream) : launch_loss_grad(a, ctx->stream);
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_distill_loss_grad: launch");
 }
 

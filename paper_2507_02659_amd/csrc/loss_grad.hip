@@ -201,6 +201,306 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
   }
 }
 
+// ------------------------------------------------------------------------------------------------ loss and gradient of a row in one workgroup
+// Where a row of draft ids fits LDS, 4 bytes each, and the q' rows are not wanted, two launches do the loss's work as well:
+//   loss_prepare_kernel  one wavefront per sequence: kinds, NLL and weights of its tokens, the number of drafted tokens considered (whole
+//                        numbers added by atomics: the order does not matter), and a record of what every draft row needs;
+//   loss_row_kernel      one workgroup per draft row.  It walks the mapped pairs in ascending target id, so that the target row is read in
+//                        order, and leaves each logit in LDS at its draft id; then it walks its draft row, which it holds in registers, for
+//                        q, r and their sums, and a second time for the gradient.  The last workgroup of all forms the loss's totals.
+// What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
+// sum q t gets the constants' part as their 64-bit difference times the mass of q.
+struct alignas(16) GradRow {
+  float mx, mxq;                // t = (zq - mxq) * s2q and (z - mx) * s2: exponents to base 2, scales as two floats
+  float s2, s2_lo, s2q, s2q_lo;
+  float inv_Sq, r0;             // q = 2^t / Sq;  r = (tq - t) ln 2 + r0, r0 = lnS - lnSq + 1
+  double dlnS;                  // lnS - lnSq
+  double c, D, a_pre;           // c and D without grad_loss / n
+  double kl_more, A_more;       // what Eq. 2's overrides add to the KL sum and to A
+  int32_t kind, row, sub, out, pre, pad[3];
+};
+static_assert(sizeof(GradRow) % 16 == 0, "read as 16-byte units");
+
+template <typename T>
+__global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
+  const int lane = threadIdx.x & 63, b = (int)blockIdx.x * 4 + uniform((int)threadIdx.x >> 6);
+  if (b >= a.B) return;
+  const int r0 = uniform(a.row_off[b]), r1 = uniform(a.row_off[b + 1]), q0 = r0 - b, k = r1 - r0 - 1;
+  const int r = min(r0 + lane, r1 - 1), q = q0 + max(0, min(lane, k - 1));
+  const float T_b = a.temperature[b], Td_b = a.draft_temperature ? a.draft_temperature[b] : T_b;
+  const int m = a.n_mapped[b], n_accept = a.n_accept[b], s = a.span_start[r], L = a.span_len[r], t = a.mapped_ids[r];
+  const float p_tok = a.p_tok[r], mx = a.row_max[r];
+  const double lnS = log(a.row_sum[r]);
+  int id = 0;
+  float mxq = 0.f;
+  double Sq = 1.0, lq = 0.0;
+  const double invT = 1.0 / (double)T_b, invTd = 1.0 / (double)Td_b;
+  const bool counts = T_b > 0.f && Td_b > 0.f;
+  if (k > 0 && counts && m > 0) {                        // (ids outside the vocabulary: nothing is mapped)
+    id = a.draft_ids[q];
+    mxq = a.drow_max[q];
+    Sq = a.drow_sum[q];
+    lq = ((double)Draft<T>::one(static_cast<const T*>(a.draft_logits) + (int64_t)q * a.V_d + id) - (double)mxq) * invTd - log(Sq);
+  }
+  const double lnSq = log(Sq);
+  // lane j: mapped token j
+  const bool mine = lane < k + 1;
+  int kind = 0;
+  if (mine && lane < m && counts) kind = L == 1 ? 1 : (!a.accepted_only || lane < n_accept) ? 2 : 0;
+  const int first = max(s, 0), d1 = __shfl(id, first);
+  double ln_pi = 0.0;
+  const double lq_first = __shfl(lq, first);
+  for (int l = 0; l < OT_MAX_NGRAM_LEN; ++l) {
+    const double x = __shfl(lq, min(first + l, 63));
+    if (l < L) ln_pi += x;
+  }
+  const double weight = kind != 2 ? 0.0 : a.lambda_mode == OT_LAMBDA_TARGET_PROB ? (double)p_tok : (double)a.lambda;
+  int n = kind == 1 ? 1 : kind == 2 ? L : 0;
+  double D = -weight * invTd, c = kind == 1 ? invTd : weight * invTd, a_pre = 0.0, kl_more = 0.0, A_more = 0.0;
+  int out = -1, pre = -1;
+  const bool ngram_kl = kind == 2 && a.approx_kl;
+  if (ngram_kl) {
+    const float* z = a.Z + (int64_t)r * a.ldz;
+    const int t_pre = a.dmap[d1];
+    out = a.tmap[t];
+    const double pi = exp(ln_pi), q_pre = -exp(lq_first) * expm1(ln_pi - lq_first);   // q(d_1) - pi, as in make_row
+    const double lp_ng = ((double)z[t] - (double)mx) * invT - lnS;
+    double pull = 0.0;
+    if (pi > 0.0) {
+      pull = ln_pi - lp_ng + 1.0;
+      kl_more = pi * (ln_pi - lp_ng);
+    }
+    if (t_pre >= 0 && t_pre != t) {
+      pre = d1;
+      if (q_pre > 0.0) {
+        const double lp_pre = ((double)z[t_pre] - (double)mx) * invT - lnS;
+        a_pre = log(q_pre) - lp_pre + 1.0;
+        pull -= a_pre;
+        kl_more += q_pre * (a_pre - 1.0);
+        A_more = exp(lq_first) * a_pre;
+      }
+    }
+    D = c * pi * pull;
+  }
+  if (mine) {
+    a.out.kind[r0 + lane] = kind;
+    a.out.nll[r0 + lane] = kind == 2 ? -ln_pi : 0.0;
+    a.out.weight[r0 + lane] = weight;
+    a.out.kl[r0 + lane] = 0.0;                           // of rows without a KL term; the others' workgroups write theirs
+  }
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) n += __shfl_xor(n, o);
+  if (lane == 0 && n > 0) __hip_atomic_fetch_add(a.n_tokens, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  // lane i: draft row i, covered by the last token that starts at or before it
+  unsigned long long starts = mine && lane < m ? 1ull << (first & 63) : 0ull;
+#pragma unroll
+  for (int o = 1; o < 64; o *= 2) starts |= __shfl_xor(starts, o);
+  const int j = max(0, (int)__popcll(starts & ((2ull << lane) - 1)) - 1);
+  const int s_j = __shfl(first, j), L_j = __shfl(L, j), kind_j = __shfl(kind, j);
+  const bool covered = (starts & ((2ull << lane) - 1)) != 0 && lane < s_j + L_j && kind_j != 0, is_first = lane == s_j;
+  GradRow R = {};
+  R.row = r0 + j;
+  R.mx = __shfl(mx, j); R.mxq = mxq;
+  const double s2 = 1.4426950408889634 * invT, s2q = 1.4426950408889634 * invTd;
+  R.s2 = (float)s2; R.s2_lo = (float)(s2 - (double)R.s2);
+  R.s2q = (float)s2q; R.s2q_lo = (float)(s2q - (double)R.s2q);
+  R.inv_Sq = (float)(1.0 / Sq);
+  R.dlnS = __shfl(lnS, j) - lnSq;
+  R.r0 = (float)(R.dlnS + 1.0);
+  R.c = __shfl(c, j); R.D = __shfl(D, j); R.a_pre = __shfl(a_pre, j);
+  R.kl_more = __shfl(kl_more, j); R.A_more = __shfl(A_more, j);
+  R.out = __shfl(out, j); R.pre = __shfl(pre, j); R.sub = id;
+  const int ngram_kl_j = __shfl((int)ngram_kl, j);
+  R.kind = !covered ? 0 : kind_j == 1 ? 1 : !ngram_kl_j ? 2 : is_first ? 3 : 2;
+  if (lane < k) static_cast<GradRow*>(a.rows)[q0 + lane] = R;
+}
+
+// The sums over all rows and the mean, by a workgroup.
+__device__ inline void grad_totals(const LossGradArgs& a, int tid, int wave, int lane, double (*s_term)[16]) {
+  double term[4] = {0.0, 0.0, 0.0, 0.0};                // direct, n-gram, direct tokens, n-gram sub-tokens
+  for (int row = tid; row < a.M; row += 1024) {
+    const int kind = a.out.kind[row];
+    const double kl = observe(a.out.kl + row), nll = a.out.nll[row], weight = a.out.weight[row];
+    if (kind == 1) {
+      term[0] += kl;
+      term[2] += 1.0;
+    } else if (kind == 2) {
+      term[1] += weight * (a.approx_kl ? kl : nll);
+      term[3] += (double)a.span_len[row];
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const double t = wave_sum(term[i]);
+    if (lane == 0) s_term[i][wave] = t;
+  }
+  __syncthreads();
+  if (wave != 0) return;
+  double t[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) t[i] = wave_sum(lane < 16 ? s_term[i][lane] : 0.0);
+  if (lane == 0) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) a.out.totals[i] = t[i];
+    a.out.totals[4] = (t[0] + t[1]) / fmax(1.0, t[2] + t[3]);
+  }
+}
+
+constexpr uint32_t kNoImage = 0x7FC0D0E5u;               // in LDS: the draft id has no image (a NaN that no arithmetic gives)
+constexpr int kRowThreads = 1024;
+template <typename T, int kVecs>
+__global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
+  typedef float f32x4 __attribute__((ext_vector_type(4)));
+  constexpr int kVec = Draft<T>::kElems, kEach = kVecs * kVec, kPairs = 8;
+  extern __shared__ __attribute__((aligned(16))) float s_z[];   // [shift + id]: the target's logit at the id's image, then r
+  __shared__ double s_term[4][16];
+  __shared__ int s_last;
+  const int drow = blockIdx.x, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  const T* zq = static_cast<const T*>(a.draft_logits) + (int64_t)drow * a.V_d;
+  T* grad = static_cast<T*>(a.grad) + (int64_t)drow * a.V_d;
+  const int shift = (int)(reinterpret_cast<uintptr_t>(zq) / sizeof(T)) & (kVec - 1);
+  const bool vectors = ((int)(reinterpret_cast<uintptr_t>(grad) / sizeof(T)) & (kVec - 1)) == shift;
+  const GradRow R = static_cast<const GradRow*>(a.rows)[drow];
+  const int n_tokens = *a.n_tokens;
+  const float up = a.grad_loss ? *a.grad_loss : 1.f;
+  const int v0 = tid * kVec - shift;                     // the thread's vector i holds ids v0 + i * kRowThreads * kVec ..
+  auto first = [&](int i) { return v0 + i * kRowThreads * kVec; };
+  auto whole = [&](int i) { return vectors && first(i) >= 0 && first(i) + kVec <= a.V_d; };
+  int2 id[kPairs], id_next[kPairs];
+  auto load_pairs = [&](int at, int2* to) {
+#pragma unroll
+    for (int e = 0; e < kPairs; ++e) to[e] = a.pairs[max(0, min(at + e * kRowThreads, a.n_pairs - 1))];
+  };
+  const bool has_kl = (R.kind & 1) && a.n_pairs > 0;
+  if (has_kl) load_pairs(tid, id);
+  float x[kEach];
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    if (whole(i)) {
+      Draft<T>::load(zq + first(i), x + i * kVec);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) x[i * kVec + e] = first(i) + e >= 0 && first(i) + e < a.V_d ? Draft<T>::one(zq + first(i) + e) : -INFINITY;
+    }
+  }
+  const float scale = up / (float)max(1, n_tokens), c = (float)R.c * scale, D = (float)R.D * scale;
+  auto q_of = [&](float zq_i, float* tq) {
+    const float d = fmaxf(zq_i - R.mxq, -1e30f);         // an id masked with -inf: q = 0, and no -inf times a low part of 0
+    *tq = fmaf(d, R.s2q, d * R.s2q_lo);
+    return __builtin_amdgcn_exp2f(*tq) * R.inv_Sq;
+  };
+  float A = 0.f;
+  if (R.kind & 1) {
+    const int slots = (a.V_d + shift + 3) / 4;
+    for (int i = tid; i < slots; i += kRowThreads) {
+      const float none = __uint_as_float(kNoImage);
+      reinterpret_cast<f32x4*>(s_z)[i] = f32x4{none, none, none, none};
+    }
+    __syncthreads();
+    const float* z = a.Z + (int64_t)R.row * a.ldz;
+    for (int at = tid; at - tid < a.n_pairs; at += kPairs * kRowThreads) {
+      float zv[kPairs];
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) zv[e] = z[id[e].x];
+      if (at - tid + kPairs * kRowThreads < a.n_pairs) load_pairs(at + kPairs * kRowThreads, id_next);
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e)
+        if (at + e * kRowThreads < a.n_pairs) s_z[shift + id[e].y] = zv[e];
+#pragma unroll
+      for (int e = 0; e < kPairs; ++e) id[e] = id_next[e];
+    }
+    __syncthreads();
+    double kl = 0.0, mass = 0.0;
+#pragma unroll
+    for (int i = 0; i < kVecs; ++i) {
+      const int base = (i * kRowThreads + tid) * kVec;   // slot of the vector's first id
+      if (base < shift + a.V_d) {
+        float zr[kVec], kl_i = 0.f, mass_i = 0.f;
+#pragma unroll
+        for (int e = 0; e < kVec; e += 4) {
+          const f32x4 w = *reinterpret_cast<const f32x4*>(s_z + base + e);
+#pragma unroll
+          for (int f = 0; f < 4; ++f) zr[e + f] = w[f];
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; ++e) {
+          const int v = base - shift + e, at = i * kVec + e;
+          float tq, r = 0.f;
+          const float q = q_of(x[at], &tq), d = zr[e] - R.mx;
+          if (v >= 0 && v < a.V_d && __float_as_uint(zr[e]) != kNoImage && v != R.out && v != R.pre && q > 0.f) {
+            if (d >= -1e20f) {
+              const float diff = (tq - fmaf(d, R.s2, d * R.s2_lo)) * 0.69314718f;
+              kl_i = fmaf(q, diff, kl_i);
+              r = diff + R.r0;
+            } else {                                     // masked by the target: with -inf the term is infinite, with a lowest number nearly
+              const double diff = ((double)tq - (double)d * (double)R.s2) * 0.6931471805599453;
+              kl += (double)q * diff;
+              r = d == -INFINITY ? INFINITY : (float)fmin(diff, 3.0e38);
+            }
+            mass_i += q;
+          }
+          if (!(d == d)) r = __float_as_uint(zr[e]) == kNoImage ? r : d;   // NaN stays one
+          if (v == R.pre) r = (float)R.a_pre;
+          zr[e] = r;
+          x[at] = q;
+        }
+#pragma unroll
+        for (int e = 0; e < kVec; e += 4) *reinterpret_cast<f32x4*>(s_z + base + e) = f32x4{zr[e], zr[e + 1], zr[e + 2], zr[e + 3]};
+        kl += (double)kl_i;
+        mass += (double)mass_i;
+      }
+    }
+    kl = wave_sum(kl);
+    mass = wave_sum(mass);
+    if (lane == 0) { s_term[0][wave] = kl; s_term[1][wave] = mass; }
+    __syncthreads();
+    kl = wave_sum(lane < 16 ? s_term[0][lane] : 0.0);
+    mass = wave_sum(lane < 16 ? s_term[1][lane] : 0.0);
+    kl += R.dlnS * mass;                                 // sum over ordinary ids of q (ln q - ln p)
+    A = (float)(kl + mass + R.A_more);
+    if (tid == 0) publish(a.out.kl + R.row, kl + R.kl_more);
+  }
+#pragma unroll
+  for (int i = 0; i < kVecs; ++i) {
+    const int base = (i * kRowThreads + tid) * kVec;
+    if (base >= shift + a.V_d) break;
+    float out[kVec];
+    if (R.kind & 1) {                                    // the thread's own words, which it wrote above
+#pragma unroll
+      for (int e = 0; e < kVec; e += 4) {
+        const f32x4 r = *reinterpret_cast<const f32x4*>(s_z + base + e);
+#pragma unroll
+        for (int f = 0; f < 4; ++f) {
+          const float q = x[i * kVec + e + f];
+          out[e + f] = q > 0.f ? c * q * (r[f] - A) : q;   // (NaN stays one)
+          if (R.kind & 2) out[e + f] = fmaf(D, (base - shift + e + f == R.sub ? 1.f : 0.f) - q, out[e + f]);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) {
+        float tq;
+        out[e] = R.kind ? D * ((base - shift + e == R.sub ? 1.f : 0.f) - q_of(x[i * kVec + e], &tq)) : 0.f;
+      }
+    }
+    if (whole(i)) {
+      Draft<T>::store(grad + first(i), out);
+    } else {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e)
+        if (first(i) + e >= 0 && first(i) + e < a.V_d) Draft<T>::store_one(grad + first(i) + e, out[e]);
+    }
+  }
+  __syncthreads();                                       // every wavefront has used the number of tokens
+  // this thread's word about the row has reached memory before it is counted in (arrive)
+  if (tid == 0) {
+    s_last = arrive(a.count, a.K);
+    if (s_last) publish(a.n_tokens, 0);                  // everyone has read it
+  }
+  __syncthreads();
+  if (s_last) grad_totals(a, tid, wave, lane, s_term);
+}
+
 template <typename T>
 hipError_t launch(const LossGradArgs& a, hipStream_t stream) {
   const int groups = ceil_div((int64_t)a.V_d + 7, kGradIds<T>);   // a row starts up to 7 elements into its first vector
@@ -211,6 +511,29 @@ hipError_t launch(const LossGradArgs& a, hipStream_t stream) {
 }
 
 }  // namespace
+
+// LDS for a row of 4-byte slots, and the vectors per thread that hold one.
+constexpr int64_t kRowLdsBytes = 150 << 10;
+constexpr int64_t row_lds_bytes(int V_d) { return 16 * (((int64_t)V_d + 16 + 3) / 4); }   // a row shifted by up to 7, in whole vectors of 8
+bool loss_grad_row_fits(int K, int V_d) { return K > 0 && row_lds_bytes(V_d) <= kRowLdsBytes; }
+size_t loss_grad_row_bytes() { return sizeof(GradRow); }
+
+template <typename T>
+static hipError_t launch_rows(const LossGradArgs& a, hipStream_t stream) {
+  hipLaunchKernelGGL(loss_prepare_kernel<T>, dim3((unsigned)ceil_div(a.B, 4)), dim3(256), 0, stream, a);
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return e;
+  constexpr int kMost = (int)(kRowLdsBytes / 4 / (kRowThreads * Draft<T>::kElems)) + 1;
+  const int vecs = ceil_div(a.V_d + Draft<T>::kElems - 1, kRowThreads * Draft<T>::kElems);
+  const size_t lds = (size_t)row_lds_bytes(a.V_d);
+  const auto kernel = vecs <= kMost / 5 ? loss_row_kernel<T, kMost / 5> : vecs <= 2 * kMost / 5 ? loss_row_kernel<T, 2 * kMost / 5>
+                      : vecs <= 4 * kMost / 5 ? loss_row_kernel<T, 4 * kMost / 5> : loss_row_kernel<T, kMost>;
+  hipLaunchKernelGGL(kernel, dim3((unsigned)a.K), dim3(kRowThreads), lds, stream, a);
+  return hipGetLastError();
+}
+hipError_t launch_loss_and_grad(const LossGradArgs& a, hipStream_t stream) {
+  return a.dtype == OT_BF16 ? launch_rows<uint16_t>(a, stream) : launch_rows<float>(a, stream);
+}
 
 hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream) {
   if (a.K == 0) return hipSuccess;

@@ -43,6 +43,8 @@ struct ot_ctx {
   double* loss_part = nullptr;        // [max_rows, kLossGroups] KL sums of a row's groups
   double* loss_mass_part = nullptr;   // the same of q's mass on the mapped ids, and
   double* loss_mass = nullptr;        // [max_rows] its sum per row: for the loss's gradient
+  void* grad_rows = nullptr;          // [max_K] records of the draft rows for the loss's gradient
+  int32_t* grad_count = nullptr;      // [2] its arrival counter and its number of tokens, 0 between calls
   int32_t* counters = nullptr;        // the arrival counters below, in one allocation
   int32_t* loss_count = nullptr;      // [max_rows + 1] arrival counters of the loss launch, 0 between launches
   int32_t* adapt_count = nullptr;     // arrival counter of the adaptive-drafting launch, 0 between launches

@@ -204,6 +204,15 @@ struct LossGradArgs {
   const int32_t* kind; const double* kl; const double* mass; const double* weight; const double* totals;
   const float* grad_loss;   // or nullptr: 1
   void* grad;               // [K, V_d]
+  // where the gradient's launches do the loss's work too: what that reads and writes besides
+  int32_t M, n_pairs, lambda_mode, accepted_only;
+  float lambda;
+  const int2* pairs;
+  const int32_t* n_accept; const float* p_tok;
+  void* rows;               // [K] records (loss_grad.hip)
+  int32_t* n_tokens;        // drafted tokens considered; 0 between calls
+  int32_t* count;           // draft rows done; 0 between calls
+  ot_loss_out out;
 };
 
 // ------------------------------------------------------------------------------------------------ launchers
@@ -234,6 +243,9 @@ bool lmhead_f32_hosts_draft_side(int M, int d, int V_t, int B, int K, int V_d, i
 hipError_t launch_qhead(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream);
 hipError_t launch_pack_quant(const uint8_t* codes, const void* scales, int scale_f16, const uint8_t* zeros, int group, int d, int V_t, const QuantHead& q,
                              uint4* packed, uint32_t* recs, hipStream_t stream);
+bool loss_grad_row_fits(int K, int V_d);   // whether launch_loss_and_grad takes such rows
+size_t loss_grad_row_bytes();         // of one of ot_ctx::grad_rows
+hipError_t launch_loss_and_grad(const LossGradArgs& a, hipStream_t stream);
 size_t logprob_segment_bytes();       // of one of ot_ctx::lp_part (logprobs.hip)
 hipError_t launch_loss_grad(const LossGradArgs& a, hipStream_t stream);
 hipError_t launch_softmax_stats(const StepArgs& a, hipStream_t stream);
