@@ -471,7 +471,7 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad is not aligned to its type");
   // where the gradient's launches take rows of this size they do the loss's work as well (without the q' rows)
   const bool in_one = ctx && in && out && in->B > 0 && in->row_off_host && !out->qprime &&
-                      loss_grad_row_fits(in->row_off_host[in->B] - in->B, ctx->V_d);
+                      loss_grad_in_one(in->row_off_host[in->B] - in->B, ctx->V_d, ctx->n_cu);
   const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, in_one);
   if (bad != OT_OK || in->B == 0) return bad;
   LossGradArgs a{};

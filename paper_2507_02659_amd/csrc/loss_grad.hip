@@ -211,13 +211,13 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 // What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
 // sum q t gets the constants' part as their 64-bit difference times the mass of q.
 struct alignas(16) GradRow {
-  float mx, mxq;                // t = (zq - mxq) * s2q and (z - mx) * s2: exponents to base 2, scales as two floats
-  float s2, s2_lo, s2q, s2q_lo;
-  float inv_Sq, r0;             // q = 2^t / Sq;  r = (tq - t) ln 2 + r0, r0 = lnS - lnSq + 1
+  float mx, mxq;                // t = (zq - mxq) * s2q and (z - mx) * s2: exponents to base 2, s2 as two floats
+  float s2, s2_lo, s2q;         // (the row sums' exponents were formed with one float of log2(e)/Td as well)
+  float r0, inv_Sq;             // q = 2^t / Sq;  r = (tq - t) ln 2 + r0, r0 = lnS - lnSq + 1
   double dlnS;                  // lnS - lnSq
   double c, D, a_pre;           // c and D without grad_loss / n
   double kl_more, A_more;       // what Eq. 2's overrides add to the KL sum and to A
-  int32_t kind, row, sub, out, pre, pad[3];
+  int32_t kind, row, sub, out, pre;
 };
 static_assert(sizeof(GradRow) % 16 == 0, "read as 16-byte units");
 
@@ -303,7 +303,7 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
   R.mx = __shfl(mx, j); R.mxq = mxq;
   const double s2 = 1.4426950408889634 * invT, s2q = 1.4426950408889634 * invTd;
   R.s2 = (float)s2; R.s2_lo = (float)(s2 - (double)R.s2);
-  R.s2q = (float)s2q; R.s2q_lo = (float)(s2q - (double)R.s2q);
+  R.s2q = (float)s2q;
   R.inv_Sq = (float)(1.0 / Sq);
   R.dlnS = __shfl(lnS, j) - lnSq;
   R.r0 = (float)(R.dlnS + 1.0);
@@ -366,13 +366,12 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   const int v0 = tid * kVec - shift;                     // the thread's vector i holds ids v0 + i * kRowThreads * kVec ..
   auto first = [&](int i) { return v0 + i * kRowThreads * kVec; };
   auto whole = [&](int i) { return vectors && first(i) >= 0 && first(i) + kVec <= a.V_d; };
-  int2 id[kPairs], id_next[kPairs];
+  int2 id[kPairs] = {};
   auto load_pairs = [&](int at, int2* to) {
 #pragma unroll
     for (int e = 0; e < kPairs; ++e) to[e] = a.pairs[max(0, min(at + e * kRowThreads, a.n_pairs - 1))];
   };
-  const bool has_kl = (R.kind & 1) && a.n_pairs > 0;
-  if (has_kl) load_pairs(tid, id);
+  if (a.n_pairs > 0) load_pairs(tid, id);
   float x[kEach];
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
@@ -386,30 +385,52 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   const float scale = up / (float)max(1, n_tokens), c = (float)R.c * scale, D = (float)R.D * scale;
   auto q_of = [&](float zq_i, float* tq) {
     const float d = fmaxf(zq_i - R.mxq, -1e30f);         // an id masked with -inf: q = 0, and no -inf times a low part of 0
-    *tq = fmaf(d, R.s2q, d * R.s2q_lo);
+    *tq = d * R.s2q;
     return __builtin_amdgcn_exp2f(*tq) * R.inv_Sq;
   };
+  // while the record and the pairs are on their way
+  const int slots = (a.V_d + shift + 3) / 4;
+  for (int i = tid; i < slots; i += kRowThreads) {
+    const float none = __uint_as_float(kNoImage);
+    reinterpret_cast<f32x4*>(s_z)[i] = f32x4{none, none, none, none};
+  }
+  // Counts the row in: its KL value has reached memory, and every wavefront has read the number of tokens (a barrier lies in front), which
+  // the last workgroup of all puts back to 0.
+  auto count_in = [&]() {
+    s_last = arrive(a.count, a.K);
+    if (s_last) publish(a.n_tokens, 0);
+  };
   float A = 0.f;
+  asm volatile("" ::"v"(scale));                         // read by now
+  __syncthreads();
   if (R.kind & 1) {
-    const int slots = (a.V_d + shift + 3) / 4;
-    for (int i = tid; i < slots; i += kRowThreads) {
-      const float none = __uint_as_float(kNoImage);
-      reinterpret_cast<f32x4*>(s_z)[i] = f32x4{none, none, none, none};
-    }
-    __syncthreads();
     const float* z = a.Z + (int64_t)R.row * a.ldz;
-    for (int at = tid; at - tid < a.n_pairs; at += kPairs * kRowThreads) {
-      float zv[kPairs];
+    // a turn's logits are asked for a turn ahead, their ids two
+    float zv[kPairs];
+    int2 id_next[kPairs];
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) zv[e] = z[id[e].x];
-      if (at - tid + kPairs * kRowThreads < a.n_pairs) load_pairs(at + kPairs * kRowThreads, id_next);
+    for (int e = 0; e < kPairs; ++e) zv[e] = z[id[e].x];
+    if (kPairs * kRowThreads < a.n_pairs) load_pairs(tid + kPairs * kRowThreads, id_next);
+    for (int at = tid; at - tid < a.n_pairs; at += kPairs * kRowThreads) {
+      float z_next[kPairs] = {};
+      int2 id_after[kPairs] = {};
+      if (at - tid + kPairs * kRowThreads < a.n_pairs) {
+#pragma unroll
+        for (int e = 0; e < kPairs; ++e) z_next[e] = z[id_next[e].x];
+      }
+      if (at - tid + 2 * kPairs * kRowThreads < a.n_pairs) load_pairs(at + 2 * kPairs * kRowThreads, id_after);
 #pragma unroll
       for (int e = 0; e < kPairs; ++e)
         if (at + e * kRowThreads < a.n_pairs) s_z[shift + id[e].y] = zv[e];
 #pragma unroll
-      for (int e = 0; e < kPairs; ++e) id[e] = id_next[e];
+      for (int e = 0; e < kPairs; ++e) { id[e] = id_next[e]; id_next[e] = id_after[e]; zv[e] = z_next[e]; }
     }
     __syncthreads();
+    if ((R.kind & 2) && tid == 0) {                      // Eq. 2's overrides are not among the ordinary ids
+      if (R.out >= 0) s_z[shift + R.out] = __uint_as_float(kNoImage);
+      if (R.pre >= 0) s_z[shift + R.pre] = __uint_as_float(kNoImage);
+    }
+    if (R.kind & 2) __syncthreads();
     double kl = 0.0, mass = 0.0;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
@@ -422,27 +443,28 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
 #pragma unroll
           for (int f = 0; f < 4; ++f) zr[e + f] = w[f];
         }
+        bool far = false;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
-          const int v = base - shift + e, at = i * kVec + e;
-          float tq, r = 0.f;
-          const float q = q_of(x[at], &tq), d = zr[e] - R.mx;
-          if (v >= 0 && v < a.V_d && __float_as_uint(zr[e]) != kNoImage && v != R.out && v != R.pre && q > 0.f) {
-            if (d >= -1e20f) {
-              const float diff = (tq - fmaf(d, R.s2, d * R.s2_lo)) * 0.69314718f;
-              kl_i = fmaf(q, diff, kl_i);
-              r = diff + R.r0;
-            } else {                                     // masked by the target: with -inf the term is infinite, with a lowest number nearly
-              const double diff = ((double)tq - (double)d * (double)R.s2) * 0.6931471805599453;
-              kl += (double)q * diff;
-              r = d == -INFINITY ? INFINITY : (float)fmin(diff, 3.0e38);
+          float tq;
+          const float q = q_of(x[i * kVec + e], &tq), d = zr[e] - R.mx;
+          const bool ordinary = __float_as_uint(zr[e]) != kNoImage, near = ordinary && !(d < -1e20f);
+          const float diff = near ? (tq - fmaf(d, R.s2, d * R.s2_lo)) * 0.69314718f : 0.f;
+          kl_i = fmaf(q, diff, kl_i);
+          mass_i += ordinary ? q : 0.f;
+          far |= ordinary && !near && q > 0.f;
+          zr[e] = near ? diff + R.r0 : ordinary ? zr[e] : 0.f;
+          x[i * kVec + e] = q;
+        }
+        if (__any(far)) {                                // masked by the target: with -inf the term is infinite, with a lowest number nearly
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) {
+            const double d = (double)zr[e] - (double)R.mx;
+            if (d < -1e20 && x[i * kVec + e] > 0.f) {    // (an r is not that small)
+              kl += (double)x[i * kVec + e] * (-d * (double)R.s2 * 0.6931471805599453);
+              zr[e] = d < -1e300 ? INFINITY : (float)fmin(-d * (double)R.s2 * 0.6931471805599453, 3.0e38);
             }
-            mass_i += q;
           }
-          if (!(d == d)) r = __float_as_uint(zr[e]) == kNoImage ? r : d;   // NaN stays one
-          if (v == R.pre) r = (float)R.a_pre;
-          zr[e] = r;
-          x[at] = q;
         }
 #pragma unroll
         for (int e = 0; e < kVec; e += 4) *reinterpret_cast<f32x4*>(s_z + base + e) = f32x4{zr[e], zr[e + 1], zr[e + 2], zr[e + 3]};
@@ -458,14 +480,23 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     mass = wave_sum(lane < 16 ? s_term[1][lane] : 0.0);
     kl += R.dlnS * mass;                                 // sum over ordinary ids of q (ln q - ln p)
     A = (float)(kl + mass + R.A_more);
-    if (tid == 0) publish(a.out.kl + R.row, kl + R.kl_more);
+    if (R.kind & 2) {
+      if (tid == 0 && R.pre >= 0) s_z[shift + R.pre] = (float)R.a_pre;
+      __syncthreads();
+    }
+    if (tid == 0) {
+      publish(a.out.kl + R.row, kl + R.kl_more);
+      count_in();
+    }
+  } else if (tid == 0) {
+    count_in();
   }
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
     const int base = (i * kRowThreads + tid) * kVec;
     if (base >= shift + a.V_d) break;
     float out[kVec];
-    if (R.kind & 1) {                                    // the thread's own words, which it wrote above
+    if (R.kind & 1) {                                    // the thread's own words, which it wrote above, but for R.pre's
 #pragma unroll
       for (int e = 0; e < kVec; e += 4) {
         const f32x4 r = *reinterpret_cast<const f32x4*>(s_z + base + e);
@@ -491,12 +522,6 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
         if (first(i) + e >= 0 && first(i) + e < a.V_d) Draft<T>::store_one(grad + first(i) + e, out[e]);
     }
   }
-  __syncthreads();                                       // every wavefront has used the number of tokens
-  // this thread's word about the row has reached memory before it is counted in (arrive)
-  if (tid == 0) {
-    s_last = arrive(a.count, a.K);
-    if (s_last) publish(a.n_tokens, 0);                  // everyone has read it
-  }
   __syncthreads();
   if (s_last) grad_totals(a, tid, wave, lane, s_term);
 }
@@ -515,7 +540,11 @@ hipError_t launch(const LossGradArgs& a, hipStream_t stream) {
 // LDS for a row of 4-byte slots, and the vectors per thread that hold one.
 constexpr int64_t kRowLdsBytes = 150 << 10;
 constexpr int64_t row_lds_bytes(int V_d) { return 16 * (((int64_t)V_d + 16 + 3) / 4); }   // a row shifted by up to 7, in whole vectors of 8
-bool loss_grad_row_fits(int K, int V_d) { return K > 0 && row_lds_bytes(V_d) <= kRowLdsBytes; }
+// One workgroup per row costs its chain of steps, about 20 us for 32000 ids, and from a quarter of the compute units on less than the loss's
+// launch and the gather; short rows are short chains.  Measured, us per call in one / with the gather: 6 rows of 32000 ids against 128256
+// 25.9 / 19.4, 24 28.7 / 22.0, 96 30.2 / 36.8, 288 60.6 / 80.5, 600 90.3 / 160.7; of 8000 against 50257 17.7 / 19.1 (6), 35.7 / 58.3 (600); one
+// vocabulary of 32000 ids on both sides 22.8 / 19.4 (6), 26.7 / 28.7 (96), 75.2 / 101.2 (600).
+bool loss_grad_in_one(int K, int V_d, int n_cu) { return K > 0 && row_lds_bytes(V_d) <= kRowLdsBytes && (4 * K >= n_cu || V_d <= 16384); }
 size_t loss_grad_row_bytes() { return sizeof(GradRow); }
 
 template <typename T>

@@ -243,7 +243,7 @@ bool lmhead_f32_hosts_draft_side(int M, int d, int V_t, int B, int K, int V_d, i
 hipError_t launch_qhead(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream);
 hipError_t launch_pack_quant(const uint8_t* codes, const void* scales, int scale_f16, const uint8_t* zeros, int group, int d, int V_t, const QuantHead& q,
                              uint4* packed, uint32_t* recs, hipStream_t stream);
-bool loss_grad_row_fits(int K, int V_d);   // whether launch_loss_and_grad takes such rows
+bool loss_grad_in_one(int K, int V_d, int n_cu);   // whether launch_loss_and_grad takes K such rows
 size_t loss_grad_row_bytes();         // of one of ot_ctx::grad_rows
 hipError_t launch_loss_and_grad(const LossGradArgs& a, hipStream_t stream);
 size_t logprob_segment_bytes();       // of one of ot_ctx::lp_part (logprobs.hip)

@@ -210,7 +210,9 @@ class Verifier:
                               hidden=inp["hidden"], draft_logits=inp["draft_logits"], draft_ids=inp["draft_ids"],
                               temperature=inp["temperature"], draft_temperature=inp["draft_temperature"],
                               seq_id=inp["seq_id"], seed=inp["seed"])
-        ot.ot_distill_loss_grad(self.ctx, sin, ot.make_step_out(inp["out"]), inp["target_logits"] if from_logits else None, lam=lam,
+        out = inp["out"]                            # of the step's outputs, what the loss reads
+        sout = ot.make_step_out({n: out[n] for n in ("n_mapped", "n_accept", "mapped_ids", "span_start", "span_len", "p_tok")})
+        ot.ot_distill_loss_grad(self.ctx, sin, sout, inp["target_logits"] if from_logits else None, lam=lam,
                                 lambda_mode=lambda_mode, ngram_term=ngram_term, accepted_only=accepted_only, buffers=buf,
                                 grad_loss=grad_loss, grad=grad)
         return dict(buf, grad=grad)

@@ -72,6 +72,34 @@ def test_vocabularies(V_t, V_d, n_direct):
         _compare(make_case(_spec("vocabularies", [5, 3, 6], V_d, dtype=dtype, V_t=V_t, V_d=V_d, n_direct=n_direct, n_ngram=min(60, V_t - n_direct))))
 
 
+@pytest.mark.parametrize("V_d", [4095, 8185, 8192, 16377, 20000, 32768, 38377, 38378, 38400])
+def test_many_rows_of_every_width(V_d):
+    """64 rows and more, which one workgroup each takes where a row fits LDS: every number of vectors per thread, the last widths that fit, and
+    the first that do not."""
+    for dtype in ("f32", "bf16"):
+        case = make_case(_spec("widths", [6, 7] * 5 + [0, 3], V_d, dtype=dtype, V_t=4000, V_d=V_d, n_direct=min(3000, V_d), n_ngram=60))
+        assert case.K >= 64
+        _compare(case, modes=[("target_prob", "approx_kl", False), ("fixed", "nll", True)])
+
+
+@pytest.mark.parametrize("V_d", [301, 20000])
+def test_targets_masked_with_the_lowest_number(V_d):
+    """The target masks ids that the drafter proposes with a finite lowest number: the loss and the gradients are huge, and finite."""
+    from paper_2507_02659_amd.runner import Verifier
+    case = make_case(_spec("lowest", [3, 3], 5, n_ngram=0, temperature=[1.0, 1.0], n_direct=300, V_d=V_d))
+    case.target_logits[0, case.direct_map[case.direct_map >= 0][:5]] = -3.0e38
+    want, scale, _ = og.hybrid_loss_grad_case(case)
+    v = Verifier.for_case(case)
+    inp = v.upload(case)
+    v.step(inp, from_logits=True)
+    got = v.distill_loss_grad(inp, from_logits=True)
+    loss = v.distill_loss(inp, from_logits=True)
+    grad = got["grad"].double().cpu().numpy()
+    np.testing.assert_allclose(got["kl"].cpu().numpy()[:case.M], loss["kl"], rtol=1e-5, atol=1e-6)
+    assert np.isfinite(grad).all() and (np.abs(grad - want) <= 2e-5 * scale + 2.0 ** -23 * np.abs(want)).all()
+    v.close()
+
+
 def test_one_vocabulary_on_both_sides():
     for V in (1000, 40000):
         _compare(make_case(_spec("identity", [5, 0, 6], V, V_t=V, V_d=V, n_direct=0, identity_map=True, permute_frac=0.02, n_ngram=0)))
