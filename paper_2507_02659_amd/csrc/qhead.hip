@@ -211,7 +211,9 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
   constexpr int kGroups = 4 / kSteps, kBlocks = tall_blocks(RT, S), kUnits = kBlocks * RT;
   constexpr int kStage = (kUnits + kTallWaves - 3) / (kTallWaves - 2);   // units per wavefront of six at least
   __shared__ u32x4 s_x[2][kUnits][4][64];
-  __shared__ f32x4 s_sum[2][kUnits][kGroups][4];
+  // sums of the hidden states of a row over a group, in rings of blocks: four groups' worth is used at a time, a chunk is staged ahead
+  constexpr int kRing = 2 * (kSteps > kBlocks ? kSteps : kBlocks);
+  __shared__ float s_sum[kRing][RT][kGroups][16];
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n_waves = blockDim.x >> 6;
   const int slot = (int)blockIdx.x >> 3, row0 = slot % m_blocks * (RT * 16), ct = slot / m_blocks * 8 + ((int)blockIdx.x & 7);
   const int first = (ct * n_waves + wave) * S;
@@ -245,7 +247,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
             s_x[buf][u][g * kSteps + t][lane] = x;
             sum = mfma(x, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, sum);
           }
-          if ((lane & 15) == 0) s_sum[buf][u][g][lane >> 4] = sum;
+          if ((lane & 15) == 0) *reinterpret_cast<f32x4*>(&s_sum[(c * kBlocks + u / RT) & (kRing - 1)][u % RT][g][4 * (lane >> 4)]) = sum;
         }
       }
     }
@@ -256,24 +258,25 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
   fetch(0);
   put(0, 0);
   f32x4 total[RT][S] = {};
-  const int chunks = (q.blocks + kBlocks - 1) / kBlocks;
-  auto block = [&](int buf, int j, Weights<S, kGroups>& W) {
+  const int padded = (q.blocks + kSteps - 1) / kSteps * kSteps, chunks = (padded + kBlocks - 1) / kBlocks;   // whole fours of groups
+  uint32_t rec4[S] = {};                                 // of four groups, a quarter of the lanes each
+  auto block = [&](int buf, int j, int b, Weights<S, kGroups>& W) {
     u32x4 w[S][4];
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) w[s][ks] = codes_to_bf16(W.w[s][ks]);
-    float scale[S][kGroups], zero[S][kGroups];
+    float scale[S][kGroups];
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
-      for (int g = 0; g < kGroups; ++g) { scale[s][g] = rec_scale(W.rec[s][g]); zero[s][g] = -rec_zero(W.rec[s][g]); }
+      for (int g = 0; g < kGroups; ++g) {
+        scale[s][g] = rec_scale(W.rec[s][g]);
+        rec4[s] = (lane >> 4) == ((b * kGroups + g) & 3) ? W.rec[s][g] : rec4[s];
+      }
     // a row tile's operands are read while the tile in front of it is multiplied
     u32x4 x[2][4];
-    f32x4 sum[2][kGroups];
     auto read = [&](int rt) {
-#pragma unroll
-      for (int g = 0; g < kGroups; ++g) sum[rt & 1][g] = s_sum[buf][j * RT + rt][g][lane >> 4];
 #pragma unroll
       for (int ks = 0; ks < 4; ++ks) x[rt & 1][ks] = s_x[buf][j * RT + rt][ks][lane];
     };
@@ -283,9 +286,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
       if (rt + 1 < RT) read(rt + 1);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
-        f32x4 acc[S];
-#pragma unroll
-        for (int s = 0; s < S; ++s) acc[s] = sum[rt & 1][g] * zero[s][g];
+        f32x4 acc[S] = {};
 #pragma unroll
         for (int t = 0; t < kSteps; ++t) {
 #pragma unroll
@@ -302,9 +303,22 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
       for (int s = 0; s < S; ++s) asm volatile("" : "+v"(total[rt][s]));
     }
   };
+  // The offsets of the last four groups, of block b and those in front of it, as one fp32 product with four terms per row tile and column tile.
+  auto offsets = [&](int b) {
+    float off[S];
+#pragma unroll
+    for (int s = 0; s < S; ++s) off[s] = -rec_scale(rec4[s]) * rec_zero(rec4[s]);
+    const int from = b * kGroups + kGroups - 4 + (lane >> 4);   // the lane's group
+#pragma unroll
+    for (int rt = 0; rt < RT; ++rt) {
+      const float sum = s_sum[from / kGroups & (kRing - 1)][rt][from % kGroups][lane & 15];
+#pragma unroll
+      for (int s = 0; s < S; ++s) total[rt][s] = __builtin_amdgcn_mfma_f32_16x16x4f32(sum, off[s], total[rt][s], 0, 0, 0);
+    }
+  };
   constexpr int kTurn = kAhead / kBlocks;                // chunks per trip: the ring's places and, if even, the buffers are constants
-  static_assert(kAhead % kBlocks == 0, "a chunk's blocks have places of their own in the ring");
-  // chunks are padded to whole trips: past the last block the hidden rows are staged as zeros, and the last block's weights are used again
+  static_assert(kAhead % kBlocks == 0 && (kAhead % kSteps == 0 || kSteps % kAhead == 0), "a chunk's blocks have places of their own in the ring");
+  // chunks are padded to whole trips: past the last block the hidden rows are staged as zeros
   for (int c0 = 0; c0 < chunks; c0 += kTurn) {
 #pragma unroll
     for (int cc = 0; cc < kTurn; ++cc) {
@@ -314,10 +328,11 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j) {
         const int b = c * kBlocks + j;
-        if (kBlocks == 1 || b < q.blocks) {
-          block(buf, j, ring[cc * kBlocks + j]);
+        if (b < q.blocks) {
+          block(buf, j, b, ring[cc * kBlocks + j]);
           load_weights<S, kGroups, false>(q, tile, min(b + kAhead, q.blocks - 1), lane, &ring[cc * kBlocks + j]);
         }
+        if ((b + 1) % kSteps == 0) offsets(b);           // (past the last block the sums are 0)
       }
       put(c + 1, buf ^ 1);
     }
@@ -377,7 +392,7 @@ hipError_t launch_up_to_16(const uint16_t* H, int M, int d, const QuantHead& q, 
 
 template <int RT, int S, int kSteps>
 hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int m_blocks, int waves, hipStream_t stream) {
-  constexpr int kAhead = S > 2 ? 2 : RT <= 4 ? 4 : 2;
+  constexpr int kAhead = S <= 2 && (kSteps == 4 || RT <= 4) ? 4 : 2;
   const int64_t grid = (int64_t)ceil_div(ceil_div(q.tiles, waves * S), 8) * 8 * m_blocks;
   if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
   hipLaunchKernelGGL((qhead_tall_kernel<RT, S, kSteps, kAhead>), dim3((unsigned)grid), dim3(64 * waves), 0, stream, H, M, d, q, Z, V_t, ldz, m_blocks);
