@@ -24,13 +24,21 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
 
 // Eight codes of one packed word as bf16 numbers 16 + c, in ascending hidden index.  The word is the one whose nibble j holds code 2 j
 // and whose nibble j + 4 code 2 j + 1 (j < 4), rotated left by 3: a pair's mantissa bits are then a shift and a mask away.
-__device__ inline u32x4 codes_to_bf16(uint32_t w) {
-  auto bits = [](uint32_t x) {                           // (x & mask) | 16: one instruction, which takes no literals, so from registers
-    uint32_t r;
-    asm("v_and_or_b32 %0, %1, %2, %3" : "=v"(r) : "v"(x), "s"(0x00780078u), "v"(0x41804180u));
-    return r;
-  };
-  return u32x4{bits(w), bits(w >> 4), bits(w >> 8), bits(__builtin_amdgcn_alignbit(w, w, 12))};
+// Mask and 16 come in registers (Bits): the instruction that does both, v_and_or_b32, takes no literals.  The compiler has to choose that
+// instruction itself: one written as inline asm is outside its bookkeeping of the waits between vector and matrix instructions, and
+// a matrix product still in flight overwrote such results.
+struct Bits {
+  uint32_t mask, sixteen;
+};
+__device__ inline Bits code_bits() {                     // the empty statements keep the compiler from folding the constants back in
+  Bits k{0x00780078u, 0x41804180u};
+  asm("" : "+s"(k.mask));
+  asm("" : "+v"(k.sixteen));
+  return k;
+}
+__device__ inline u32x4 codes_to_bf16(uint32_t w, Bits k) {
+  return u32x4{(w & k.mask) | k.sixteen, (w >> 4 & k.mask) | k.sixteen, (w >> 8 & k.mask) | k.sixteen,
+               (__builtin_amdgcn_alignbit(w, w, 12) & k.mask) | k.sixteen};
 }
 // A group's scale and 16 + zero point of one column: the scale's fp32 bits, of which a bf16 or fp16 scale leaves the low 13 free.
 __device__ inline float rec_scale(uint32_t r) { return __uint_as_float(r & 0xFFFFE000u); }
@@ -123,6 +131,7 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
                                                             int64_t ldz, int chunk_blocks, int parts) {
   constexpr int kGroups = 4 / kSteps;
   extern __shared__ u32x4 s_x[];
+  const Bits bits = code_bits();
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), n_waves = blockDim.x >> 6;
   const int part = wave % parts, first = ((int)blockIdx.x * (n_waves / parts) + wave / parts) * S;
   int tile[S];
@@ -161,7 +170,7 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
               const u32x4 xf = x[ks * 64];
               sum = mfma(xf, u32x4{0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u}, sum);
 #pragma unroll
-              for (int s = 0; s < S; ++s) acc[s] = mfma(xf, codes_to_bf16(ring[i].w[s][ks]), acc[s]);
+              for (int s = 0; s < S; ++s) acc[s] = mfma(xf, codes_to_bf16(ring[i].w[s][ks], bits), acc[s]);
             }
 #pragma unroll
             for (int s = 0; s < S; ++s) {
@@ -210,6 +219,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
                                                                      int V_t, int64_t ldz, int m_blocks) {
   constexpr int kGroups = 4 / kSteps, kBlocks = tall_blocks(RT, S), kUnits = kBlocks * RT;
   constexpr int kStage = (kUnits + kTallWaves - 3) / (kTallWaves - 2);   // units per wavefront of six at least
+  const Bits bits = code_bits();
   __shared__ u32x4 s_x[2][kUnits][4][64];
   // sums of the hidden states of a row over a group, in rings of blocks: four groups' worth is used at a time, a chunk is staged ahead
   constexpr int kRing = 2 * (kSteps > kBlocks ? kSteps : kBlocks);
@@ -265,7 +275,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
     for (int s = 0; s < S; ++s)
 #pragma unroll
-      for (int ks = 0; ks < 4; ++ks) w[s][ks] = codes_to_bf16(W.w[s][ks]);
+      for (int ks = 0; ks < 4; ++ks) w[s][ks] = codes_to_bf16(W.w[s][ks], bits);
     float scale[S][kGroups];
 #pragma unroll
     for (int s = 0; s < S; ++s)
