@@ -213,7 +213,7 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
 // hidden rows come through LDS in chunks of kBlocks * 128 hidden indices, two buffers, one barrier per chunk.  A wavefront stages whole
 // (row tile, block) units, in the order of the matrix instruction's operand, and forms their groups' sums on the way (a product with ones).
 constexpr int kTallWaves = 8;
-constexpr int tall_blocks(int RT, int S) { return S > 2 ? (RT <= 2 ? 2 : 1) : RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }
+constexpr int tall_blocks(int RT, int S) { return S > 2 ? (RT <= 4 ? 2 : 1) : RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }
 template <int RT, int S, int kSteps, int kAhead>
 __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint16_t* __restrict__ H, int M, int d, QuantHead q, float* __restrict__ Z,
                                                                      int V_t, int64_t ldz, int m_blocks) {
