@@ -284,7 +284,8 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
         scale[s][g] = rec_scale(W.rec[s][g]);
         rec4[s] = (lane >> 4) == ((b * kGroups + g) & 3) ? W.rec[s][g] : rec4[s];
       }
-    // a row tile's operands are read while the tile in front of it is multiplied
+    // a row tile's operands are read while the tile in front of it is multiplied; the fence keeps the compiler from sinking each read to
+    // its use, which leaves the latency of LDS open in front of every product
     u32x4 x[2][4];
     auto read = [&](int rt) {
 #pragma unroll
@@ -294,6 +295,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
     for (int rt = 0; rt < RT; ++rt) {
       if (rt + 1 < RT) read(rt + 1);
+      __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         f32x4 acc[S] = {};
@@ -338,10 +340,9 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
       for (int j = 0; j < kBlocks; ++j) {
         const int b = c * kBlocks + j;
-        if (b < q.blocks) {
-          block(buf, j, b, ring[cc * kBlocks + j]);
-          load_weights<S, kGroups, false>(q, tile, min(b + kAhead, q.blocks - 1), lane, &ring[cc * kBlocks + j]);
-        }
+        if (b < q.blocks) block(buf, j, b, ring[cc * kBlocks + j]);
+        // loaded without a condition (a repeat past the end): the count of loads in flight is then known where the staged rows are waited for
+        load_weights<S, kGroups, false>(q, tile, min(b + kAhead, q.blocks - 1), lane, &ring[cc * kBlocks + j]);
         if ((b + 1) % kSteps == 0) offsets(b);           // (past the last block the sums are 0)
       }
       put(c + 1, buf ^ 1);
