@@ -389,7 +389,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     return __builtin_amdgcn_exp2f(*tq) * R.inv_Sq;
   };
   // while the record and the pairs are on their way
-  const int slots = (a.V_d + shift + 3) / 4;
+  const int slots = (a.V_d + shift + kVec - 1) / kVec * (kVec / 4);   // whole vectors, as they are read
   for (int i = tid; i < slots; i += kRowThreads) {
     const float none = __uint_as_float(kNoImage);
     reinterpret_cast<f32x4*>(s_z)[i] = f32x4{none, none, none, none};

@@ -118,6 +118,35 @@ def test_targets_of_ngrams_that_are_images():
     _compare(case)
 
 
+@pytest.mark.parametrize("V_d", [301, 1001, 16379])
+def test_what_shared_memory_held_before_does_not_matter(V_d):
+    """A 4-bit head that has just taken hidden rows of NaN leaves them in the shared memory of every compute unit; the draft rows end inside a
+    vector of 8."""
+    from paper_2507_02659_amd import binding as ot
+    from paper_2507_02659_amd.runner import QuantWeights, Verifier
+    d, V = 4096, 8192
+    codes = torch.zeros(d // 2, V, dtype=torch.uint8, device="cuda:0")
+    head = Verifier.quantized(QuantWeights(codes, torch.ones(d // 128, V, device="cuda:0").bfloat16(), None, 128), V_d=1, direct_map=np.zeros(1, np.int32),
+                              max_batch=16, max_k=0)
+    hidden = torch.full((16, d), float("nan"), device="cuda:0").bfloat16()
+    case = make_case(_spec("after_nan", [4] * 40, 7, dtype="bf16", V_t=max(600, V_d), V_d=V_d))
+    v = Verifier.for_case(case)
+    try:
+        inp = v.upload(case)
+        v.step(inp, from_logits=True)
+        how = dict(from_logits=True, lam=0.2, ngram_term=ot.OT_NGRAM_TERM_APPROX_KL)
+        plain = v.distill_loss(inp, **how)
+        for _ in range(3):
+            assert torch.isnan(head.lm_head(hidden)).all()
+            torch.cuda.synchronize()
+            got = v.distill_loss_grad(inp, **how)
+            np.testing.assert_allclose(got["kl"].cpu().numpy()[:case.M], plain["kl"], rtol=2e-6, atol=1e-6)
+            assert torch.isfinite(got["grad"].float()).all()
+    finally:
+        v.close()
+        head.close()
+
+
 def test_draft_temperatures_and_upstream_gradient():
     case = make_case(_spec("temperatures", [4, 3, 5, 2, 6], 21, temperature=[1.0, 0.5, 1.0, 0.7, 0.0], draft_temperature=[0.6, 1.0, 0.0, 1.5, 1.0]))
     _compare(case, grad_loss=-2.5)
