@@ -116,7 +116,7 @@ void ot_verify_destroy(ot_ctx* ctx);          /* synchronises the stream, frees 
 /* W[k][v] = scale[k / group][v] * (code[k][v] - zero[k / group][v]) with codes of 0..15: a quarter of the OT_BF16 weights'
  * bytes, and up to 176 rows the weight stream is what bounds a step.  Codes times hidden states are exact, their sums over a
  * group and the sums of scaled groups are fp32; the hidden states are not rounded, so the logits are those of the weights above
- * to fp32 rounding.  A hidden row with an infinity or a NaN has NaN logits; hidden states are taken to stay below 2^100.   */
+ * to fp32 rounding.  Scales are finite.  A hidden row with an infinity or a NaN has NaN logits; hidden states are taken to stay below 2^100.   */
 typedef struct ot_quant_weights {
   int32_t        group;        /* 32, 64 or 128: so many consecutive hidden indices share a scale and a zero point; d may end
                                   inside a group                                                              */
@@ -132,8 +132,8 @@ typedef struct ot_quant_weights {
 int  ot_verify_init_quantized(const ot_verify_config* cfg, const ot_quant_weights* weights, ot_ctx** out);
 
 /* The logits alone: z = h . W of M hidden rows through the context's head of any type.  hidden: DEVICE [M, d] row-major,
- * cfg.dtype (OT_BF16: from a multiple of 16 bytes on); logits: DEVICE fp32, row m at logits + m * ld, ld >= V_t; 0 <= M <= max_batch * (max_k + 1).  Nothing of the
- * context's workspace is touched.                                                                              */
+ * cfg.dtype (OT_BF16: from a multiple of 16 bytes on); logits: DEVICE fp32, row m at logits + m * ld, ld >= V_t;
+ * 0 <= M <= max_batch * (max_k + 1).  Nothing of the context's workspace is touched.                              */
 int  ot_lm_head(ot_ctx* ctx, int32_t M, const void* hidden, float* logits, int64_t ld);
 
 /* ---- the n-gram cache ---------------------------------------------------------------------------------- */
@@ -272,7 +272,7 @@ typedef struct ot_loss_out {
 int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step_out, const float* target_logits_or_null,
                     const ot_loss_config* cfg, ot_loss_out* out);
 
-/* The values of ot_distill_loss (same arguments, same outputs), and the gradient of grad_loss * totals[4] with respect to the
+/* The values of ot_distill_loss (same arguments, same outputs, equal to fp32 rounding of the terms), and the gradient of grad_loss * totals[4] with respect to the
  * drafter's logits: grad, DEVICE [K, V_d] in cfg.dtype, written whole (zeros in the rows of draft tokens without a term).
  * grad_loss: DEVICE, one float, or NULL for 1.  p, the weights lambda and the translation are constants; q' depends on the draft
  * logits as Eq. 1 and Eq. 2 say, so with OT_NGRAM_TERM_APPROX_KL the logits of all of an n-gram's sub-tokens get a gradient.
@@ -295,7 +295,8 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
  * device: of the target, the drafter or another model.                                                          */
 #define OT_MAX_TOP 64                 /* n_top at most                                                          */
 typedef struct ot_logprob_in {
-  int32_t        M, V;                /* rows; ids per row                                                      */
+  int32_t        M, V;                /* rows, as many as a launch takes (2^24 - 1; of the gradient fewer where V is above 4000);     
+                                         ids per row, 1..2^30                                                  */
   int32_t        dtype;               /* OT_BF16 or OT_F32: type of the logits                                  */
   int32_t        n_tok, n_top;        /* given tokens per row (0: none); alternatives per row, 0..OT_MAX_TOP    */
   int32_t        given_rows_only;

@@ -539,8 +539,8 @@ hipError_t launch_logprobs(const ot_ctx* ctx, const LogprobArgs& a, hipStream_t 
 
 int check_in(const ot_ctx* ctx, const ot_logprob_in* in, const char* who) {
   if (in->dtype != OT_BF16 && in->dtype != OT_F32) return ot_fail(OT_ERR_DTYPE, "%s: logits are OT_BF16 or OT_F32 (%d)", who, in->dtype);
-  if (in->M < 0 || in->V < 1 || in->n_tok < 0 || in->ld < in->V)
-    return ot_fail(OT_ERR_SHAPE, "%s: need M >= 0, V >= 1, n_tok >= 0 and ld >= V (M = %d, V = %d, n_tok = %d, ld = %lld)", who, in->M, in->V, in->n_tok, (long long)in->ld);
+  if (in->M < 0 || in->V < 1 || in->V > (1 << 30) || in->n_tok < 0 || in->ld < in->V)
+    return ot_fail(OT_ERR_SHAPE, "%s: need M >= 0, 1 <= V <= 2^30, n_tok >= 0 and ld >= V (M = %d, V = %d, n_tok = %d, ld = %lld)", who, in->M, in->V, in->n_tok, (long long)in->ld);
   if (in->n_top < 0 || in->n_top > OT_MAX_TOP) return ot_fail(OT_ERR_SHAPE, "%s: n_top must be in 0..%d (%d)", who, OT_MAX_TOP, in->n_top);
   if (in->reserved != 0) return ot_fail(OT_ERR_SHAPE, "%s: reserved must be 0", who);
   if (in->given_rows_only && in->n_tok == 0) return ot_fail(OT_ERR_SHAPE, "%s: given_rows_only needs tokens", who);
@@ -568,6 +568,7 @@ int ot_token_logprobs(ot_ctx* ctx, const ot_logprob_in* in, ot_logprob_out* out)
   if ((in->n_tok > 0 && !out->logprob) || (in->n_top > 0 && (!out->top_ids || !out->top_logprobs)))
     return ot_fail(OT_ERR_NULL, "ot_token_logprobs: logprob, top_ids and top_logprobs are required where they have entries");
   if (!out->row_max != !out->row_sumexp) return ot_fail(OT_ERR_NULL, "ot_token_logprobs: row_max and row_sumexp come together");
+  if (!grid_fits(in->M, 64 * kRowWaves)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs: %d rows are too many for a launch", in->M);
   const LogprobArgs a{*in, *out};
   const hipError_t e = in->dtype == OT_BF16 ? launch_logprobs<uint16_t>(ctx, a, ctx->stream) : launch_logprobs<float>(ctx, a, ctx->stream);
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, "ot_token_logprobs: launch");
@@ -585,7 +586,7 @@ int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logpro
     return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: grad is not aligned to its type");
   if (grad == in->logits && ld_grad != in->ld) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: in place, ld_grad must be ld");
   const int chunks = ceil_div((int64_t)in->V + 7, in->dtype == OT_BF16 ? kGradChunk<uint16_t> : kGradChunk<float>);   // a row starts up to 7 elements into its first vector
-  if ((int64_t)chunks * in->M > 0x7FFFFFFF) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: %d rows of %d ids are too many for a launch", in->M, in->V);
+  if (!grid_fits((int64_t)chunks * in->M, 256)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: %d rows of %d ids are too many for a launch", in->M, in->V);
   const LogprobGradArgs a{*in, fwd->row_max, fwd->row_sumexp, fwd->entropy, grad_logprob, grad_entropy, grad, ld_grad};
   const auto kernel = in->dtype == OT_BF16 ? logprob_grad_kernel<uint16_t> : logprob_grad_kernel<float>;
   hipLaunchKernelGGL(kernel, dim3((unsigned)chunks * (unsigned)in->M), dim3(256), 0, ctx->stream, a, chunks);

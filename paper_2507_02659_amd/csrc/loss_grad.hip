@@ -530,7 +530,7 @@ template <typename T>
 hipError_t launch(const LossGradArgs& a, hipStream_t stream) {
   const int groups = ceil_div((int64_t)a.V_d + 7, kGradIds<T>);   // a row starts up to 7 elements into its first vector
   const int64_t grid = (int64_t)groups * ceil_div(a.K, 8) * 8;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (!grid_fits(grid, 256)) return hipErrorInvalidValue;
   hipLaunchKernelGGL(loss_grad_kernel<T>, dim3((unsigned)grid), dim3(256), 0, stream, a, groups);
   return hipGetLastError();
 }

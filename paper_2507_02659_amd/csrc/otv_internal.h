@@ -28,6 +28,8 @@ constexpr int kLossGroups = 64;      // workgroups per row of the distillation l
 
 constexpr int kLogprobSegments = 4096;  // workgroups of the log-probabilities' rows that are split, at most
 
+// Whether a launch takes so many workgroups: its threads are counted in 32 bits.
+inline bool grid_fits(int64_t workgroups, int threads) { return workgroups * threads <= 0xFFFFFFFFll; }
 inline int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
 
 // ------------------------------------------------------------------------------------------------ n-gram table

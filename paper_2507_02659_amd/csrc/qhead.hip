@@ -405,7 +405,7 @@ template <int RT, int S, int kSteps>
 hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int m_blocks, int waves, hipStream_t stream) {
   constexpr int kAhead = S <= 2 && (kSteps == 4 || RT <= 4) ? 4 : 2;
   const int64_t grid = (int64_t)ceil_div(ceil_div(q.tiles, waves * S), 8) * 8 * m_blocks;
-  if (grid > 0x7FFFFFFF) return hipErrorInvalidValue;
+  if (!grid_fits(grid, 64 * waves)) return hipErrorInvalidValue;
   hipLaunchKernelGGL((qhead_tall_kernel<RT, S, kSteps, kAhead>), dim3((unsigned)grid), dim3(64 * waves), 0, stream, H, M, d, q, Z, V_t, ldz, m_blocks);
   return hipGetLastError();
 }

@@ -313,6 +313,9 @@ def test_refusals(v):
     assert code(row_off=tok, B=0, temperature=lp) == ot.OT_ERR_SHAPE and code(row_off=tok, B=3) == ot.OT_ERR_SHAPE
     assert code(logits=z.data_ptr() + 2) == ot.OT_ERR_SHAPE
 
+    # more than a launch takes: refused before any pointer is followed
+    assert code(V=2 ** 30 + 1, ld=2 ** 31) == ot.OT_ERR_SHAPE and code(M=2 ** 24) == ot.OT_ERR_SHAPE
+
     fwd = {"row_max": lp, "row_sumexp": lp, "entropy": lp}
 
     def gcode(fwd=fwd, grad=z, ld=100, gH=None, **kw):
@@ -323,6 +326,7 @@ def test_refusals(v):
     wide = torch.zeros(4, 200, device=DEV)
     assert gcode(grad=None) == ot.OT_ERR_NULL and gcode(fwd={"row_max": lp}) == ot.OT_ERR_NULL and gcode(ld=99) == ot.OT_ERR_SHAPE
     assert gcode(fwd={"row_max": lp, "row_sumexp": lp}, gH=lp) == ot.OT_ERR_NULL and gcode(grad=wide.data_ptr() + 2, ld=200) == ot.OT_ERR_SHAPE
+    assert gcode(M=2 ** 24) == ot.OT_ERR_SHAPE
     assert gcode(grad=z, ld=101) == ot.OT_ERR_SHAPE and gcode(dtype=3) == ot.OT_ERR_DTYPE
     for bad in (dict(logits=z.half()), dict(logits=z.t()), dict(logits=z[:1].expand(4, 100)), dict(tokens=tok.long()), dict(tokens=tok[:3]),
                 dict(temperature=lp[:3]), dict(temperature=lp.double())):
