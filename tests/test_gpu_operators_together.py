@@ -53,3 +53,45 @@ def test_an_iteration():
         grad = loss["grad"].double().cpu().numpy()
         assert (np.abs(grad - want) <= 8e-6 * scale * (1 + 2.0 ** -8) + 2.0 ** -8 * np.abs(want) + 1e-37).all()
     v.close()
+
+
+def test_what_shared_memory_held_before_does_not_matter():
+    """Each operator after a 4-bit head that took hidden rows of NaN, and after one that took zeros: the same bits."""
+    from paper_2507_02659_amd.runner import Verifier
+    rng = np.random.default_rng(5)
+    w, _ = _weights(rng, 4096, 8192, 128, "bf16", False)
+    before = Verifier.quantized(w, V_d=1, direct_map=np.zeros(1, np.int32), max_batch=16, max_k=0)
+    fill = [torch.full((16, 4096), x, device="cuda:0").bfloat16() for x in (0.0, float("nan"))]
+    calls = {}
+    opened = [before]
+    for group in (32, 64, 128):
+        for M, d, V in ((1, 136, 300), (16, 8200, 515), (24, 264, 333), (48, 520, 2049), (80, 1000, 700), (144, 1032, 900), (161, 384, 300)):
+            head = Verifier.quantized(_weights(rng, d, V, group, "bf16", True)[0], V_d=1, direct_map=np.zeros(1, np.int32), max_batch=M, max_k=0)
+            opened.append(head)
+            calls[f"head {M} {d} {V} {group}"] = lambda head=head, h=torch.randn(M, d, device="cuda:0").bfloat16(): [head.lm_head(h)]
+    for dtype in (torch.float32, torch.bfloat16):
+        for M, V in ((1, 3), (2, 32003), (40, 20001), (700, 515)):
+            z, t = torch.randn(M, V, device="cuda:0").to(dtype), torch.randint(0, V, (M, 2), device="cuda:0", dtype=torch.int32)
+
+            def logprobs(z=z, t=t):
+                out = before.token_logprobs(z, t, n_top=7)
+                return [*out.values(), before.token_logprobs_grad(z, t, out, grad_logprob=torch.ones_like(t, dtype=torch.float32))]
+            calls[f"log-probabilities {M} {V} {dtype}"] = logprobs
+    for dtype, V_d, k in (("bf16", 301, [3, 5]), ("f32", 301, [3, 5]), ("bf16", 20003, [2]), ("f32", 20003, [4] * 20), ("bf16", 20003, [4] * 20)):
+        case = make_case(CaseSpec(name="loss", dtype=dtype, d=8, V_t=21000, V_d=V_d, k=k, temperature=[1.0] * len(k), n_direct=240, n_ngram=80, ngram_len=(2, 4),
+                                  plant_cover=0.5, align=0.5, data_seed=1, philox_seed=2, logits_only=True))
+        v = Verifier.for_case(case)
+        opened.append(v)
+        inp = v.upload(case)
+        v.step(inp, from_logits=True)
+        calls[f"loss {dtype} {V_d} {len(k)}"] = lambda v=v, inp=inp: [x for x in v.distill_loss_grad(inp, from_logits=True).values() if x is not None]
+    for name, call in calls.items():
+        print(name, flush=True)
+        got = []
+        for hidden in fill:
+            before.lm_head(hidden)
+            got.append([r.cpu() for r in call()])
+        for a, b in zip(*got):
+            assert torch.equal(a.nan_to_num(), b.nan_to_num()) and torch.equal(a.isnan(), b.isnan()), name
+    for v in opened:
+        v.close()
