@@ -8,8 +8,13 @@
 //                     and in the first one c q_i (a_i - A) as above with Eq. 2's overrides: a_i = r(t_pre) at the first sub-token,
 //                     0 at the pre-image of t_ng.  (pi, the product of the sub-tokens' q, moves q'(t_ng) = pi and
 //                     q'(t_pre) = q(d_1) - pi against each other.)
-// A needs no sum of its own over the target row: the loss has left sum q' (ln q' - ln p), so A is that plus the mass of q on the ids that
+// A needs no sum of its own over the target row: it is sum q' (ln q' - ln p), the loss's value, plus the mass of q on the ids that
 // have an image (less and plus the overrides' terms).
+//
+// Two forms (loss_grad_in_one): behind the loss's launch, which leaves that value and the mass, a gather from the target row by
+// draft id (loss_grad_kernel); or loss and gradient of a draft row in one workgroup (loss_row_kernel), which reads the target row in order.
+// Bound by memory: every 128-byte line of a target row holds an image, so it is read whole.  128 rows of 32000 ids against 128256 30 us
+// (2.7 TB/s: a chain of steps per row, one row per workgroup, below), 384 against 152064 65 us (3.7 TB/s).
 #include "device_math.h"
 #include "otv_internal.h"
 
@@ -120,8 +125,8 @@ __device__ inline RowGrad make_row(const LossGradArgs& a, int drow, int lane) {
 }
 
 // Grid = groups of draft ids x draft rows, the groups of a row on one XCD back to back, so that its L2 holds the target row that they gather
-// from (across all of them: 58 us for 128 rows of 32000 ids with the loss in front).  A thread has whole vectors of its row, laid out from the 16-byte boundary at or before the row's
-// start; the row's ends go element by element.
+// from (across all of them: 58 us for 128 rows of 32000 ids with the loss in front).  A thread has whole vectors of its row, laid out from
+// the 16-byte boundary at or before the row's start; the row's ends go element by element.
 constexpr int kGradVecs = 2;
 template <typename T>
 constexpr int kGradIds = 256 * kGradVecs * Draft<T>::kElems;
@@ -208,6 +213,8 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 //   loss_row_kernel      one workgroup per draft row.  It walks the mapped pairs in ascending target id, so that the target row is read in
 //                        order, and leaves each logit in LDS at its draft id; then it walks its draft row, which it holds in registers, for
 //                        q, r and their sums, and a second time for the gradient.  The last workgroup of all forms the loss's totals.
+// Of 30 us for 128 rows of 32000 ids the record's round trip takes 2.7, clearing LDS 1.7, the pairs 9.7, the two sweeps 2.2 and 1.4, the sums
+// 2.6, arrival and totals 2.4, and the launch in front 4.
 // What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
 // sum q t gets the constants' part as their 64-bit difference times the mass of q.
 struct alignas(16) GradRow {

@@ -6,6 +6,12 @@
 // then the group's scale multiplies 16 rows x 16 columns in four instructions.  Products of a bf16 number and 16 + c are exact in
 // fp32, so what is rounded is the sums alone; they are at most 31 / |c - zp| times as large as with the centred codes, which
 // costs less than the fp32 rounding of a group's scaled sum in the total over the groups.
+//
+// What bounds it, groups of 128, weights from memory: up to 16 rows the weight stream (6 rows x 3584 x 152064 53-56 us, 5.3 TB/s, what a
+// large copy moves; a bf16 head 163); above, the trips through LDS and registers between the products: 144 x 4096 x 128256 167-175 us, 0.9
+// PFLOP/s, where the products alone take 95 and the weights 55.  With parts of the work left out (timing only): LDS reads 35 us less, staging
+// 24, dequantisation 4, scaling 0.  Wavefronts of 64 columns, one per SIMD, with 32 x 32 x 16 products took 314 us, two blocks of 128 per
+// barrier at nine row tiles 185.
 #include <algorithm>
 
 #include "device_math.h"
@@ -209,10 +215,11 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
   }
 }
 
-// More than 16 rows: blocks of RT tiles of 16 rows.  A wavefront owns S tiles of 16 columns over the whole hidden dimension; the block's
+// More than 16 rows: blocks of RT tiles of 16 rows, so that weights are read and dequantised once for up to 144 rows.  A wavefront owns S tiles of 16 columns over the whole hidden dimension; the block's
 // hidden rows come through LDS in chunks of kBlocks * 128 hidden indices, two buffers, one barrier per chunk.  A wavefront stages whole
 // (row tile, block) units, in the order of the matrix instruction's operand, and forms their groups' sums on the way (a product with ones).
 constexpr int kTallWaves = 8;
+// Blocks per chunk: as many as registers and LDS hold (36 rows x 128256 with two instead of one 78.5 us instead of 82.2).
 constexpr int tall_blocks(int RT, int S) { return S > 2 ? (RT <= 4 ? 2 : 1) : RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }
 template <int RT, int S, int kSteps, int kAhead>
 __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint16_t* __restrict__ H, int M, int d, QuantHead q, float* __restrict__ Z,
@@ -389,6 +396,9 @@ hipError_t launch_rows16(const uint16_t* H, int M, int d, const QuantHead& q, fl
   return hipGetLastError();
 }
 
+// One workgroup per compute unit and round, of 16 wavefronts: its column tiles, up to four per wavefront, side by side, and where they are
+// fewer than the wavefronts, as many parts of the hidden dimension as there are wavefronts for.  Without the parts 6 rows x 152064 take 55.9
+// us instead of 54.3, the rest is the same within 2 % (with 8 wavefronts of twice the tiles 57.3): the loads in flight are enough.
 template <int kSteps>
 hipError_t launch_up_to_16(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
   const int rounds = ceil_div(q.tiles, 64 * n_cu), per_cu = ceil_div(q.tiles, rounds * n_cu);
@@ -401,6 +411,7 @@ hipError_t launch_up_to_16(const uint16_t* H, int M, int d, const QuantHead& q, 
   }
 }
 
+// Weights four blocks ahead, two where the registers do not hold four.
 template <int RT, int S, int kSteps>
 hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int m_blocks, int waves, hipStream_t stream) {
   constexpr int kAhead = S <= 2 && (kSteps == 4 || RT <= 4) ? 4 : 2;
@@ -410,6 +421,16 @@ hipError_t launch_tall(const uint16_t* H, int M, int d, const QuantHead& q, floa
   return hipGetLastError();
 }
 
+// Blocks of at most nine row tiles (a tenth would not fit the registers beside two column tiles).  Of the column tiles S per wavefront and the
+// 8 to 6 wavefronts per workgroup, those whose rounds of the chip take least: a round lasts as long as a workgroup has column tiles, and a
+// column tile costs 6 : 7 : 8 at four, two and one per wavefront, which share what is read from LDS.  Measured, us, groups of 128:
+//   rows x 128256, d = 4096   4 tiles  2      1              rows x 152064, d = 4096   chosen        least rounds alone   8 wavefronts alone
+//   24                        62.7     74.6   74.9           24                        86.1 (2 x 7)  88.4                 90.0
+//   48                        75.4     86.9   98.0           80                        155           175                  175
+//   80                        100.8    118.8  145.8          144                       224           267                  267
+//   144 (nine row tiles)      -        172    219
+// and 24 rows x 32003, d = 2056: one tile 14.5, two 18.2 (half of the compute units idle).  Four tiles fit the registers with one scale
+// per block of 128 and up to five row tiles.
 template <int kSteps>
 hipError_t launch_above_16(const uint16_t* H, int M, int d, const QuantHead& q, float* Z, int V_t, int64_t ldz, int n_cu, hipStream_t stream) {
   const int m_blocks = ceil_div(M, 9 * 16), RT = ceil_div(M, 16 * m_blocks);
@@ -418,7 +439,7 @@ hipError_t launch_above_16(const uint16_t* H, int M, int d, const QuantHead& q, 
   int64_t best = INT64_MAX;
   for (int s = 1; s <= most; s *= 2)
     for (int w = 8; w >= 6; --w) {
-      const int64_t cost = (int64_t)ceil_div((int64_t)ceil_div(q.tiles, s * w) * m_blocks, n_cu) * s * w;
+      const int64_t cost = (int64_t)ceil_div((int64_t)ceil_div(q.tiles, s * w) * m_blocks, n_cu) * s * w * (s == 4 ? 6 : s == 2 ? 7 : 8);
       if (cost < best || (cost == best && s > S)) { best = cost; S = s; waves = w; }
     }
 #define OT_TALL(rt, s) if (RT == rt && S == s) return launch_tall<rt, s, kSteps>(H, M, d, q, Z, V_t, ldz, m_blocks, waves, stream)
