@@ -465,17 +465,20 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
                          const ot_loss_config* cfg, ot_loss_out* out, const float* grad_loss, void* grad) {
   if (ctx)
     if (const int bad = ot_check_device(ctx, "ot_distill_loss_grad")) return bad;
-  if (in && in->B > 0 && in->row_off_host && in->row_off_host[in->B] > in->B && !grad)
-    return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
-  if (ctx && reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
+  if (const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, true)) return bad;   // the offsets are read below
+  const int K = in->B > 0 ? in->row_off_host[in->B] - in->B : 0;
+  if (K > 0 && !grad) return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
+  if (reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad is not aligned to its type");
+  if (K > 0 && grad == in->draft_logits)
+    return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad must not be the drafter's logits, which other rows' gradients read");
   // where the gradient's launches take rows of this size they do the loss's work as well (without the q' rows)
-  const bool in_one = ctx && in && out && in->B > 0 && in->row_off_host && !out->qprime &&
-                      loss_grad_in_one(in->row_off_host[in->B] - in->B, ctx->V_d, ctx->n_cu);
-  const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, in_one);
-  if (bad != OT_OK || in->B == 0) return bad;
+  const bool in_one = !out->qprime && loss_grad_in_one(K, ctx->V_d, ctx->n_cu);
+  if (!in_one)
+    if (const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, false)) return bad;
+  if (in->B == 0) return OT_OK;
   LossGradArgs a{};
-  a.B = in->B; a.K = in->row_off_host[in->B] - in->B; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
+  a.B = in->B; a.K = K; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
   a.approx_kl = cfg->ngram_term == OT_NGRAM_TERM_APPROX_KL;
   a.row_off = in->row_off; a.temperature = in->temperature; a.draft_temperature = in->draft_temperature;
   a.draft_logits = in->draft_logits; a.draft_ids = in->draft_ids; a.dmap = ctx->dmap; a.tmap = ctx->tmap;

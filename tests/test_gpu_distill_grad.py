@@ -247,6 +247,8 @@ def test_refusals_and_an_empty_batch():
     assert code(grad=None) == ot.OT_ERR_NULL and code(grad=grad.data_ptr() + 2) == ot.OT_ERR_SHAPE and code(lambda_mode=5) == ot.OT_ERR_SHAPE
     assert code(ngram_term=2) == ot.OT_ERR_SHAPE and code(B=-1) == ot.OT_ERR_SHAPE and code(B=99) == ot.OT_ERR_SHAPE
     assert code(buffers=dict(buf, kl=None)) == ot.OT_ERR_NULL
+    assert code(B=99, grad=None) == ot.OT_ERR_SHAPE      # sizes first: the offsets of 99 sequences are not there
+    assert code(grad=inp["draft_logits"]) == ot.OT_ERR_SHAPE
     with pytest.raises(ValueError):
         v.distill_loss_grad(inp, from_logits=True, grad_loss=torch.ones(1, dtype=torch.float64, device="cuda:0"))
     empty = dict({n: None for n in names}, B=0, step=0, seed=0)

@@ -148,6 +148,28 @@ def test_other_heads_give_their_steps_logits(dtype, M):
     np.testing.assert_array_equal(got, want)
 
 
+@pytest.mark.parametrize("head,M", [("bf16", 1), ("bf16", 30), ("bf16", 200), ("f32", 5), ("f32", 40), ("4 bit", 3), ("4 bit", 40)])
+def test_rows_of_logits_anywhere(head, M):
+    """Rows an odd number of elements apart, from any element on: the same logits, and nothing between the rows is written."""
+    from paper_2507_02659_amd import binding as ot
+    from paper_2507_02659_amd.runner import Verifier
+    d, V, ld = 520, 1003, 1009
+    dtype = torch.float32 if head == "f32" else torch.bfloat16
+    if head == "4 bit":
+        v = _verifier(_weights(np.random.default_rng(M), d, V, 64, "bf16", True)[0], M)
+    else:
+        v = Verifier(d=d, V_t=V, V_d=1, dtype=head, W=torch.randn(d, V, device=DEV).to(dtype), direct_map=np.zeros(1, np.int32), max_batch=M, max_k=0)
+    h = torch.randn(M, d, device=DEV).to(dtype)
+    want = v.lm_head(h)
+    for start in (0, 1, 2, 3):
+        memory = torch.full((M * ld + 8,), -7.0, device=DEV)
+        ot.ot_lm_head(v.ctx, M, h, memory.data_ptr() + 4 * start, ld)
+        rows = memory[start: start + M * ld].view(M, ld)
+        assert torch.equal(rows[:, :V], want)
+        assert (rows[:, V:] == -7).all() and (memory[:start] == -7).all() and (memory[start + M * ld:] == -7).all()
+    v.close()
+
+
 @pytest.mark.parametrize("draft_side", ["AUTO", "IN_LM_HEAD"])
 def test_a_step_through_a_quantized_head(draft_side):
     """Against the step of the oracle on the head's own logits: integers equal, probabilities to 1e-3."""
