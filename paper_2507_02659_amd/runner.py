@@ -5,7 +5,9 @@ verification path happens here; every stage runs in libotverify's kernels.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
+import itertools
 from dataclasses import dataclass
 from typing import Optional
 
@@ -55,7 +57,11 @@ class QuantWeights:
 
 
 class Verifier:
-    """One library context plus (optionally) one n-gram cache, for batches of a fixed model shape."""
+    """One library context plus (optionally) one n-gram cache, for batches of a fixed model shape.
+
+    Work is enqueued on `stream` (None: the default stream).  Inputs have to be ready on it, and outputs are ready on it."""
+
+    _numbers = itertools.count()
 
     def __init__(self, *, d, V_t, V_d, dtype: str, W, direct_map, max_batch, max_k, max_ngram_len=2,
                  device="cuda:0", stream: Optional[torch.cuda.Stream] = None, draft_side: int = ot.OT_DRAFT_SIDE_AUTO):
@@ -65,6 +71,7 @@ class Verifier:
         self.dtype = dtype
         self.d, self.V_t, self.V_d = d, V_t, V_d
         self.stream = stream
+        self._number = next(self._numbers)          # of this verifier, never used again
         torch.cuda.set_device(self.device)
         common = dict(d=d, V_t=V_t, V_d=V_d, max_batch=max_batch, max_k=max_k, max_ngram_len=max_ngram_len, direct_map=direct_map,
                       dtype=ot.OT_BF16 if dtype == "bf16" else ot.OT_F32, stream=None if stream is None else stream.cuda_stream,
@@ -187,14 +194,16 @@ class Verifier:
         dev = self.device
         M = max(inp["M"], 1)
         key = ("loss_buffers", M, with_qprime)
-        buf = inp.get(key)
+        buf = inp.get(key + (self._number,))        # a batch may go through several verifiers, each on its stream and with its V_t
         if buf is None:
-            buf = {"kind": torch.full((M,), -7, dtype=torch.int32, device=dev),
-                   "totals": torch.full((5,), -7.0, dtype=torch.float64, device=dev)}
-            buf.update({n: torch.full((M,), -7.0, dtype=torch.float64, device=dev) for n in ("kl", "nll", "weight")})
-            if with_qprime:
-                buf["qprime"] = torch.full((M, self.V_t), -7.0, dtype=torch.float32, device=dev)
-            inp[key] = buf
+            with self._on_stream():                 # the loss writes them there: filled anywhere else, they could be filled after it
+                buf = {"kind": torch.full((M,), -7, dtype=torch.int32, device=dev),
+                       "totals": torch.full((5,), -7.0, dtype=torch.float64, device=dev)}
+                buf.update({n: torch.full((M,), -7.0, dtype=torch.float64, device=dev) for n in ("kl", "nll", "weight")})
+                if with_qprime:
+                    buf["qprime"] = torch.full((M, self.V_t), -7.0, dtype=torch.float32, device=dev)
+            inp[key + (self._number,)] = buf
+        inp[key] = buf                              # the last call's
         return buf
 
     def distill_loss_grad(self, inp: dict, *, from_logits: bool = False, lam: float = 0.2, lambda_mode: int = ot.OT_LAMBDA_FIXED,
@@ -218,11 +227,15 @@ class Verifier:
         return dict(buf, grad=grad)
 
     # ------------------------------------------------------------------ logits and log-probabilities
+    def _on_stream(self):
+        """Makes the verifier's stream the current one."""
+        return contextlib.nullcontext() if self.stream is None else torch.cuda.stream(self.stream)
+
     def _empty(self, shape, dtype) -> torch.Tensor:
         """Memory for outputs that work on the verifier's stream writes."""
         if self.stream is None:
             return torch.empty(shape, dtype=dtype, device=self.device)
-        with torch.cuda.stream(self.stream):
+        with self._on_stream():
             return torch.empty(shape, dtype=dtype, device=self.device)
 
     def lm_head(self, hidden: torch.Tensor) -> torch.Tensor:
