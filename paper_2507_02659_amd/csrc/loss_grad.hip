@@ -124,6 +124,21 @@ __device__ inline RowGrad make_row(const LossGradArgs& a, int drow, int lane) {
   return R;
 }
 
+// ln q of a draft logit, and ln p of a target logit, of a row.
+__device__ inline double ln_q(const RowGrad& R, float x) { return ((double)x - R.mxq) * R.invTd - R.lnSq; }
+__device__ inline double ln_p(const RowGrad& R, float z) { return ((double)z - R.mx) * R.invT - R.lnS; }
+// The gradient at draft id i of a row with (kKl) or without a KL part; x: its logit, z: the target's logit at its image.
+template <bool kKl>
+__device__ inline float grad_at(const RowGrad& R, int i, float x, int image, float z) {
+  const double lq = ln_q(R, x), q = exp_neg_fast(lq), pull = R.D * ((i == R.sub ? 1.0 : 0.0) - q);
+  if (!kKl) return (float)pull;
+  double r = image >= 0 && i != R.out ? lq - ln_p(R, z) + 1.0 : 0.0;
+  if (i == R.pre) r = R.a_pre;
+  double g = q > 0.0 ? R.c * q * (r - R.A) : 0.0;
+  if (R.kind & 2) g += pull;
+  return (float)g;
+}
+
 // Grid = groups of draft ids x draft rows, the groups of a row on one XCD back to back, so that its L2 holds the target row that they gather
 // from (across all of them: 58 us for 128 rows of 32000 ids with the loss in front).  A thread has whole vectors of its row, laid out from
 // the 16-byte boundary at or before the row's start; the row's ends go element by element.
@@ -178,21 +193,10 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 #pragma unroll
     for (int e = 0; e < kEach; ++e) zv[e] = z[max(image[e], 0)];
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = first(e / kVec) + e % kVec;
-      const double lq = ((double)x[e] - R.mxq) * R.invTd - R.lnSq, q = exp_neg_fast(lq);
-      double r = image[e] >= 0 && i != R.out ? lq - (((double)zv[e] - R.mx) * R.invT - R.lnS) + 1.0 : 0.0;
-      if (i == R.pre) r = R.a_pre;
-      double g = q > 0.0 ? R.c * q * (r - R.A) : 0.0;
-      if (R.kind & 2) g += R.D * ((i == R.sub ? 1.0 : 0.0) - q);
-      out[e] = (float)g;
-    }
+    for (int e = 0; e < kEach; ++e) out[e] = grad_at<true>(R, first(e / kVec) + e % kVec, x[e], image[e], zv[e]);
   } else {
 #pragma unroll
-    for (int e = 0; e < kEach; ++e) {
-      const int i = first(e / kVec) + e % kVec;
-      out[e] = R.kind ? (float)(R.D * ((i == R.sub ? 1.0 : 0.0) - exp_neg_fast(((double)x[e] - R.mxq) * R.invTd - R.lnSq))) : 0.f;
-    }
+    for (int e = 0; e < kEach; ++e) out[e] = R.kind ? grad_at<false>(R, first(e / kVec) + e % kVec, x[e], -1, 0.f) : 0.f;
   }
 #pragma unroll
   for (int i = 0; i < kGradVecs; ++i) {
@@ -217,6 +221,9 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 // 2.6, arrival and totals 2.4, and the launch in front 4.
 // What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
 // sum q t gets the constants' part as their 64-bit difference times the mass of q.
+// Of temperatures below 2.1e-8 (kMostScale) that arithmetic leaves float32's range (exponents of -1e30 for masked ids, differences of a
+// target that the temperature tears apart): such rows are done as the other form does all of them, in 64 bits and from memory.
+constexpr float kMostScale = 0x1p26f;
 struct alignas(16) GradRow {
   float mx, mxq;                // t = (zq - mxq) * s2q and (z - mx) * s2: exponents to base 2, s2 as two floats
   float s2, s2_lo, s2q;         // (the row sums' exponents were formed with one float of log2(e)/Td as well)
@@ -224,7 +231,9 @@ struct alignas(16) GradRow {
   double dlnS;                  // lnS - lnSq
   double c, D, a_pre;           // c and D without grad_loss / n
   double kl_more, A_more;       // what Eq. 2's overrides add to the KL sum and to A
-  int32_t kind, row, sub, out, pre;
+  double invTd, lnSq, invT, lnS;   // for rows in 64 bits
+  int32_t kind;                 // RowGrad's, and 4: in 64 bits
+  int32_t row, sub, out, pre;
 };
 static_assert(sizeof(GradRow) % 16 == 0, "read as 16-byte units");
 
@@ -318,7 +327,9 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
   R.kl_more = __shfl(kl_more, j); R.A_more = __shfl(A_more, j);
   R.out = __shfl(out, j); R.pre = __shfl(pre, j); R.sub = id;
   const int ngram_kl_j = __shfl((int)ngram_kl, j);
+  R.invTd = invTd; R.lnSq = lnSq; R.invT = invT; R.lnS = __shfl(lnS, j);
   R.kind = !covered ? 0 : kind_j == 1 ? 1 : !ngram_kl_j ? 2 : is_first ? 3 : 2;
+  if (R.kind != 0 && !(fmaxf(R.s2, R.s2q) <= kMostScale)) R.kind |= 4;
   if (lane < k) static_cast<GradRow*>(a.rows)[q0 + lane] = R;
 }
 
@@ -410,8 +421,38 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   float A = 0.f;
   asm volatile("" ::"v"(scale));                         // read by now
   __syncthreads();
-  if (R.kind & 1) {
-    const float* z = a.Z + (int64_t)R.row * a.ldz;
+  const float* z = a.Z + (int64_t)R.row * a.ldz;
+  const bool wide = (R.kind & 4) != 0;                   // in 64 bits
+  if (wide) {
+    RowGrad X;
+    X.mxq = (double)R.mxq; X.invTd = R.invTd; X.lnSq = R.lnSq; X.mx = (double)R.mx; X.invT = R.invT; X.lnS = R.lnS;
+    X.c = R.c * (double)up / (double)max(1, n_tokens); X.D = R.D * (double)up / (double)max(1, n_tokens);
+    X.a_pre = R.a_pre; X.kind = R.kind; X.sub = R.sub; X.out = R.out; X.pre = R.pre;
+    double kl = 0.0, mass = 0.0;
+    for (int i = tid; (R.kind & 1) && i < a.V_d; i += kRowThreads) {
+      const int image = a.dmap[i];
+      if (image < 0 || i == R.out || i == R.pre) continue;
+      const double lq = ln_q(X, Draft<T>::one(zq + i)), q = exp_neg_fast(lq);
+      mass += q;
+      if (q > 0.0) kl += q * (lq - ln_p(X, z[image]));
+    }
+    kl = wave_sum(kl);
+    mass = wave_sum(mass);
+    if (lane == 0) { s_term[2][wave] = kl; s_term[3][wave] = mass; }
+    __syncthreads();
+    kl = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
+    mass = wave_sum(lane < 16 ? s_term[3][lane] : 0.0);
+    X.A = kl + mass + R.A_more;
+    for (int i = tid; i < a.V_d; i += kRowThreads) {
+      const float xi = Draft<T>::one(zq + i);
+      const int image = R.kind & 1 ? a.dmap[i] : -1;
+      Draft<T>::store_one(grad + i, R.kind & 1 ? grad_at<true>(X, i, xi, image, z[max(image, 0)]) : grad_at<false>(X, i, xi, -1, 0.f));
+    }
+    if (tid == 0) {
+      if (R.kind & 1) publish(a.out.kl + R.row, kl + R.kl_more);
+      count_in();
+    }
+  } else if (R.kind & 1) {
     // a turn's logits are asked for a turn ahead, their ids two
     float zv[kPairs];
     int2 id_next[kPairs];
@@ -501,7 +542,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {
     const int base = (i * kRowThreads + tid) * kVec;
-    if (base >= shift + a.V_d) break;
+    if (wide || base >= shift + a.V_d) break;
     float out[kVec];
     if (R.kind & 1) {                                    // the thread's own words, which it wrote above, but for R.pre's
 #pragma unroll
