@@ -221,8 +221,10 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 // 2.6, arrival and totals 2.4, and the launch in front 4.
 // What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
 // sum q t gets the constants' part as their 64-bit difference times the mass of q.
-// Of temperatures below 2.1e-8 (kMostScale) that arithmetic leaves float32's range (exponents of -1e30 for masked ids, differences of a
-// target that the temperature tears apart): such rows are done as the other form does all of them, in 64 bits and from memory.
+// Rows for which that arithmetic leaves float32's range are done as the other form does all of them, in 64 bits and from memory: those of
+// temperatures below 2.1e-8 (kMostScale), where exponents overflow; and those that propose an id which the target masks (with -inf, or with a
+// number as low as -1e20): its term is infinite or nearly, however small q is, and a q below 2^-126 is not there in float32.  An n-gram's
+// overrides that the target masks show in the record's numbers.
 constexpr float kMostScale = 0x1p26f;
 struct alignas(16) GradRow {
   float mx, mxq;                // t = (zq - mxq) * s2q and (z - mx) * s2: exponents to base 2, s2 as two floats
@@ -329,7 +331,8 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
   const int ngram_kl_j = __shfl((int)ngram_kl, j);
   R.invTd = invTd; R.lnSq = lnSq; R.invT = invT; R.lnS = __shfl(lnS, j);
   R.kind = !covered ? 0 : kind_j == 1 ? 1 : !ngram_kl_j ? 2 : is_first ? 3 : 2;
-  if (R.kind != 0 && !(fmaxf(R.s2, R.s2q) <= kMostScale)) R.kind |= 4;
+  const double most = fmax(fmax(fabs(R.a_pre), fabs(R.A_more)), fabs(R.D) + fabs(R.c));   // (a NaN of D shows in the comparison)
+  if (R.kind != 0 && !(fmaxf(R.s2, R.s2q) <= kMostScale && most <= 1e20)) R.kind |= 4;
   if (lane < k) static_cast<GradRow*>(a.rows)[q0 + lane] = R;
 }
 
@@ -372,7 +375,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   constexpr int kVec = Draft<T>::kElems, kEach = kVecs * kVec, kPairs = 8;
   extern __shared__ __attribute__((aligned(16))) float s_z[];   // [shift + id]: the target's logit at the id's image, then r
   __shared__ double s_term[4][16];
-  __shared__ int s_last;
+  __shared__ int s_last, s_far;
   const int drow = blockIdx.x, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const T* zq = static_cast<const T*>(a.draft_logits) + (int64_t)drow * a.V_d;
   T* grad = static_cast<T*>(a.grad) + (int64_t)drow * a.V_d;
@@ -420,39 +423,11 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   };
   float A = 0.f;
   asm volatile("" ::"v"(scale));                         // read by now
+  if (tid == 0) s_far = R.kind & 4;
   __syncthreads();
   const float* z = a.Z + (int64_t)R.row * a.ldz;
-  const bool wide = (R.kind & 4) != 0;                   // in 64 bits
-  if (wide) {
-    RowGrad X;
-    X.mxq = (double)R.mxq; X.invTd = R.invTd; X.lnSq = R.lnSq; X.mx = (double)R.mx; X.invT = R.invT; X.lnS = R.lnS;
-    X.c = R.c * (double)up / (double)max(1, n_tokens); X.D = R.D * (double)up / (double)max(1, n_tokens);
-    X.a_pre = R.a_pre; X.kind = R.kind; X.sub = R.sub; X.out = R.out; X.pre = R.pre;
-    double kl = 0.0, mass = 0.0;
-    for (int i = tid; (R.kind & 1) && i < a.V_d; i += kRowThreads) {
-      const int image = a.dmap[i];
-      if (image < 0 || i == R.out || i == R.pre) continue;
-      const double lq = ln_q(X, Draft<T>::one(zq + i)), q = exp_neg_fast(lq);
-      mass += q;
-      if (q > 0.0) kl += q * (lq - ln_p(X, z[image]));
-    }
-    kl = wave_sum(kl);
-    mass = wave_sum(mass);
-    if (lane == 0) { s_term[2][wave] = kl; s_term[3][wave] = mass; }
-    __syncthreads();
-    kl = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
-    mass = wave_sum(lane < 16 ? s_term[3][lane] : 0.0);
-    X.A = kl + mass + R.A_more;
-    for (int i = tid; i < a.V_d; i += kRowThreads) {
-      const float xi = Draft<T>::one(zq + i);
-      const int image = R.kind & 1 ? a.dmap[i] : -1;
-      Draft<T>::store_one(grad + i, R.kind & 1 ? grad_at<true>(X, i, xi, image, z[max(image, 0)]) : grad_at<false>(X, i, xi, -1, 0.f));
-    }
-    if (tid == 0) {
-      if (R.kind & 1) publish(a.out.kl + R.row, kl + R.kl_more);
-      count_in();
-    }
-  } else if (R.kind & 1) {
+  bool wide = (R.kind & 4) != 0;                         // in 64 bits; the same in all threads
+  if ((R.kind & 1) && !wide) {
     // a turn's logits are asked for a turn ahead, their ids two
     float zv[kPairs];
     int2 id_next[kPairs];
@@ -500,20 +475,11 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
           const float diff = near ? (tq - fmaf(d, R.s2, d * R.s2_lo)) * 0.69314718f : 0.f;
           kl_i = fmaf(q, diff, kl_i);
           mass_i += ordinary ? q : 0.f;
-          far |= ordinary && !near && q > 0.f;
-          zr[e] = near ? diff + R.r0 : ordinary ? zr[e] : 0.f;
+          far |= ordinary && !near && tq > -1080.f;      // in 64 bits q may be above 0
+          zr[e] = near ? diff + R.r0 : 0.f;
           x[i * kVec + e] = q;
         }
-        if (__any(far)) {                                // masked by the target: with -inf the term is infinite, with a lowest number nearly
-#pragma unroll
-          for (int e = 0; e < kVec; ++e) {
-            const double d = (double)zr[e] - (double)R.mx;
-            if (d < -1e20 && x[i * kVec + e] > 0.f) {    // (an r is not that small)
-              kl += (double)x[i * kVec + e] * (-d * (double)R.s2 * 0.6931471805599453);
-              zr[e] = d < -1e300 ? INFINITY : (float)fmin(-d * (double)R.s2 * 0.6931471805599453, 3.0e38);
-            }
-          }
-        }
+        if (far) s_far = 4;
 #pragma unroll
         for (int e = 0; e < kVec; e += 4) *reinterpret_cast<f32x4*>(s_z + base + e) = f32x4{zr[e], zr[e + 1], zr[e + 2], zr[e + 3]};
         kl += (double)kl_i;
@@ -524,6 +490,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     mass = wave_sum(mass);
     if (lane == 0) { s_term[0][wave] = kl; s_term[1][wave] = mass; }
     __syncthreads();
+    wide = s_far != 0;
     kl = wave_sum(lane < 16 ? s_term[0][lane] : 0.0);
     mass = wave_sum(lane < 16 ? s_term[1][lane] : 0.0);
     kl += R.dlnS * mass;                                 // sum over ordinary ids of q (ln q - ln p)
@@ -532,12 +499,42 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
       if (tid == 0 && R.pre >= 0) s_z[shift + R.pre] = (float)R.a_pre;
       __syncthreads();
     }
-    if (tid == 0) {
+    if (tid == 0 && !wide) {
       publish(a.out.kl + R.row, kl + R.kl_more);
       count_in();
     }
-  } else if (tid == 0) {
+  } else if (!wide && tid == 0) {
     count_in();
+  }
+  if (wide) {
+    RowGrad X;
+    X.mxq = (double)R.mxq; X.invTd = R.invTd; X.lnSq = R.lnSq; X.mx = (double)R.mx; X.invT = R.invT; X.lnS = R.lnS;
+    X.c = R.c * (double)up / (double)max(1, n_tokens); X.D = R.D * (double)up / (double)max(1, n_tokens);
+    X.a_pre = R.a_pre; X.kind = R.kind; X.sub = R.sub; X.out = R.out; X.pre = R.pre;
+    double kl = 0.0, mass = 0.0;
+    for (int i = tid; (R.kind & 1) && i < a.V_d; i += kRowThreads) {
+      const int image = a.dmap[i];
+      if (image < 0 || i == R.out || i == R.pre) continue;
+      const double lq = ln_q(X, Draft<T>::one(zq + i)), q = exp_neg_fast(lq);
+      mass += q;
+      if (q > 0.0) kl += q * (lq - ln_p(X, z[image]));
+    }
+    kl = wave_sum(kl);
+    mass = wave_sum(mass);
+    if (lane == 0) { s_term[2][wave] = kl; s_term[3][wave] = mass; }
+    __syncthreads();
+    kl = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
+    mass = wave_sum(lane < 16 ? s_term[3][lane] : 0.0);
+    X.A = kl + mass + R.A_more;
+    for (int i = tid; i < a.V_d; i += kRowThreads) {
+      const float xi = Draft<T>::one(zq + i);
+      const int image = R.kind & 1 ? a.dmap[i] : -1;
+      Draft<T>::store_one(grad + i, R.kind & 1 ? grad_at<true>(X, i, xi, image, z[max(image, 0)]) : grad_at<false>(X, i, xi, -1, 0.f));
+    }
+    if (tid == 0) {
+      if (R.kind & 1) publish(a.out.kl + R.row, kl + R.kl_more);
+      count_in();
+    }
   }
 #pragma unroll
   for (int i = 0; i < kVecs; ++i) {

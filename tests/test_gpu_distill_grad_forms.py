@@ -30,3 +30,47 @@ def test_tiny_target_temperatures(dtype, with_qprime):
     temps = [1.0, 3e-8, 2e-8, 1e-9, 1e-20, 1e-30]
     case = make_case(_spec("tiny_target", [5, 3, 6, 4, 4, 7], 43, dtype=dtype, temperature=temps, draft_temperature=[1.0, 0.7, 1.0, 1.0, 0.5, 1.0]))
     _compare(case, modes=MODES, with_qprime=with_qprime)
+
+
+def _two_forms(case, **how):
+    """ot_distill_loss, and the gradient's outputs of both forms, as numpy arrays."""
+    from paper_2507_02659_amd.runner import Verifier
+    v = Verifier.for_case(case)
+    inp = v.upload(case)
+    v.step(inp, from_logits=True)
+    loss = v.distill_loss(inp, from_logits=True, **how)
+    got = [{n: t.double().cpu().numpy() for n, t in v.distill_loss_grad(inp, from_logits=True, with_qprime=q, **how).items()} for q in (False, True)]
+    v.close()
+    return loss, got
+
+
+def _tail_ids(case, b, td):
+    """Mapped draft ids of sequence b's first row whose q is there in 64 bits and below 2^-126 at the draft temperature."""
+    row = np.asarray(case.draft_logits[int(case.row_off[b]) - b], np.float64) / td
+    lq = row - row.max() - np.log(np.exp(row - row.max()).sum())
+    return np.flatnonzero((lq < -90) & (lq > -600) & (case.direct_map >= 0))
+
+
+@pytest.mark.parametrize("V_t,V_d,n_direct", [(600, 301, 300), (9500, 9001, 9000)])
+def test_a_masked_target_under_a_tiny_probability(V_t, V_d, n_direct):
+    """The target gives 0 to an id that the drafter proposes with q' of 1e-40 and less: the term is infinite in every form."""
+    case = make_case(_spec("far", [4, 3, 5], 9, n_ngram=0, temperature=[1.0] * 3, draft_temperature=[0.05, 0.05, 1.0], n_direct=n_direct, V_t=V_t, V_d=V_d))
+    ids = _tail_ids(case, 0, 0.05)
+    assert ids.size > 3
+    case.target_logits[0, case.direct_map[ids[0]]] = -np.inf
+    loss, got = _two_forms(case)
+    assert loss["kind"][0] == 1 and loss["kl"][0] == np.inf and np.isfinite(loss["kl"][1:]).all() and loss["loss"] == np.inf
+    for g in got:
+        np.testing.assert_allclose(g["kl"][:case.M], loss["kl"], rtol=2e-6, atol=1e-6)
+        assert g["totals"][4] == np.inf
+        assert not np.isfinite(g["grad"][0]).all() and np.isfinite(g["grad"][1:]).all()
+    np.testing.assert_array_equal(np.isnan(got[0]["grad"]), np.isnan(got[1]["grad"]))
+
+
+@pytest.mark.parametrize("with_qprime", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_targets_masked_with_low_numbers(dtype, with_qprime):
+    """A third of the target's ids masked with -1e37, n-gram targets and first sub-tokens' images among them: huge terms, and finite."""
+    case = make_case(_spec("low", [5, 3, 6, 4, 4, 7], 47, dtype=dtype, temperature=[1.0, 0.7, 1.0, 1.0, 0.8, 1.0], draft_temperature=[1.0, 0.05, 1.0, 0.3, 1.0, 0.1]))
+    case.target_logits[np.random.default_rng(3).random(case.target_logits.shape) < 0.3] = -1e37
+    _compare(case, modes=MODES, with_qprime=with_qprime)
