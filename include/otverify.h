@@ -276,7 +276,8 @@ int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step_o
  * drafter's logits: grad, DEVICE [K, V_d] in cfg.dtype, not the logits themselves, written whole (zeros in the rows of draft tokens without a term).
  * grad_loss: DEVICE, one float, or NULL for 1.  p, the weights lambda and the translation are constants; q' depends on the draft
  * logits as Eq. 1 and Eq. 2 say, so with OT_NGRAM_TERM_APPROX_KL the logits of all of an n-gram's sub-tokens get a gradient.
- * An id that the drafter's logits mask (-inf) gets zero.  Where a term is infinite (the target gives 0 to a token that the drafter
+ * An id that the drafter's logits mask (-inf) gets zero, and so does a row that they mask whole, which adds nothing.  A draft row
+ * with a NaN or +inf among its logits: its KL value, the totals and its gradient are NaN.  Where a term is infinite (the target gives 0 to a token that the drafter
  * proposes with q' > 0), its rows' gradients are not finite either.                                              */
 int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step_out, const float* target_logits_or_null,
                          const ot_loss_config* cfg, ot_loss_out* out, const float* grad_loss_or_null, void* grad);

@@ -330,6 +330,7 @@ __global__ __launch_bounds__(kThreads, 4) void loss_kernel(LossArgs a, LossRowOf
       kl += R.pi * (R.ln_pi - (((double)z[R.t_ng] - R.mx) * R.invT - R.lnS));
     kl = need_kl ? block_sum<kWaves>(kl, s_term[0], wave, lane) : 0.0;
     if (kMass && need_kl) mass = block_sum<kWaves>(mass, s_term[1], wave, lane);
+    if (kMass && need_kl && R.lnSq != R.lnSq) kl = R.lnSq;   // a NaN among the draft row's logits, where no q is above 0
   }
   if (wave == 0) {
     bool row_done = need_kl || grp == 0;

@@ -8,6 +8,8 @@
 //                     and in the first one c q_i (a_i - A) as above with Eq. 2's overrides: a_i = r(t_pre) at the first sub-token,
 //                     0 at the pre-image of t_ng.  (pi, the product of the sub-tokens' q, moves q'(t_ng) = pi and
 //                     q'(t_pre) = q(d_1) - pi against each other.)
+// A draft row that the drafter's mask leaves empty has no mass: nothing is added for it, and its gradient is 0.  One with a NaN or +inf has
+// no distribution: its KL value and gradient are NaN.
 // A needs no sum of its own over the target row: it is sum q' (ln q' - ln p), the loss's value, plus the mass of q on the ids that
 // have an image (less and plus the overrides' terms).
 //
@@ -21,10 +23,14 @@
 namespace otv {
 namespace {
 
+// 0, or NaN where the row's sum is.
+__device__ inline double nan_of(double lnS) { return lnS != lnS ? lnS : 0.0; }
+
 struct RowGrad {
   double mxq, invTd, lnSq;      // ln q(i) = (zq_i - mxq) * invTd - lnSq
   double mx, invT, lnS;         // ln p(v) = (z_v - mx) * invT - lnS
   double c, A, D, a_pre;
+  double none;                  // what an id with q = 0 gets: 0, or NaN in a row without a distribution
   int32_t kind;                 // 0: zeros, 1: the KL part, 2: D alone, 3: both
   int32_t row, sub;             // the token's target row; the draft row's drafted id
   int32_t out, pre;             // draft ids whose a is 0 / a_pre, or -1
@@ -88,6 +94,7 @@ __device__ inline RowGrad make_row(const LossGradArgs& a, int drow, int lane) {
   R.invTd = 1.0 / (double)Td_b; R.invT = 1.0 / (double)T_b;
   const double lnSq_l = log(dsum_l);
   R.mxq = (double)__shfl(dmx_l, at); R.lnSq = __shfl(lnSq_l, at);
+  R.none = nan_of(R.lnSq);
   R.mx = (double)__shfl(mx_l, j); R.lnS = log(__shfl(sum_l, j));
   R.c = (double)up / n * R.invTd;
   R.kind = 1;
@@ -130,11 +137,11 @@ __device__ inline double ln_p(const RowGrad& R, float z) { return ((double)z - R
 // The gradient at draft id i of a row with (kKl) or without a KL part; x: its logit, z: the target's logit at its image.
 template <bool kKl>
 __device__ inline float grad_at(const RowGrad& R, int i, float x, int image, float z) {
-  const double lq = ln_q(R, x), q = exp_neg_fast(lq), pull = R.D * ((i == R.sub ? 1.0 : 0.0) - q);
+  const double lq = ln_q(R, x), q = exp_neg_fast(lq), pull = R.D * ((i == R.sub ? 1.0 : 0.0) - q) + R.none;
   if (!kKl) return (float)pull;
   double r = image >= 0 && i != R.out ? lq - ln_p(R, z) + 1.0 : 0.0;
   if (i == R.pre) r = R.a_pre;
-  double g = q > 0.0 ? R.c * q * (r - R.A) : 0.0;
+  double g = q > 0.0 ? R.c * q * (r - R.A) : R.none;
   if (R.kind & 2) g += pull;
   return (float)g;
 }
@@ -322,14 +329,15 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
   const double s2 = 1.4426950408889634 * invT, s2q = 1.4426950408889634 * invTd;
   R.s2 = (float)s2; R.s2_lo = (float)(s2 - (double)R.s2);
   R.s2q = (float)s2q;
-  R.inv_Sq = (float)(1.0 / Sq);
-  R.dlnS = __shfl(lnS, j) - lnSq;
+  R.inv_Sq = Sq == 0.0 ? 0.f : (float)(1.0 / Sq);
+  R.lnS = __shfl(lnS, j);
+  R.dlnS = Sq == 0.0 ? 0.0 : R.lnS - lnSq;               // (times the mass, which is 0 then)
   R.r0 = (float)(R.dlnS + 1.0);
   R.c = __shfl(c, j); R.D = __shfl(D, j); R.a_pre = __shfl(a_pre, j);
   R.kl_more = __shfl(kl_more, j); R.A_more = __shfl(A_more, j);
   R.out = __shfl(out, j); R.pre = __shfl(pre, j); R.sub = id;
   const int ngram_kl_j = __shfl((int)ngram_kl, j);
-  R.invTd = invTd; R.lnSq = lnSq; R.invT = invT; R.lnS = __shfl(lnS, j);
+  R.invTd = invTd; R.lnSq = lnSq; R.invT = invT;
   R.kind = !covered ? 0 : kind_j == 1 ? 1 : !ngram_kl_j ? 2 : is_first ? 3 : 2;
   const double most = fmax(fmax(fabs(R.a_pre), fabs(R.A_more)), fabs(R.D) + fabs(R.c));   // (a NaN of D shows in the comparison)
   if (R.kind != 0 && !(fmaxf(R.s2, R.s2q) <= kMostScale && most <= 1e20)) R.kind |= 4;
@@ -511,7 +519,8 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     X.mxq = (double)R.mxq; X.invTd = R.invTd; X.lnSq = R.lnSq; X.mx = (double)R.mx; X.invT = R.invT; X.lnS = R.lnS;
     X.c = R.c * (double)up / (double)max(1, n_tokens); X.D = R.D * (double)up / (double)max(1, n_tokens);
     X.a_pre = R.a_pre; X.kind = R.kind; X.sub = R.sub; X.out = R.out; X.pre = R.pre;
-    double kl = 0.0, mass = 0.0;
+    X.none = nan_of(X.lnSq);
+    double kl = X.none, mass = 0.0;
     for (int i = tid; (R.kind & 1) && i < a.V_d; i += kRowThreads) {
       const int image = a.dmap[i];
       if (image < 0 || i == R.out || i == R.pre) continue;

@@ -74,3 +74,35 @@ def test_targets_masked_with_low_numbers(dtype, with_qprime):
     case = make_case(_spec("low", [5, 3, 6, 4, 4, 7], 47, dtype=dtype, temperature=[1.0, 0.7, 1.0, 1.0, 0.8, 1.0], draft_temperature=[1.0, 0.05, 1.0, 0.3, 1.0, 0.1]))
     case.target_logits[np.random.default_rng(3).random(case.target_logits.shape) < 0.3] = -1e37
     _compare(case, modes=MODES, with_qprime=with_qprime)
+
+
+@pytest.mark.parametrize("approx_kl", [False, True])
+@pytest.mark.parametrize("tiny", [False, True])
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_rows_without_a_distribution(dtype, tiny, approx_kl):
+    """Draft rows that the mask leaves empty (no mass: nothing is added, gradients 0), that hold a NaN at a mapped or an unmapped id or +inf
+    (NaN), target rows without a logit above -inf and with a NaN; the rows next to them stay as they are."""
+    from paper_2507_02659_amd import binding as ot
+    bits = {"f32": (np.float32(-np.inf), np.float32(np.nan), np.float32(np.inf)), "bf16": (np.uint16(0xFF80), np.uint16(0x7FC0), np.uint16(0x7F80))}[dtype]
+    case = make_case(_spec("empty", [2] * 8, 51, dtype=dtype, n_ngram=0, n_direct=300, V_t=600, temperature=[1.0] * 8, draft_temperature=[1e-9 if tiny else 0.7] * 8))
+    mapped, unmapped = np.flatnonzero(case.direct_map >= 0), np.flatnonzero(case.direct_map < 0)
+    assert (case.direct_map[case.draft_ids] >= 0).all()
+    case.draft_logits[0] = bits[0]
+    case.draft_logits[2, mapped[7]] = bits[1]
+    case.draft_logits[4, unmapped[0]] = bits[1]
+    case.draft_logits[6, mapped[9]] = bits[2]
+    case.target_logits[12] = -np.inf                      # of draft row 8
+    case.target_logits[15, case.direct_map[mapped[0]]] = np.nan   # of draft row 10
+    how = dict(ngram_term=ot.OT_NGRAM_TERM_APPROX_KL if approx_kl else ot.OT_NGRAM_TERM_NLL)
+    loss, (one, gather) = _two_forms(case, **how)
+    assert (loss["kind"].reshape(8, 3)[:, :2] == 1).all()
+    for g in (one, gather):
+        kl, grad = g["kl"][:case.M], g["grad"]
+        assert kl[0] == 0 and not grad[0].any()
+        assert np.isnan(kl[[3, 6, 9, 12, 15]]).all() and np.isnan(g["totals"][4])
+        assert np.isnan(grad[[2, 4, 6]]).all() and np.isnan(grad[[8, 10]]).any(1).all()
+        others = np.setdiff1d(np.arange(case.K), [0, 2, 4, 6, 8, 10])
+        rows = others + others // 2
+        assert np.isfinite(grad[others]).all() and (tiny or grad[others].any())
+        np.testing.assert_allclose(kl[rows], loss["kl"][rows], rtol=2e-6, atol=1e-6)
+    np.testing.assert_array_equal(np.isnan(one["grad"]), np.isnan(gather["grad"]))
