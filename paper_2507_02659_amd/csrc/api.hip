@@ -70,20 +70,20 @@ extern "C" {
 const char* ot_last_error(void) { return g_err; }
 const char* ot_version(void) { return "otverify 0.1 (gfx950)"; }
 
-// qw: the 4-bit weights of a quantized head (already checked), or NULL: cfg->W.
-static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot_ctx** out) {
-  if (!cfg || !out) return fail(OT_ERR_NULL, "ot_verify_init: cfg and out must not be NULL");
-  if ((!qw && !cfg->W) || !cfg->direct_map) return fail(OT_ERR_NULL, "ot_verify_init: W and direct_map must not be NULL");
-  if (cfg->dtype != OT_BF16 && cfg->dtype != OT_F32) return fail(OT_ERR_DTYPE, "ot_verify_init: unknown dtype %d", cfg->dtype);
-  if (cfg->d <= 0 || cfg->V_t <= 0 || cfg->V_d <= 0) return fail(OT_ERR_SHAPE, "ot_verify_init: d, V_t, V_d must be positive");
-  if (cfg->dtype == OT_BF16 && cfg->d % 8 != 0) return fail(OT_ERR_SHAPE, "ot_verify_init: bf16 needs d %% 8 == 0 (d = %d)", cfg->d);
+// who: the entry point, for its errors; qw: the 4-bit weights of a quantized head (already checked), or NULL: cfg->W.
+static int init_impl(const char* who, const ot_verify_config* cfg, const ot_quant_weights* qw, ot_ctx** out) {
+  if (!cfg || !out) return fail(OT_ERR_NULL, "%s: cfg and out must not be NULL", who);
+  if ((!qw && !cfg->W) || !cfg->direct_map) return fail(OT_ERR_NULL, "%s: W and direct_map must not be NULL", who);
+  if (cfg->dtype != OT_BF16 && cfg->dtype != OT_F32) return fail(OT_ERR_DTYPE, "%s: unknown dtype %d", who, cfg->dtype);
+  if (cfg->d <= 0 || cfg->V_t <= 0 || cfg->V_d <= 0) return fail(OT_ERR_SHAPE, "%s: d, V_t, V_d must be positive", who);
+  if (cfg->dtype == OT_BF16 && cfg->d % 8 != 0) return fail(OT_ERR_SHAPE, "%s: bf16 needs d %% 8 == 0 (d = %d)", who, cfg->d);
   if (cfg->max_batch < 1 || cfg->max_k < 0 || cfg->max_k > OT_MAX_K)
-    return fail(OT_ERR_SHAPE, "ot_verify_init: need max_batch >= 1 and 0 <= max_k <= %d", OT_MAX_K);
+    return fail(OT_ERR_SHAPE, "%s: need max_batch >= 1 and 0 <= max_k <= %d", who, OT_MAX_K);
   if (cfg->max_ngram_len < 2 || cfg->max_ngram_len > OT_MAX_NGRAM_LEN)
-    return fail(OT_ERR_SHAPE, "ot_verify_init: max_ngram_len must be in 2..%d", OT_MAX_NGRAM_LEN);
+    return fail(OT_ERR_SHAPE, "%s: max_ngram_len must be in 2..%d", who, OT_MAX_NGRAM_LEN);
   if (cfg->draft_side < OT_DRAFT_SIDE_AUTO || cfg->draft_side > OT_DRAFT_SIDE_SEPARATE)
-    return fail(OT_ERR_SHAPE, "ot_verify_init: draft_side must be one of OT_DRAFT_SIDE_*");
-  if ((int64_t)cfg->max_batch * (cfg->max_k + 1) > (1 << 20)) return fail(OT_ERR_SHAPE, "ot_verify_init: more than 2^20 rows");
+    return fail(OT_ERR_SHAPE, "%s: draft_side must be one of OT_DRAFT_SIDE_*", who);
+  if ((int64_t)cfg->max_batch * (cfg->max_k + 1) > (1 << 20)) return fail(OT_ERR_SHAPE, "%s: more than 2^20 rows", who);
 
   // direct map: in range and one-to-one on its mapped part
   std::vector<int32_t> tmap_h;
@@ -91,14 +91,14 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
     tmap_h.reserve((size_t)cfg->V_t + 1 + 2 * (size_t)std::min(cfg->V_d, cfg->V_t));
     tmap_h.assign((size_t)cfg->V_t, -1);
   } catch (const std::bad_alloc&) {
-    return fail(OT_ERR_NOMEM, "ot_verify_init: host allocation failed");
+    return fail(OT_ERR_NOMEM, "%s: host allocation failed", who);
   }
   size_t n_pairs = 0;
   for (int32_t dd = 0; dd < cfg->V_d; ++dd) {
     const int32_t t = cfg->direct_map[dd];
     if (t == -1) continue;
-    if (t < 0 || t >= cfg->V_t) return fail(OT_ERR_MAP, "ot_verify_init: direct_map[%d] = %d is outside [0, V_t)", dd, t);
-    if (tmap_h[t] != -1) return fail(OT_ERR_MAP, "ot_verify_init: draft ids %d and %d both map to target id %d", tmap_h[t], dd, t);
+    if (t < 0 || t >= cfg->V_t) return fail(OT_ERR_MAP, "%s: direct_map[%d] = %d is outside [0, V_t)", who, dd, t);
+    if (tmap_h[t] != -1) return fail(OT_ERR_MAP, "%s: draft ids %d and %d both map to target id %d", who, tmap_h[t], dd, t);
     tmap_h[t] = dd;
     n_pairs += 1;
   }
@@ -108,7 +108,7 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   try {
     tmap_h.resize(pairs_at + 2 * n_pairs);
   } catch (const std::bad_alloc&) {
-    return fail(OT_ERR_NOMEM, "ot_verify_init: host allocation failed");
+    return fail(OT_ERR_NOMEM, "%s: host allocation failed", who);
   }
   size_t n_near = 0;
   for (size_t t = 0, at = pairs_at; t < (size_t)cfg->V_t; ++t) {
@@ -119,7 +119,7 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   }
 
   ot_ctx* c = new (std::nothrow) ot_ctx();
-  if (!c) return fail(OT_ERR_NOMEM, "ot_verify_init: host allocation failed");
+  if (!c) return fail(OT_ERR_NOMEM, "%s: host allocation failed", who);
   c->d = cfg->d; c->V_t = cfg->V_t; c->V_d = cfg->V_d; c->max_batch = cfg->max_batch; c->max_k = cfg->max_k;
   c->dtype = cfg->dtype; c->max_ngram_len = cfg->max_ngram_len; c->draft_side = cfg->draft_side;
   c->stream = static_cast<hipStream_t>(cfg->stream);
@@ -170,7 +170,7 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
   c->lp_part = lp_part;
   const size_t n_counters = 1 + (R + 1) + kLogprobSegments + 2;   // of adaptive drafting, the loss, the log-probabilities, the gradient
   ok = ok && dev_alloc(c, &c->counters, n_counters);
-  if (!ok) { free_ctx(c); return fail(OT_ERR_NOMEM, "ot_verify_init: device allocation failed"); }
+  if (!ok) { free_ctx(c); return fail(OT_ERR_NOMEM, "%s: device allocation failed", who); }
 
   if (c->zeros) e = hipMemsetAsync(c->zeros, 0, 64, c->stream);
   if (e == hipSuccess) e = hipMemsetAsync(c->counters, 0, sizeof(int32_t) * n_counters, c->stream);
@@ -193,14 +193,14 @@ static int init_impl(const ot_verify_config* cfg, const ot_quant_weights* qw, ot
       e = launch_pack_w_f32(static_cast<const float*>(cfg->W), c->d, c->V_t, c->Wf, c->stream);
   }
   if (e == hipSuccess) e = hipStreamSynchronize(c->stream);    // tmap_h and the caller's W are released here
-  if (e != hipSuccess) { free_ctx(c); return fail_hip(e, "ot_verify_init"); }
+  if (e != hipSuccess) { free_ctx(c); return fail_hip(e, who); }
   *out = c;
   return OT_OK;
 }
 
 int ot_verify_init(const ot_verify_config* cfg, ot_ctx** out) {
   if (out) *out = nullptr;
-  return init_impl(cfg, nullptr, out);
+  return init_impl("ot_verify_init", cfg, nullptr, out);
 }
 
 int ot_verify_init_quantized(const ot_verify_config* cfg, const ot_quant_weights* qw, ot_ctx** out) {
@@ -210,7 +210,7 @@ int ot_verify_init_quantized(const ot_verify_config* cfg, const ot_quant_weights
   if (qw->group != 32 && qw->group != 64 && qw->group != 128) return fail(OT_ERR_SHAPE, "ot_verify_init_quantized: group must be 32, 64 or 128 (%d)", qw->group);
   if (qw->scale_dtype != OT_BF16 && qw->scale_dtype != OT_F16) return fail(OT_ERR_DTYPE, "ot_verify_init_quantized: scales are OT_BF16 or OT_F16 (%d)", qw->scale_dtype);
   if (cfg->dtype != OT_BF16) return fail(OT_ERR_DTYPE, "ot_verify_init_quantized: cfg->dtype must be OT_BF16 (%d)", cfg->dtype);
-  return init_impl(cfg, qw, out);
+  return init_impl("ot_verify_init_quantized", cfg, qw, out);
 }
 
 void ot_verify_destroy(ot_ctx* ctx) {

@@ -394,29 +394,30 @@ using namespace otv;
 #pragma GCC visibility push(default)
 extern "C" {
 
-static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
+// who: the entry point, for its errors.
+static int loss_impl(const char* who, ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
                      const ot_loss_config* cfg, ot_loss_out* out, bool with_mass, bool check_only) {
-  if (!ctx || !in || !step || !cfg || !out) return ot_fail(OT_ERR_NULL, "ot_distill_loss: ctx, in, step_out, cfg and out must not be NULL");
+  if (!ctx || !in || !step || !cfg || !out) return ot_fail(OT_ERR_NULL, "%s: ctx, in, step_out, cfg and out must not be NULL", who);
   if (cfg->lambda_mode != OT_LAMBDA_FIXED && cfg->lambda_mode != OT_LAMBDA_TARGET_PROB)
-    return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: unknown lambda_mode %d", cfg->lambda_mode);
+    return ot_fail(OT_ERR_SHAPE, "%s: unknown lambda_mode %d", who, cfg->lambda_mode);
   if (cfg->ngram_term != OT_NGRAM_TERM_NLL && cfg->ngram_term != OT_NGRAM_TERM_APPROX_KL)
-    return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: unknown ngram_term %d", cfg->ngram_term);
-  if (in->B < 0 || in->B > ctx->max_batch) return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: B = %d exceeds max_batch = %d", in->B, ctx->max_batch);
+    return ot_fail(OT_ERR_SHAPE, "%s: unknown ngram_term %d", who, cfg->ngram_term);
+  if (in->B < 0 || in->B > ctx->max_batch) return ot_fail(OT_ERR_SHAPE, "%s: B = %d exceeds max_batch = %d", who, in->B, ctx->max_batch);
   if (!out->kind || !out->kl || !out->nll || !out->weight || !out->totals)
-    return ot_fail(OT_ERR_NULL, "ot_distill_loss: kind, kl, nll, weight and totals are required");
+    return ot_fail(OT_ERR_NULL, "%s: kind, kl, nll, weight and totals are required", who);
   if (in->B > 0) {
     if (!in->row_off || !in->row_off_host || !in->temperature)
-      return ot_fail(OT_ERR_NULL, "ot_distill_loss: row_off, row_off_host and temperature must not be NULL");
+      return ot_fail(OT_ERR_NULL, "%s: row_off, row_off_host and temperature must not be NULL", who);
     if (!step->n_mapped || !step->n_accept || !step->mapped_ids || !step->span_start || !step->span_len || !step->p_tok)
-      return ot_fail(OT_ERR_NULL, "ot_distill_loss: the step's n_mapped, n_accept, mapped_ids, span_start, span_len and p_tok are required");
-    if (in->row_off_host[0] != 0) return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: row_off[0] must be 0");
+      return ot_fail(OT_ERR_NULL, "%s: the step's n_mapped, n_accept, mapped_ids, span_start, span_len and p_tok are required", who);
+    if (in->row_off_host[0] != 0) return ot_fail(OT_ERR_SHAPE, "%s: row_off[0] must be 0", who);
     for (int b = 0; b < in->B; ++b) {
       const int64_t rows = (int64_t)in->row_off_host[b + 1] - in->row_off_host[b];
-      if (rows < 1 || rows - 1 > ctx->max_k) return ot_fail(OT_ERR_SHAPE, "ot_distill_loss: sequence %d owns %lld rows", b, (long long)rows);
+      if (rows < 1 || rows - 1 > ctx->max_k) return ot_fail(OT_ERR_SHAPE, "%s: sequence %d owns %lld rows", who, b, (long long)rows);
     }
   }
   const int M = in->B > 0 ? in->row_off_host[in->B] : 0;
-  if (M - in->B > 0 && (!in->draft_logits || !in->draft_ids)) return ot_fail(OT_ERR_NULL, "ot_distill_loss: draft_logits and draft_ids must not be NULL");
+  if (M - in->B > 0 && (!in->draft_logits || !in->draft_ids)) return ot_fail(OT_ERR_NULL, "%s: draft_logits and draft_ids must not be NULL", who);
 
   if (check_only) return OT_OK;
 
@@ -453,20 +454,21 @@ static int loss_impl(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step,
                                 : (p.threads == 1024 ? loss_kernel<1024, false> : p.threads == 512 ? loss_kernel<512, false> : loss_kernel<256, false>);
   hipLaunchKernelGGL(kernel, grid, block, lds, st, a, ro, seq_rows, n_arrivals, p.groups, p.group_terms, p.staged);
   const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return ot_fail_hip(e, "ot_distill_loss: launch");
+  if (e != hipSuccess) return ot_fail(OT_ERR_HIP, "%s: launch: %s", who, hipGetErrorString(e));
   return OT_OK;
 }
 
 int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
                     const ot_loss_config* cfg, ot_loss_out* out) {
-  return loss_impl(ctx, in, step, target_logits, cfg, out, false, false);
+  return loss_impl("ot_distill_loss", ctx, in, step, target_logits, cfg, out, false, false);
 }
 
 int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step, const float* target_logits,
                          const ot_loss_config* cfg, ot_loss_out* out, const float* grad_loss, void* grad) {
   if (ctx)
     if (const int bad = ot_check_device(ctx, "ot_distill_loss_grad")) return bad;
-  if (const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, true)) return bad;   // the offsets are read below
+  constexpr const char* who = "ot_distill_loss_grad";
+  if (const int bad = loss_impl(who, ctx, in, step, target_logits, cfg, out, true, true)) return bad;   // the offsets are read below
   const int K = in->B > 0 ? in->row_off_host[in->B] - in->B : 0;
   if (K > 0 && !grad) return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
   if (reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
@@ -476,7 +478,7 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
   // where the gradient's launches take rows of this size they do the loss's work as well (without the q' rows)
   const bool in_one = !out->qprime && loss_grad_in_one(K, ctx->V_d, ctx->n_cu);
   if (!in_one)
-    if (const int bad = loss_impl(ctx, in, step, target_logits, cfg, out, true, false)) return bad;
+    if (const int bad = loss_impl(who, ctx, in, step, target_logits, cfg, out, true, false)) return bad;
   if (in->B == 0) return OT_OK;
   LossGradArgs a{};
   a.B = in->B; a.K = K; a.V_t = ctx->V_t; a.V_d = ctx->V_d; a.dtype = ctx->dtype;
