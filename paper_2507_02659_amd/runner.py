@@ -73,12 +73,15 @@ class Verifier:
         self.stream = stream
         self._number = next(self._numbers)          # of this verifier, never used again
         torch.cuda.set_device(self.device)
+        if self.device == torch.device("cuda"):     # as its tensors will say
+            self.device = torch.device("cuda", torch.cuda.current_device())
         common = dict(d=d, V_t=V_t, V_d=V_d, max_batch=max_batch, max_k=max_k, max_ngram_len=max_ngram_len, direct_map=direct_map,
                       dtype=ot.OT_BF16 if dtype == "bf16" else ot.OT_F32, stream=None if stream is None else stream.cuda_stream,
                       draft_side=draft_side)
         self.ctx = None
         if isinstance(W, QuantWeights):
             W.check()
+            self._here(codes=W.codes, scales=W.scales, zeros=W.zeros)
             assert tuple(W.codes.shape) == (d // 2, V_t)
             torch.cuda.synchronize(self.device)
             self.ctx = ot.ot_verify_init_quantized(codes=W.codes, scales=W.scales, zeros=W.zeros, group=W.group,
@@ -211,10 +214,12 @@ class Verifier:
                           grad_loss: Optional[torch.Tensor] = None) -> dict:
         """Enqueues ot_distill_loss_grad after a step on `inp`.  Returns device tensors: "grad", the gradient of grad_loss * loss (a float32
         tensor of one element; None: 1) with respect to the draft logits [K, V_d], and the loss's outputs (the same buffers every call)."""
-        buf = self._loss_buffers(inp, with_qprime)
         if grad_loss is not None and (grad_loss.dtype != torch.float32 or grad_loss.numel() != 1):
             raise ValueError("grad_loss is one float32")
-        grad = self._empty((inp["K"], self.V_d), inp["draft_logits"].dtype)
+        zq = inp["draft_logits"]                    # the gradient is allocated like them
+        self._here(draft_logits=zq, grad_loss=grad_loss)
+        buf = self._loss_buffers(inp, with_qprime)
+        grad = self._empty(zq.shape, zq.dtype)
         sin = ot.make_step_in(B=inp["B"], step=inp["step"], row_off=inp["row_off"], row_off_host=inp["row_off_host"],
                               hidden=inp["hidden"], draft_logits=inp["draft_logits"], draft_ids=inp["draft_ids"],
                               temperature=inp["temperature"], draft_temperature=inp["draft_temperature"],
@@ -238,17 +243,26 @@ class Verifier:
         with self._on_stream():
             return torch.empty(shape, dtype=dtype, device=self.device)
 
+    def _type(self):
+        return torch.bfloat16 if self.dtype == "bf16" else torch.float32
+
+    def _here(self, **tensors):
+        """Refuses tensors that are not on the verifier's device, where their addresses mean nothing."""
+        for name, t in tensors.items():
+            if t is not None and t.device != self.device:
+                raise ValueError(f"{name} is on {t.device}, the verifier on {self.device}")
+
     def lm_head(self, hidden: torch.Tensor) -> torch.Tensor:
         """Logits [M, V_t] (float32) of hidden rows [M, d] through the verifier's head (ot_lm_head)."""
-        if hidden.dtype != (torch.bfloat16 if self.dtype == "bf16" else torch.float32) or hidden.dim() != 2 or hidden.shape[1] != self.d:
+        if hidden.dtype != self._type() or hidden.dim() != 2 or hidden.shape[1] != self.d:
             raise ValueError(f"hidden rows are [M, {self.d}] of the verifier's type, not {tuple(hidden.shape)} {hidden.dtype}")
+        self._here(hidden=hidden)
         M = hidden.shape[0]
         logits = self._empty((M, self.V_t), torch.float32)
         ot.ot_lm_head(self.ctx, M, hidden, logits, self.V_t)
         return logits
 
-    @staticmethod
-    def _logprob_in(logits, tokens, temperature, row_off, n_top, given_rows_only):
+    def _logprob_in(self, logits, tokens, temperature, row_off, n_top, given_rows_only):
         M, V = logits.shape
         if logits.dtype not in (torch.bfloat16, torch.float32) or (V > 1 and logits.stride(1) != 1):
             raise ValueError("logits are [M, V] bfloat16 or float32 with neighbouring ids next to each other")
@@ -262,6 +276,7 @@ class Verifier:
             raise ValueError(f"temperatures are {B} float32")
         if row_off is not None and row_off.dtype != torch.int32:
             raise ValueError("row_off is int32")
+        self._here(logits=logits, tokens=tokens, temperature=temperature, row_off=row_off)
         # rows may lie further apart than V, and overlap nothing: one row alone may have any stride
         return ot.make_logprob_in(M=M, V=V, dtype=ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, logits=logits.data_ptr(),
                                   ld=logits.stride(0) if M > 1 else V, tokens=tokens, n_tok=n_tok, n_top=n_top, temperature=temperature,
@@ -300,6 +315,9 @@ class Verifier:
         for name, g, shape in (("grad_logprob", grad_logprob, None if tokens is None else tokens.shape), ("grad_entropy", grad_entropy, logits.shape[:1])):
             if g is not None and (g.dtype != torch.float32 or g.shape != shape):
                 raise ValueError(f"{name} is float32 {shape}")
+        for name in ("row_max", "row_sumexp") if grad_entropy is None else ("row_max", "row_sumexp", "entropy"):
+            self._here(**{name: forward.get(name)})
+        self._here(grad_logprob=grad_logprob, grad_entropy=grad_entropy)
         grad = self._empty(logits.shape, logits.dtype)
         ot.ot_token_logprobs_grad(self.ctx, given, ot.make_logprob_out(forward), grad_logprob, grad_entropy, grad, logits.shape[1])
         return grad
