@@ -316,7 +316,10 @@ class Verifier:
             if g is not None and (g.dtype != torch.float32 or g.shape != shape):
                 raise ValueError(f"{name} is float32 {shape}")
         for name in ("row_max", "row_sumexp") if grad_entropy is None else ("row_max", "row_sumexp", "entropy"):
-            self._here(**{name: forward.get(name)})
+            t = forward.get(name)
+            if t is None or t.dtype != torch.float32 or t.shape != logits.shape[:1]:
+                raise ValueError(f"forward holds {name}, float32 [{logits.shape[0]}]")
+            self._here(**{name: t})
         self._here(grad_logprob=grad_logprob, grad_entropy=grad_entropy)
         grad = self._empty(logits.shape, logits.dtype)
         ot.ot_token_logprobs_grad(self.ctx, given, ot.make_logprob_out(forward), grad_logprob, grad_entropy, grad, logits.shape[1])

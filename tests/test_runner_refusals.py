@@ -66,6 +66,14 @@ def test_statistics_of_another_call(v):
     grads = dict(grad_logprob=torch.zeros(4), grad_entropy=torch.zeros(4))
     with pytest.raises(Reached):
         v.token_logprobs_grad(**given, forward=forward, **grads)
+    for name in forward:
+        for bad in (torch.zeros(3), torch.zeros(4, 1), torch.zeros(4, dtype=torch.float64), None):
+            with pytest.raises(ValueError, match=name):
+                v.token_logprobs_grad(**given, forward=dict(forward, **{name: bad}), **grads)
+        with pytest.raises(ValueError, match=name):
+            v.token_logprobs_grad(**given, forward={n: t for n, t in forward.items() if n != name}, **grads)
+    with pytest.raises(Reached):                          # without a gradient of the entropy it is not read
+        v.token_logprobs_grad(**given, forward=dict(forward, entropy=None), grad_logprob=grads["grad_logprob"])
     for name in ("row_max", "row_sumexp", "entropy", "grad_logprob", "grad_entropy"):
         away = torch.zeros(4, device="meta")
         with pytest.raises(ValueError, match=name + " is on meta"):
