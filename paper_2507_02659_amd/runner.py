@@ -217,6 +217,8 @@ class Verifier:
         if grad_loss is not None and (grad_loss.dtype != torch.float32 or grad_loss.numel() != 1):
             raise ValueError("grad_loss is one float32")
         zq = inp["draft_logits"]                    # the gradient is allocated like them
+        if zq.dtype != self._type() or zq.shape != (inp["K"], self.V_d):
+            raise ValueError(f"draft logits are [{inp['K']}, {self.V_d}] of the verifier's type, not {tuple(zq.shape)} {zq.dtype}")
         self._here(draft_logits=zq, grad_loss=grad_loss)
         buf = self._loss_buffers(inp, with_qprime)
         grad = self._empty(zq.shape, zq.dtype)

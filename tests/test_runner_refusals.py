@@ -86,8 +86,10 @@ def test_draft_logits_of_another_type(v):
     inp = dict(none, B=1, M=3, K=2, step=0, seed=0, out=out, draft_logits=torch.zeros(2, 30, dtype=torch.bfloat16))
     with pytest.raises(Reached):
         v.distill_loss_grad(inp)
-    with pytest.raises(ValueError, match="draft_logits is on meta"):
-        v.distill_loss_grad(dict(inp, draft_logits=torch.zeros(2, 30, dtype=torch.bfloat16, device="meta")))
+    for bad in (torch.zeros(2, 30), torch.zeros(2, 29, dtype=torch.bfloat16), torch.zeros(1, 30, dtype=torch.bfloat16),
+                torch.zeros(2, 30, dtype=torch.bfloat16, device="meta")):
+        with pytest.raises(ValueError, match="draft"):
+            v.distill_loss_grad(dict(inp, draft_logits=bad))
     with pytest.raises(ValueError, match="grad_loss is on meta"):
         v.distill_loss_grad(inp, grad_loss=torch.ones(1, device="meta"))
 
