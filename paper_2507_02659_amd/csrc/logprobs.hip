@@ -453,6 +453,20 @@ __global__ __launch_bounds__(256) void logprob_grad_kernel(LogprobGradArgs a, in
   // thread's vector i holds ids v0 + 256 i kVec ..; of the row's first one the ids below 0, of its last one those past the end are nobody's
   const int c0 = (int)(blockIdx.x % (unsigned)chunks) * kChunk - shift, v0 = c0 + tid * kVec;
   auto whole = [&](int i) { const int at = v0 + i * 256 * kVec; return vectors && at >= 0 && at + kVec <= in.V; };
+  if (in.given_rows_only && a.row_sumexp[row] == 0.f) {  // a row that is not read (or one without a distribution)
+    const float zero[kVec] = {};
+#pragma unroll
+    for (int i = 0; i < kLoads; ++i) {
+      if (whole(i)) {
+        store_vec(grad + v0 + i * 256 * kVec, zero);
+      } else {
+#pragma unroll
+        for (int e = 0; e < kVec; ++e)
+          if (const int at = v0 + i * 256 * kVec + e; at >= 0 && at < in.V) store_one(grad + at, 0.f);
+      }
+    }
+    return;
+  }
   typename Vec<T>::Raw raw[kLoads];
 #pragma unroll
   for (int i = 0; i < kLoads; ++i)

@@ -1,0 +1,40 @@
+"""Rows of logits that a call of the log-probabilities does not read, and rows whose largest logits are shared by as many lanes as a list of
+alternatives holds, or one more."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import logprobs as ol
+from test_gpu_logprobs import DEV, v  # noqa: F401
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("V", [5, 1003, 40003])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
+def test_rows_that_are_not_given_may_hold_anything(v, V, dtype):  # noqa: F811
+    """With given_rows_only the rows without a token are unwritten memory of the caller's: here NaN and infinities.  Their gradients are zeros, those
+    of the others are what they are without the option; also over the logits themselves, and with tokens of which one in a row is -1."""
+    rng = np.random.default_rng(V)
+    M = 9
+    z = torch.from_numpy(rng.standard_normal((M, V)).astype(np.float32)).to(dtype).to(DEV)
+    tokens = rng.integers(0, V, (M, 2)).astype(np.int32)
+    tokens[[1, 2, 5, 8]] = -1
+    tokens[3, 0] = -1
+    absent = [1, 2, 5, 8]
+    for i, bad in zip(absent, (float("nan"), float("inf"), -float("inf"), 3.0)):
+        z[i] = bad
+    tok = torch.from_numpy(tokens).to(DEV)
+    g, gH = torch.randn(M, 2, device=DEV), torch.randn(M, device=DEV)
+    keep = [m for m in range(M) if m not in absent]
+    print(f"given rows V={V} {dtype}", flush=True)
+    full = z.clone()                                      # the same batch (rows start at the same places) with nothing unwritten
+    full[absent] = 1.0
+    want = v.token_logprobs_grad(full, tok, v.token_logprobs(full, tok), grad_logprob=g, grad_entropy=gH)
+    fwd = v.token_logprobs(z, tok, given_rows_only=True)
+    got = v.token_logprobs_grad(z, tok, fwd, grad_logprob=g, grad_entropy=gH, given_rows_only=True)
+    assert not got[absent].any() and torch.equal(got[keep], want[keep])
+    from paper_2507_02659_amd import binding as ot
+    given = v._logprob_in(z, tok, None, None, 0, True)
+    ot.ot_token_logprobs_grad(v.ctx, given, ot.make_logprob_out(fwd), g, gH, z, V)
+    assert torch.equal(z, got)
