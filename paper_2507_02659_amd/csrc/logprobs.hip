@@ -313,7 +313,10 @@ __global__ __launch_bounds__(64 * kWaves) void logprob_kernel(LogprobArgs a, int
     const key_t worst = lane_key(holder, 63);
     __syncthreads();
     list = 0;
-    if (worst != 0 && key_logit(worst) >= bar) {         // more lanes than the list holds reach the bar (equal logits): all of them
+    // more lanes than the list holds reach the bar (equal logits): all of them.  (Of 64 alternatives the last holder is the bar.)
+    bool all_lanes = worst != 0 && key_logit(worst) >= bar;
+    if (all_lanes) all_lanes = __syncthreads_count(lane_max >= bar) > 64;
+    if (all_lanes) {
       for (int t = tile0 + wave; t < end; t += kWaves) {
         float v[kPer];
         load(t, lane);

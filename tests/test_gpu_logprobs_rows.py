@@ -38,3 +38,20 @@ def test_rows_that_are_not_given_may_hold_anything(v, V, dtype):  # noqa: F811
     given = v._logprob_in(z, tok, None, None, 0, True)
     ot.ot_token_logprobs_grad(v.ctx, given, ot.make_logprob_out(fwd), g, gH, z, V)
     assert torch.equal(z, got)
+
+
+@pytest.mark.parametrize("n_top", [1, 63, 64])
+@pytest.mark.parametrize("n_best", [62, 63, 64, 65, 256])
+def test_best_logits_in_as_many_lanes(v, n_best, n_top):  # noqa: F811
+    """n_best lanes of a workgroup hold one largest logit each, equal ones or not; the lanes next to them hold second best ones."""
+    z = torch.full((3, 256 * 16), -1.0, device=DEV)
+    lanes = torch.arange(n_best, device=DEV) * 4              # the first vector of lane i
+    z[:, lanes] = 5.0
+    z[1, lanes] += torch.randperm(n_best, device=DEV) * 0.01
+    z[2, lanes + 1] = torch.linspace(1, 4, n_best, device=DEV)
+    got = v.token_logprobs(z, n_top=n_top)
+    want = ol.token_logprobs(z.double().cpu().numpy(), None, np.ones(3), n_top)
+    print(f"lanes {n_best} alternatives {n_top}", flush=True)
+    np.testing.assert_array_equal(got["top_ids"].cpu().numpy(), want["top_ids"])
+    # exponents up to 6 * log2(e): three roundings of 2^-24 |t| and six half-steps on each exponential, as many on ln S; and the result's
+    np.testing.assert_allclose(got["top_logprobs"].cpu().numpy(), want["top_logprobs"], rtol=2.0 ** -24, atol=(3 * 10 + 6) * 2.0 ** -24)
