@@ -278,7 +278,9 @@ class Verifier:
             raise ValueError(f"temperatures are {B} float32")
         if row_off is not None and row_off.dtype != torch.int32:
             raise ValueError("row_off is int32")
-        self._here(logits=logits, tokens=tokens, temperature=temperature, row_off=row_off)
+        dev = self.device                           # (a call of one row is bound by the host)
+        if logits.device != dev or (tokens is not None and tokens.device != dev) or (temperature is not None and temperature.device != dev) or row_off is not None:
+            self._here(logits=logits, tokens=tokens, temperature=temperature, row_off=row_off)
         # rows may lie further apart than V, and overlap nothing: one row alone may have any stride
         return ot.make_logprob_in(M=M, V=V, dtype=ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, logits=logits.data_ptr(),
                                   ld=logits.stride(0) if M > 1 else V, tokens=tokens, n_tok=n_tok, n_top=n_top, temperature=temperature,
