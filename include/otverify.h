@@ -114,9 +114,11 @@ void ot_verify_destroy(ot_ctx* ctx);          /* synchronises the stream, frees 
 
 /* ---- a target head of 4-bit weights --------------------------------------------------------------------- */
 /* W[k][v] = scale[k / group][v] * (code[k][v] - zero[k / group][v]) with codes of 0..15: a quarter of the OT_BF16 weights'
- * bytes, and up to 176 rows the weight stream is what bounds a step.  Codes times hidden states are exact, their sums over a
- * group and the sums of scaled groups are fp32; the hidden states are not rounded, so the logits are those of the weights above
- * to fp32 rounding.  Scales are finite.  A hidden row with an infinity or a NaN has NaN logits; hidden states are taken to stay below 2^100.   */
+ * bytes, and up to 176 rows the weight stream is what bounds a step.  The hidden states are not rounded, products with
+ * codes less 7.5 are exact, and what is summed in fp32 is h (code - 7.5), of which (zero - 7.5) times the sum of h is taken off, per group, then the
+ * scaled groups: a logit is that of the weights above but for the roundings, 2^-24 each, of these sums' partial ones.  (A column whose codes
+ * equal its zero point leaves what that rounds off and not exactly 0.)  Scales are finite.  A hidden row with an infinity or a NaN has NaN
+ * logits, and so is a logit that float32 does not hold; hidden states are taken to stay below 2^100.                                          */
 typedef struct ot_quant_weights {
   int32_t        group;        /* 32, 64 or 128: so many consecutive hidden indices share a scale and a zero point; d may end
                                   inside a group                                                              */

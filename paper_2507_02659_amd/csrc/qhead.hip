@@ -1,11 +1,12 @@
 // A target head of 4-bit weights with group scales: z[m][v] = sum over groups g of s[g][v] * sum_{k in g} h[m][k] (c[k][v] - zp[g][v]).
 //
-// The codes c (0..15) become bf16 operands of v_mfma_f32_16x16x32_bf16 in two instructions per pair and none of them a
-// conversion: the bits 0x4180 | c << 3 are the bf16 number 16 + c, exactly.  So a group's product comes out as
-// sum h (16 + c), and the sum of the group's hidden states, the same for every column, takes (16 + zp) times itself off it;
-// then the group's scale multiplies 16 rows x 16 columns in four instructions.  Products of a bf16 number and 16 + c are exact in
-// fp32, so what is rounded is the sums alone; they are at most 31 / |c - zp| times as large as with the centred codes, which
-// costs less than the fp32 rounding of a group's scaled sum in the total over the groups.
+// The codes c (0..15) become bf16 operands c - 7.5 of v_mfma_f32_16x16x32_bf16: with c's range in the middle of the format's, so that what
+// a group's product sums is of the size of the weights.  (With 16 + c, one instruction less per word, the sums were 24 times the hidden states
+// and their rounding 2 to 5 times as large in the logits, without end where c = zp.)  A group's product is sum h (c - 7.5), and the sum of the
+// group's hidden states, the same for every column, takes (zp - 7.5) times itself off it; then the group's scale multiplies 16 rows x 16 columns
+// in four instructions.  Products of a bf16 number and c - 7.5 are exact in fp32, so what is rounded is the sums alone, 2^-24 of each: a group's
+// at most once per hidden index, partial sums of h (c - 7.5) and of h (these times zp - 7.5), and the running total of scaled groups once per
+// group, above 16 rows with the offsets of up to four groups in it.  The roundings add up as a random walk.
 //
 // What bounds it, groups of 128, weights from memory: up to 16 rows the weight stream (6 rows x 3584 x 152064 53-56 us, 5.3 TB/s, what a
 // large copy moves; a bf16 head 163); above, the trips through LDS and registers between the products: 144 x 4096 x 128256 167-175 us, 0.9
@@ -28,27 +29,37 @@ __device__ inline f32x4 mfma(u32x4 a, u32x4 b, f32x4 c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
 }
 
-// Eight codes of one packed word as bf16 numbers 16 + c, in ascending hidden index.  The word is the one whose nibble j holds code 2 j
-// and whose nibble j + 4 code 2 j + 1 (j < 4), rotated left by 3: a pair's mantissa bits are then a shift and a mask away.
-// Mask and 16 come in registers (Bits): the instruction that does both, v_and_or_b32, takes no literals.  The compiler has to choose that
-// instruction itself: one written as inline asm is outside its bookkeeping of the waits between vector and matrix instructions, and
+// Eight codes of one packed word as bf16 numbers c - 7.5, in ascending hidden index.  With c - 7.5 = +-(2 m + 1)/2 the fp8 number (e4m3) of sign,
+// exponent 0 or 1 and low bits 2 m + 1 is +-(2 m + 1) 2^-9: below 16 of these steps fp8 is a fixed-point format.  Codes 0 .. 3 have sign and m in
+// bits 7 and 3 .. 1 of the word's four bytes, and so have codes 4 .. 7 in the word read backwards; a mask and the low one away from that are
+// four fp8 numbers, of which a conversion with a factor of 2^8 makes two bf16 numbers at a time.
+// Mask, ones and factor come in registers (Bits): the instructions that use them take no literals.  The compiler has to choose these
+// instructions itself: one written as inline asm is outside its bookkeeping of the waits between vector and matrix instructions, and
 // a matrix product still in flight overwrote such results.
 struct Bits {
-  uint32_t mask, sixteen;
+  uint32_t mask, ones;
+  float factor;
 };
 __device__ inline Bits code_bits() {                     // the empty statements keep the compiler from folding the constants back in
-  Bits k{0x00780078u, 0x41804180u};
+  Bits k{0x8E8E8E8Eu, 0x01010101u, 256.f};
   asm("" : "+s"(k.mask));
-  asm("" : "+v"(k.sixteen));
+  asm("" : "+v"(k.ones));
+  asm("" : "+s"(k.factor));
   return k;
 }
-__device__ inline u32x4 codes_to_bf16(uint32_t w, Bits k) {
-  return u32x4{(w & k.mask) | k.sixteen, (w >> 4 & k.mask) | k.sixteen, (w >> 8 & k.mask) | k.sixteen,
-               (__builtin_amdgcn_alignbit(w, w, 12) & k.mask) | k.sixteen};
+template <bool kHigh>
+__device__ inline uint32_t fp8_to_bf16(uint32_t w, Bits k) {
+  return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(w, k.factor, kHigh));
 }
-// A group's scale and 16 + zero point of one column: the scale's fp32 bits, of which a bf16 or fp16 scale leaves the low 13 free.
+__device__ inline u32x4 codes_to_bf16(uint32_t w, Bits k) {
+  const uint32_t a = (w & k.mask) | k.ones, b = (__builtin_bitreverse32(w) & k.mask) | k.ones;
+  return u32x4{fp8_to_bf16<false>(a, k), fp8_to_bf16<true>(a, k), fp8_to_bf16<false>(b, k), fp8_to_bf16<true>(b, k)};
+}
+// A group's scale and zero point less 7.5 of one column: the scale's fp32 bits, of which a bf16 or fp16 scale leaves the low 13 free.
 __device__ inline float rec_scale(uint32_t r) { return __uint_as_float(r & 0xFFFFE000u); }
-__device__ inline float rec_zero(uint32_t r) { return (float)(r & 0xFFu); }
+__device__ inline float rec_zero(uint32_t r) { return (float)(r & 0xFFu) - 7.5f; }
+// What a hidden state that is infinite or NaN has left of a row's logits: no code makes 0 of it, so they are infinite or NaN, and become NaN.
+__device__ inline float nan_if_infinite(float z) { return fmaf(z, 0.f, z); }
 
 // One thread per lane's uint4 of codes: tile of 16 columns, block of 128 hidden indices, lane = 16 * (k / 8 % 4) + column.
 __global__ void pack_codes_kernel(const uint8_t* __restrict__ codes, int d, int V_t, int blocks, int64_t n, u32x4* __restrict__ packed) {
@@ -61,12 +72,13 @@ __global__ void pack_codes_kernel(const uint8_t* __restrict__ codes, int d, int 
   for (int ks = 0; ks < 4; ++ks) {
     uint32_t x = 0;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      const int k = b * 128 + ks * 32 + (lane >> 4) * 8 + 2 * j;         // even, as is d
-      const uint32_t both = k < d && v < V_t ? codes[(int64_t)(k >> 1) * V_t + v] : 0u;
-      x |= (both & 15u) << (4 * j) | (both >> 4) << (4 * j + 16);
+    for (int j = 0; j < 8; ++j) {
+      const int k = b * 128 + ks * 32 + (lane >> 4) * 8 + j;
+      const uint32_t c = k < d && v < V_t ? codes[(int64_t)(k >> 1) * V_t + v] >> (4 * (k & 1)) & 15u : 8u;
+      const uint32_t m = c & 8u ? c & 7u : ~c & 7u, bits = (c < 8u ? 0x80u : 0u) | m << 1;
+      x |= j < 4 ? bits << (8 * j) : __builtin_bitreverse32(bits << (8 * (j - 4)));
     }
-    w[ks] = x << 3 | x >> 29;
+    w[ks] = x;
   }
   packed[i] = w;
 }
@@ -79,11 +91,11 @@ __global__ void pack_scales_kernel(const void* __restrict__ scales, int f16, con
   const int64_t cell = i / per_block, tb = cell >> 4;
   const int g = (int)(tb % blocks) * per_block + (int)(i % per_block);
   const int64_t v = tb / blocks * 16 + (cell & 15);
-  uint32_t r = 16;
+  uint32_t r = 0;
   if (g < groups && v < V_t) {
     const int64_t at = (int64_t)g * V_t + v;
     const float s = f16 ? (float)static_cast<const _Float16*>(scales)[at] : bf16_to_f32(static_cast<const uint16_t*>(scales)[at]);
-    r = (__float_as_uint(s) & 0xFFFFE000u) | (16u + (zeros ? zeros[at] & 15u : 8u));
+    r = (__float_as_uint(s) & 0xFFFFE000u) | (zeros ? zeros[at] & 15u : 8u);
   }
   recs[i] = r;
 }
@@ -210,7 +222,7 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
       const int row = 4 * (lane >> 4) + e;
-      if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = total[s][e];
+      if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = nan_if_infinite(total[s][e]);
     }
   }
 }
@@ -363,7 +375,7 @@ __global__ __launch_bounds__(64 * kTallWaves) void qhead_tall_kernel(const uint1
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const int row = row0 + rt * 16 + 4 * (lane >> 4) + e;
-        if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = total[rt][s][e];
+        if (row < M && v < V_t) Z[(int64_t)row * ldz + v] = nan_if_infinite(total[rt][s][e]);
       }
     }
 }
