@@ -59,7 +59,7 @@ class QuantWeights:
 class Verifier:
     """One library context plus (optionally) one n-gram cache, for batches of a fixed model shape.
 
-    Work is enqueued on `stream` (None: the default stream).  Inputs have to be ready on it, and outputs are ready on it."""
+    Work is enqueued on `stream` (None: the default stream).  Inputs have to be ready on it; outputs are allocated and ready on it."""
 
     _numbers = itertools.count()
 
@@ -249,10 +249,14 @@ class Verifier:
         return torch.bfloat16 if self.dtype == "bf16" else torch.float32
 
     def _here(self, **tensors):
-        """Refuses tensors that are not on the verifier's device, where their addresses mean nothing."""
+        """Refuses tensors that are not on the verifier's device, where their addresses mean nothing.  Of the others the allocator learns that
+        the verifier's stream uses them: the caller may drop them before the work there is done."""
         for name, t in tensors.items():
-            if t is not None and t.device != self.device:
-                raise ValueError(f"{name} is on {t.device}, the verifier on {self.device}")
+            if t is not None:
+                if t.device != self.device:
+                    raise ValueError(f"{name} is on {t.device}, the verifier on {self.device}")
+                if self.stream is not None:
+                    t.record_stream(self.stream)
 
     def lm_head(self, hidden: torch.Tensor) -> torch.Tensor:
         """Logits [M, V_t] (float32) of hidden rows [M, d] through the verifier's head (ot_lm_head)."""
@@ -279,7 +283,7 @@ class Verifier:
         if row_off is not None and row_off.dtype != torch.int32:
             raise ValueError("row_off is int32")
         dev = self.device                           # (a call of one row is bound by the host)
-        if logits.device != dev or (tokens is not None and tokens.device != dev) or (temperature is not None and temperature.device != dev) or row_off is not None:
+        if self.stream is not None or logits.device != dev or (tokens is not None and tokens.device != dev) or (temperature is not None and temperature.device != dev) or row_off is not None:
             self._here(logits=logits, tokens=tokens, temperature=temperature, row_off=row_off)
         # rows may lie further apart than V, and overlap nothing: one row alone may have any stride
         return ot.make_logprob_in(M=M, V=V, dtype=ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, logits=logits.data_ptr(),
