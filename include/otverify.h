@@ -275,7 +275,7 @@ int ot_distill_loss(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* step_o
                     const ot_loss_config* cfg, ot_loss_out* out);
 
 /* The values of ot_distill_loss (same arguments, same outputs, equal to fp32 rounding of the terms), and the gradient of grad_loss * totals[4] with respect to the
- * drafter's logits: grad, DEVICE [K, V_d] in cfg.dtype, not the logits themselves, written whole (zeros in the rows of draft tokens without a term).
+ * drafter's logits: grad, DEVICE [K, V_d] in cfg.dtype, nowhere in the logits themselves, written whole (zeros in the rows of draft tokens without a term).
  * grad_loss: DEVICE, one float, or NULL for 1.  p, the weights lambda and the translation are constants; q' depends on the draft
  * logits as Eq. 1 and Eq. 2 say, so with OT_NGRAM_TERM_APPROX_KL the logits of all of an n-gram's sub-tokens get a gradient.
  * An id that the drafter's logits mask (-inf) gets zero, and so does a row that they mask whole, which adds nothing.  A draft row

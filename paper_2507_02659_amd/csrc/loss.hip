@@ -473,8 +473,10 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
   if (K > 0 && !grad) return ot_fail(OT_ERR_NULL, "ot_distill_loss_grad: grad must not be NULL");
   if (reinterpret_cast<uintptr_t>(grad) % (ctx->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad is not aligned to its type");
-  if (K > 0 && grad == in->draft_logits)
-    return ot_fail(OT_ERR_SHAPE, "ot_distill_loss_grad: grad must not be the drafter's logits, which other rows' gradients read");
+  // other rows' gradients read the logits: the gradient has to be elsewhere altogether
+  const uintptr_t bytes = (uintptr_t)K * ctx->V_d * (ctx->dtype == OT_BF16 ? 2 : 4), to = reinterpret_cast<uintptr_t>(grad),
+                  from = reinterpret_cast<uintptr_t>(in->draft_logits);
+  if (K > 0 && to < from + bytes && from < to + bytes) return ot_fail(OT_ERR_SHAPE, "%s: grad overlaps the drafter's logits", who);
   // where the gradient's launches take rows of this size they do the loss's work as well (without the q' rows)
   const bool in_one = !out->qprime && loss_grad_in_one(K, ctx->V_d, ctx->n_cu);
   if (!in_one)

@@ -106,3 +106,37 @@ def test_rows_without_a_distribution(dtype, tiny, approx_kl):
         assert np.isfinite(grad[others]).all() and (tiny or grad[others].any())
         np.testing.assert_allclose(kl[rows], loss["kl"][rows], rtol=2e-6, atol=1e-6)
     np.testing.assert_array_equal(np.isnan(one["grad"]), np.isnan(gather["grad"]))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_a_gradient_over_the_logits_is_refused(dtype):
+    """At the logits, and anywhere that shares a byte with them: one id before or behind, a row further, the last id; next to them it is taken."""
+    import torch
+
+    from paper_2507_02659_amd import binding as ot
+    from paper_2507_02659_amd.runner import Verifier
+    case = make_case(_spec("overlap", [3, 2], 3, dtype=dtype))
+    v = Verifier.for_case(case)
+    inp = v.upload(case)
+    K, V_d, size = case.K, case.V_d, 2 if dtype == "bf16" else 4
+    memory = torch.zeros(3 * K, V_d, dtype=inp["draft_logits"].dtype, device="cuda:0")
+    memory[K:2 * K] = inp["draft_logits"]
+    inp["draft_logits"] = memory[K:2 * K]
+    v.step(inp, from_logits=True)
+    want = v.distill_loss_grad(inp, from_logits=True)["grad"]
+    names = ("B", "step", "row_off", "row_off_host", "hidden", "draft_logits", "draft_ids", "temperature", "draft_temperature", "seq_id", "seed")
+    sin, sout = ot.make_step_in(**{n: inp[n] for n in names}), ot.make_step_out(inp["out"])
+
+    def call(at):
+        ot.ot_distill_loss_grad(v.ctx, sin, sout, inp["target_logits"], lam=0.2, lambda_mode=0, ngram_term=0, accepted_only=False,
+                                buffers=v._loss_buffers(inp, False), grad_loss=None, grad=memory.data_ptr() + size * at)
+
+    for at in (K * V_d, K * V_d + 1, K * V_d - 1, (K + 1) * V_d, 2 * K * V_d - 1, 1):
+        with pytest.raises(ot.OtError) as e:
+            call(at)
+        assert e.value.code == ot.OT_ERR_SHAPE and "overlaps" in e.value.message
+    for first in (0, 2 * K):
+        call(first * V_d)
+        v.synchronize()
+        assert torch.equal(memory[first:first + K], want)
+    v.close()
