@@ -324,7 +324,8 @@ int ot_token_logprobs(ot_ctx* ctx, const ot_logprob_in* in, ot_logprob_out* out)
  * and 0 for ids masked with -inf.
  * `in` and `forward` are those of ot_token_logprobs, whose row_max, row_sumexp and (with grad_entropy) entropy are read.
  * grad_logprob DEVICE [M, n_tok], grad_entropy DEVICE [M]: either may be NULL (zero).  grad: DEVICE, row m at grad + m * ld_grad
- * elements, ld_grad >= V, written whole up to V; it may be the logits themselves (with the same ld).               */
+ * elements, ld_grad >= V, written whole up to V; it may be the logits themselves (with the same ld), or
+ * share no byte with their rows.                                                                                 */
 int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logprob_out* forward, const float* grad_logprob_or_null,
                            const float* grad_entropy_or_null, void* grad, int64_t ld_grad);
 

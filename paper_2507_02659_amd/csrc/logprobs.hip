@@ -567,6 +567,16 @@ int check_in(const ot_ctx* ctx, const ot_logprob_in* in, const char* who) {
   return ot_check_device(ctx, who);
 }
 
+// Whether rows of the gradient share memory with rows of the logits and are not those rows themselves.
+bool overlaps(const ot_logprob_in& in, const void* grad, int64_t ld_grad) {
+  const int64_t size = in.dtype == OT_BF16 ? 2 : 4, row = in.V * size, step = in.ld * size;
+  const uintptr_t from = reinterpret_cast<uintptr_t>(in.logits), to = reinterpret_cast<uintptr_t>(grad);
+  if (to == from || to >= from + (uintptr_t)((in.M - 1) * step + row) || from >= to + (uintptr_t)((in.M - 1) * ld_grad * size + row)) return false;
+  if (ld_grad != in.ld) return true;
+  const int64_t apart = (int64_t)(to > from ? (to - from) % (uintptr_t)step : step - (int64_t)((from - to) % (uintptr_t)step));
+  return apart < row || apart > step - row;              // (a row's end, and the next row's start)
+}
+
 }  // namespace
 
 size_t logprob_segment_bytes() { return sizeof(Segment); }
@@ -602,6 +612,7 @@ int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logpro
   if (reinterpret_cast<uintptr_t>(grad) % (in->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: grad is not aligned to its type");
   if (grad == in->logits && ld_grad != in->ld) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: in place, ld_grad must be ld");
+  if (overlaps(*in, grad, ld_grad)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: rows of grad overlap other places of the logits' rows");
   const int chunks = ceil_div((int64_t)in->V + 7, in->dtype == OT_BF16 ? kGradChunk<uint16_t> : kGradChunk<float>);   // a row starts up to 7 elements into its first vector
   if (!grid_fits((int64_t)chunks * in->M, 256)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: %d rows of %d ids are too many for a launch", in->M, in->V);
   const LogprobGradArgs a{*in, fwd->row_max, fwd->row_sumexp, fwd->entropy, grad_logprob, grad_entropy, grad, ld_grad};
