@@ -194,19 +194,19 @@ class Verifier:
         return res
 
     def _loss_buffers(self, inp: dict, with_qprime: bool) -> dict:
-        dev = self.device
         M = max(inp["M"], 1)
-        key = ("loss_buffers", M, with_qprime)
-        buf = inp.get(key + (self._number,))        # a batch may go through several verifiers, each on its stream and with its V_t
+        own = ("loss_buffers", M, with_qprime, self._number)   # a batch may go through several verifiers, each on its stream and with its V_t
+        buf = inp.get(own)
         if buf is None:
+            dev = self.device
             with self._on_stream():                 # the loss writes them there: filled anywhere else, they could be filled after it
                 buf = {"kind": torch.full((M,), -7, dtype=torch.int32, device=dev),
                        "totals": torch.full((5,), -7.0, dtype=torch.float64, device=dev)}
                 buf.update({n: torch.full((M,), -7.0, dtype=torch.float64, device=dev) for n in ("kl", "nll", "weight")})
                 if with_qprime:
                     buf["qprime"] = torch.full((M, self.V_t), -7.0, dtype=torch.float32, device=dev)
-            inp[key + (self._number,)] = buf
-        inp[key] = buf                              # the last call's
+            inp[own] = buf
+        inp["loss_buffers", M, with_qprime] = buf   # the last call's
         return buf
 
     def distill_loss_grad(self, inp: dict, *, from_logits: bool = False, lam: float = 0.2, lambda_mode: int = ot.OT_LAMBDA_FIXED,
@@ -217,17 +217,19 @@ class Verifier:
         if grad_loss is not None and (grad_loss.dtype != torch.float32 or grad_loss.numel() != 1):
             raise ValueError("grad_loss is one float32")
         zq = inp["draft_logits"]                    # the gradient is allocated like them
-        if zq.dtype != self._type() or zq.shape != (inp["K"], self.V_d):
+        if zq.dtype != self._type() or zq.dim() != 2 or zq.size(0) != inp["K"] or zq.size(1) != self.V_d:
             raise ValueError(f"draft logits are [{inp['K']}, {self.V_d}] of the verifier's type, not {tuple(zq.shape)} {zq.dtype}")
-        self._here(draft_logits=zq, grad_loss=grad_loss)
+        if self.stream is not None or zq.device != self.device or (grad_loss is not None and grad_loss.device != self.device):
+            self._here(draft_logits=zq, grad_loss=grad_loss)
         buf = self._loss_buffers(inp, with_qprime)
         grad = self._empty(zq.shape, zq.dtype)
         sin = ot.make_step_in(B=inp["B"], step=inp["step"], row_off=inp["row_off"], row_off_host=inp["row_off_host"],
                               hidden=inp["hidden"], draft_logits=inp["draft_logits"], draft_ids=inp["draft_ids"],
                               temperature=inp["temperature"], draft_temperature=inp["draft_temperature"],
                               seq_id=inp["seq_id"], seed=inp["seed"])
-        out = inp["out"]                            # of the step's outputs, what the loss reads
-        sout = ot.make_step_out({n: out[n] for n in ("n_mapped", "n_accept", "mapped_ids", "span_start", "span_len", "p_tok")})
+        out, at = inp["out"], ot._ptr               # of the step's outputs, what the loss reads
+        sout = ot.ot_step_out(n_mapped=at(out["n_mapped"]), n_accept=at(out["n_accept"]), mapped_ids=at(out["mapped_ids"]),
+                              span_start=at(out["span_start"]), span_len=at(out["span_len"]), p_tok=at(out["p_tok"]))
         ot.ot_distill_loss_grad(self.ctx, sin, sout, inp["target_logits"] if from_logits else None, lam=lam,
                                 lambda_mode=lambda_mode, ngram_term=ngram_term, accepted_only=accepted_only, buffers=buf,
                                 grad_loss=grad_loss, grad=grad)
@@ -262,7 +264,8 @@ class Verifier:
         """Logits [M, V_t] (float32) of hidden rows [M, d] through the verifier's head (ot_lm_head)."""
         if hidden.dtype != self._type() or hidden.dim() != 2 or hidden.shape[1] != self.d:
             raise ValueError(f"hidden rows are [M, {self.d}] of the verifier's type, not {tuple(hidden.shape)} {hidden.dtype}")
-        self._here(hidden=hidden)
+        if self.stream is not None or hidden.device != self.device:
+            self._here(hidden=hidden)
         M = hidden.shape[0]
         logits = self._empty((M, self.V_t), torch.float32)
         ot.ot_lm_head(self.ctx, M, hidden, logits, self.V_t)
@@ -286,9 +289,8 @@ class Verifier:
         if self.stream is not None or logits.device != dev or (tokens is not None and tokens.device != dev) or (temperature is not None and temperature.device != dev) or row_off is not None:
             self._here(logits=logits, tokens=tokens, temperature=temperature, row_off=row_off)
         # rows may lie further apart than V, and overlap nothing: one row alone may have any stride
-        return ot.make_logprob_in(M=M, V=V, dtype=ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, logits=logits.data_ptr(),
-                                  ld=logits.stride(0) if M > 1 else V, tokens=tokens, n_tok=n_tok, n_top=n_top, temperature=temperature,
-                                  row_off=row_off, B=B, given_rows_only=given_rows_only)
+        return ot.ot_logprob_in(M, V, ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, n_tok, n_top, 1 if given_rows_only else 0, B, 0,
+                                logits.stride(0) if M > 1 else V, logits.data_ptr(), ot._ptr(tokens), ot._ptr(temperature), ot._ptr(row_off))
 
     def token_logprobs(self, logits: torch.Tensor, tokens: Optional[torch.Tensor] = None, *, temperature: Optional[torch.Tensor] = None,
                        row_off: Optional[torch.Tensor] = None, n_top: int = 0, given_rows_only: bool = False) -> dict:
@@ -314,23 +316,33 @@ class Verifier:
                                                                 p + 4 * (at_top + n_top * M) if n_top else None))
         return out
 
+    def _statistic(self, forward, name, M):
+        """Address of a statistic that token_logprobs left."""
+        t = forward.get(name)
+        if t is None or t.dtype != torch.float32 or t.dim() != 1 or t.numel() != M or not t.is_contiguous():
+            raise ValueError(f"forward holds {name}, float32 [{M}]")
+        if self.stream is not None or t.device != self.device:
+            self._here(**{name: t})
+        return t.data_ptr()
+
     def token_logprobs_grad(self, logits: torch.Tensor, tokens: Optional[torch.Tensor], forward: dict, *, grad_logprob: Optional[torch.Tensor] = None,
                             grad_entropy: Optional[torch.Tensor] = None, temperature: Optional[torch.Tensor] = None,
                             row_off: Optional[torch.Tensor] = None, given_rows_only: bool = False) -> torch.Tensor:
         """Gradient of sum grad_logprob * logprob + sum grad_entropy * entropy with respect to the logits, in their type
         (ot_token_logprobs_grad).  forward: what token_logprobs returned for the same arguments."""
         given = self._logprob_in(logits, tokens, temperature, row_off, 0, given_rows_only)
-        for name, g, shape in (("grad_logprob", grad_logprob, None if tokens is None else tokens.shape), ("grad_entropy", grad_entropy, logits.shape[:1])):
-            if g is not None and (g.dtype != torch.float32 or g.shape != shape):
-                raise ValueError(f"{name} is float32 {shape}")
-        for name in ("row_max", "row_sumexp") if grad_entropy is None else ("row_max", "row_sumexp", "entropy"):
-            t = forward.get(name)
-            if t is None or t.dtype != torch.float32 or t.shape != logits.shape[:1]:
-                raise ValueError(f"forward holds {name}, float32 [{logits.shape[0]}]")
-            self._here(**{name: t})
-        self._here(grad_logprob=grad_logprob, grad_entropy=grad_entropy)
+        M = given.M
+        if grad_logprob is not None and (tokens is None or grad_logprob.dtype != torch.float32 or grad_logprob.shape != tokens.shape):
+            raise ValueError(f"grad_logprob is float32 {None if tokens is None else tuple(tokens.shape)}")
+        if grad_entropy is not None and (grad_entropy.dtype != torch.float32 or grad_entropy.dim() != 1 or grad_entropy.numel() != M):
+            raise ValueError(f"grad_entropy is float32 [{M}]")
+        if self.stream is not None or (grad_logprob is not None and grad_logprob.device != self.device) or (
+                grad_entropy is not None and grad_entropy.device != self.device):
+            self._here(grad_logprob=grad_logprob, grad_entropy=grad_entropy)
+        stats = ot.ot_logprob_out(None, None if grad_entropy is None else self._statistic(forward, "entropy", M), self._statistic(forward, "row_max", M),
+                                  self._statistic(forward, "row_sumexp", M), None, None)
         grad = self._empty(logits.shape, logits.dtype)
-        ot.ot_token_logprobs_grad(self.ctx, given, ot.make_logprob_out(forward), grad_logprob, grad_entropy, grad, logits.shape[1])
+        ot.ot_token_logprobs_grad(self.ctx, given, stats, grad_logprob, grad_entropy, grad, given.V)
         return grad
 
     def step_logprobs(self, inp: dict, *, from_logits: bool = False, n_top: int = 0, at_temperature: bool = True) -> dict:
