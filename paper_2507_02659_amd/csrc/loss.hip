@@ -488,7 +488,7 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
   a.row_off = in->row_off; a.temperature = in->temperature; a.draft_temperature = in->draft_temperature;
   a.draft_logits = in->draft_logits; a.draft_ids = in->draft_ids; a.dmap = ctx->dmap; a.tmap = ctx->tmap;
   a.Z = target_logits ? target_logits : ctx->Z; a.ldz = ctx->V_t;
-  a.row_max = ctx->row_max; a.row_sum = ctx->row_sum; a.drow_max = ctx->drow_max; a.drow_sum = ctx->drow_sum;
+  a.row_max = ctx->row_max; a.row_sum = ctx->row_sum; a.drow_max = ctx->drow_max; a.drow_sum = ctx->drow_sum; a.drow_arg = ctx->drow_arg;
   a.n_mapped = step->n_mapped; a.mapped_ids = step->mapped_ids; a.span_start = step->span_start; a.span_len = step->span_len;
   a.kind = out->kind; a.kl = out->kl; a.mass = ctx->loss_mass; a.weight = out->weight; a.totals = out->totals;
   a.grad_loss = grad_loss; a.grad = grad;

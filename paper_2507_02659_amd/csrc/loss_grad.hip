@@ -228,6 +228,10 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 // 2.6, arrival and totals 2.4, and the launch in front 4.
 // What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
 // sum q t gets the constants' part as their 64-bit difference times the mass of q.
+// The likeliest id, of which a sure drafter has nearly all of q, is left out of the sums: with `rest` the mass of the others, its 1 - q is
+// rest, and a - A = a rest - (sum q a of the others).  Formed from q, both would be what is left of numbers next to each other: the rows'
+// sums, which the step leaves, know 1 - q to 2^-24 at best, and with float32 q nothing below that came out right (rows of 1 - q = 1e-8 were
+// off by 14 times their gradient; by 0.16 times with the other form, which has the step's sums alone).
 // Rows for which that arithmetic leaves float32's range are done as the other form does all of them, in 64 bits and from memory: those of
 // temperatures below 2.1e-8 (kMostScale), where exponents overflow; and those that propose an id which the target masks (with -inf, or with a
 // number as low as -1e20): its term is infinite or nearly, however small q is, and a q below 2^-126 is not there in float32.  An n-gram's
@@ -243,6 +247,7 @@ struct alignas(16) GradRow {
   double invTd, lnSq, invT, lnS;   // for rows in 64 bits
   int32_t kind;                 // RowGrad's, and 4: in 64 bits
   int32_t row, sub, out, pre;
+  int32_t top;                  // the row's likeliest id, or -1
 };
 static_assert(sizeof(GradRow) % 16 == 0, "read as 16-byte units");
 
@@ -261,10 +266,12 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
   double Sq = 1.0, lq = 0.0;
   const double invT = 1.0 / (double)T_b, invTd = 1.0 / (double)Td_b;
   const bool counts = T_b > 0.f && Td_b > 0.f;
+  int top = -1;
   if (k > 0 && counts && m > 0) {                        // (ids outside the vocabulary: nothing is mapped)
     id = a.draft_ids[q];
     mxq = a.drow_max[q];
     Sq = a.drow_sum[q];
+    if (Sq > 0.0) top = a.drow_arg[q];
     lq = ((double)Draft<T>::one(static_cast<const T*>(a.draft_logits) + (int64_t)q * a.V_d + id) - (double)mxq) * invTd - log(Sq);
   }
   const double lnSq = log(Sq);
@@ -335,7 +342,7 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
   R.r0 = (float)(R.dlnS + 1.0);
   R.c = __shfl(c, j); R.D = __shfl(D, j); R.a_pre = __shfl(a_pre, j);
   R.kl_more = __shfl(kl_more, j); R.A_more = __shfl(A_more, j);
-  R.out = __shfl(out, j); R.pre = __shfl(pre, j); R.sub = id;
+  R.out = __shfl(out, j); R.pre = __shfl(pre, j); R.sub = id; R.top = top;
   const int ngram_kl_j = __shfl((int)ngram_kl, j);
   R.invTd = invTd; R.lnSq = lnSq; R.invT = invT;
   R.kind = !covered ? 0 : kind_j == 1 ? 1 : !ngram_kl_j ? 2 : is_first ? 3 : 2;
@@ -384,6 +391,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   extern __shared__ __attribute__((aligned(16))) float s_z[];   // [shift + id]: the target's logit at the id's image, then r
   __shared__ double s_term[4][16];
   __shared__ int s_last, s_far;
+  __shared__ float s_top;                                // the target's logit at the likeliest id's image
   const int drow = blockIdx.x, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   const T* zq = static_cast<const T*>(a.draft_logits) + (int64_t)drow * a.V_d;
   T* grad = static_cast<T*>(a.grad) + (int64_t)drow * a.V_d;
@@ -417,6 +425,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     *tq = d * R.s2q;
     return __builtin_amdgcn_exp2f(*tq) * R.inv_Sq;
   };
+  const int top_vec = R.kind != 0 && R.top >= 0 ? (shift + R.top) / (kRowThreads * kVec) : -1;   // the vectors that hold the likeliest id
   // while the record and the pairs are on their way
   const int slots = (a.V_d + shift + kVec - 1) / kVec * (kVec / 4);   // whole vectors, as they are read
   for (int i = tid; i < slots; i += kRowThreads) {
@@ -429,7 +438,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     s_last = arrive(a.count, a.K);
     if (s_last) publish(a.n_tokens, 0);
   };
-  float A = 0.f;
+  float A = 0.f, out_top = 0.f;
   asm volatile("" ::"v"(scale));                         // read by now
   if (tid == 0) s_far = R.kind & 4;
   __syncthreads();
@@ -462,7 +471,9 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
       if (R.pre >= 0) s_z[shift + R.pre] = __uint_as_float(kNoImage);
     }
     if (R.kind & 2) __syncthreads();
+    if (R.top >= 0 && tid == (shift + R.top) / kVec % kRowThreads) s_top = s_z[shift + R.top];   // its own word, below
     double kl = 0.0, mass = 0.0;
+    float rest_own = 0.f;
 #pragma unroll
     for (int i = 0; i < kVecs; ++i) {
       const int base = (i * kRowThreads + tid) * kVec;   // slot of the vector's first id
@@ -474,6 +485,10 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
 #pragma unroll
           for (int f = 0; f < 4; ++f) zr[e + f] = w[f];
         }
+        if (i == top_vec) {                              // the likeliest id stays out of the sums
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x[i * kVec + e] = base - shift + e == R.top ? -INFINITY : x[i * kVec + e];
+        }
         bool far = false;
 #pragma unroll
         for (int e = 0; e < kVec; ++e) {
@@ -483,6 +498,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
           const float diff = near ? (tq - fmaf(d, R.s2, d * R.s2_lo)) * 0.69314718f : 0.f;
           kl_i = fmaf(q, diff, kl_i);
           mass_i += ordinary ? q : 0.f;
+          rest_own += q;
           far |= ordinary && !near && tq > -1080.f;      // in 64 bits q may be above 0
           zr[e] = near ? diff + R.r0 : 0.f;
           x[i * kVec + e] = q;
@@ -496,13 +512,31 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     }
     kl = wave_sum(kl);
     mass = wave_sum(mass);
-    if (lane == 0) { s_term[0][wave] = kl; s_term[1][wave] = mass; }
+    double rest = wave_sum((double)rest_own);
+    if (lane == 0) { s_term[0][wave] = kl; s_term[1][wave] = mass; s_term[2][wave] = rest; }
     __syncthreads();
     wide = s_far != 0;
     kl = wave_sum(lane < 16 ? s_term[0][lane] : 0.0);
     mass = wave_sum(lane < 16 ? s_term[1][lane] : 0.0);
+    rest = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
     kl += R.dlnS * mass;                                 // sum over ordinary ids of q (ln q - ln p)
-    A = (float)(kl + mass + R.A_more);
+    double A_rest = kl + mass + (R.pre == R.top ? 0.0 : R.A_more), a_top = 0.0;
+    if (R.top >= 0) {
+      const double q_top = 1.0 - rest;
+      if (R.pre == R.top) {
+        a_top = R.a_pre;
+      } else if (__float_as_uint(s_top) != kNoImage) {
+        const double diff = -R.lnSq - (((double)s_top - (double)R.mx) * R.invT - R.lnS);
+        a_top = diff + 1.0;
+        kl += q_top * diff;
+        wide |= diff > 1e20;                             // masked by the target
+      }
+      A = (float)(A_rest + q_top * a_top);
+      out_top = (float)(R.c * (double)scale * q_top * (a_top * rest - A_rest));
+      if (R.kind & 2) out_top += (float)(R.D * (double)scale * (R.top == R.sub ? rest : -q_top));
+    } else {
+      A = (float)A_rest;
+    }
     if (R.kind & 2) {
       if (tid == 0 && R.pre >= 0) s_z[shift + R.pre] = (float)R.a_pre;
       __syncthreads();
@@ -511,6 +545,19 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
       publish(a.out.kl + R.row, kl + R.kl_more);
       count_in();
     }
+  } else if (R.kind == 2 && R.top >= 0) {                // without a KL part: what is left of the likeliest id
+    float rest_own = 0.f;
+#pragma unroll
+    for (int i = 0; i < kEach; ++i) {
+      float tq;
+      rest_own += q_of(first(i / kVec) + i % kVec == R.top ? -INFINITY : x[i], &tq);
+    }
+    double rest = wave_sum((double)rest_own);
+    if (lane == 0) s_term[2][wave] = rest;
+    __syncthreads();
+    rest = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
+    out_top = (float)(R.D * (double)scale * (R.top == R.sub ? rest : rest - 1.0));
+    if (tid == 0) count_in();
   } else if (!wide && tid == 0) {
     count_in();
   }
@@ -567,6 +614,10 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
         float tq;
         out[e] = R.kind ? D * ((base - shift + e == R.sub ? 1.f : 0.f) - q_of(x[i * kVec + e], &tq)) : 0.f;
       }
+    }
+    if (i == top_vec) {
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) out[e] = base - shift + e == R.top ? out_top : out[e];
     }
     if (whole(i)) {
       Draft<T>::store(grad + first(i), out);

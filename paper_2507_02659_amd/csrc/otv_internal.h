@@ -201,7 +201,7 @@ struct LossGradArgs {
   const float* Z;
   int64_t ldz;
   const float* row_max; const double* row_sum;
-  const float* drow_max; const double* drow_sum;
+  const float* drow_max; const double* drow_sum; const int32_t* drow_arg;
   const int32_t* n_mapped; const int32_t* mapped_ids; const int32_t* span_start; const int32_t* span_len;
   const int32_t* kind; const double* kl; const double* mass; const double* weight; const double* totals;
   const float* grad_loss;   // or nullptr: 1

@@ -140,3 +140,33 @@ def test_a_gradient_over_the_logits_is_refused(dtype):
         v.synchronize()
         assert torch.equal(memory[first:first + K], want)
     v.close()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V_t,V_d,n_direct", [(600, 301, 240), (9000, 8000, 7000), (20000, 33001, 15000)])
+@pytest.mark.parametrize("up", [6, 14, 22])
+def test_a_sure_drafter(up, V_t, V_d, n_direct, dtype):
+    """Rows whose likeliest id has all of q but 1e-1 to 1e-8: its gradient is made of what the others have, and is right relative to that.  (The
+    tolerance of every other id is that of the other tests; of the likeliest one, q (a - A) = q (a rest - sum of the others' q a), D (1 - q) =
+    D rest: the terms' own bounds times rest, and the others'.  rest, a float32 sum of V_d / 1024 values in a thread, is off by 2^-24 each at most.)"""
+    from oracle import distill_grad as og
+    case = make_case(_spec("sure", [6, 7, 5, 6] * 4, 31 + up, dtype=dtype, V_t=V_t, V_d=V_d, n_direct=n_direct, temperature=[1.0] * 16))
+    rng = np.random.default_rng(up)
+    rows, ids = np.arange(case.K), np.where(rng.random(case.K) < 0.8, case.draft_ids, rng.integers(0, V_d, case.K))
+    z = (case.draft_logits.astype(np.uint32) << 16).view(np.float32) if dtype == "bf16" else case.draft_logits
+    z[rows, ids] = np.round(z.max(1) + up)                # whole numbers: bfloat16 holds them
+    case.draft_logits = (z.view(np.uint32) >> 16).astype(np.uint16) if dtype == "bf16" else z
+    assert case.K >= 64
+    want, scale, _ = og.hybrid_loss_grad_case(case)
+    wide = z.astype(np.longdouble)
+    e = np.exp(wide - wide.max(1, keepdims=True))
+    e[rows, ids] = 0.0
+    rest = (e.sum(1) / (1.0 + e.sum(1))).astype(np.float64)
+    others = scale.copy()
+    others[rows, ids] = 0.0
+    scale[rows, ids] = scale[rows, ids] * rest + others.sum(1)
+    _, (got, _) = _two_forms(case)
+    tol = 8e-6 * scale
+    tol += (2.0 ** -8 if dtype == "bf16" else 2.0 ** -24) * (np.abs(want) + tol) + 1e-37
+    off = np.abs(got["grad"] - want) / tol
+    assert off.max() <= 1.0, (off.max(), np.unravel_index(off.argmax(), off.shape))
