@@ -8,11 +8,12 @@
 // at most once per hidden index, partial sums of h (c - 7.5) and of h (these times zp - 7.5), and the running total of scaled groups once per
 // group, above 16 rows with the offsets of up to four groups in it.  The roundings add up as a random walk.
 //
-// What bounds it, groups of 128, weights from memory: up to 16 rows the weight stream (6 rows x 3584 x 152064 53-56 us, 5.3 TB/s, what a
-// large copy moves; a bf16 head 163); above, the trips through LDS and registers between the products: 144 x 4096 x 128256 167-175 us, 0.9
-// PFLOP/s, where the products alone take 95 and the weights 55.  With parts of the work left out (timing only): LDS reads 35 us less, staging
-// 24, dequantisation 4, scaling 0.  Wavefronts of 64 columns, one per SIMD, with 32 x 32 x 16 products took 314 us, two blocks of 128 per
-// barrier at nine row tiles 185.
+// What bounds it, groups of 128, weights from memory: up to 16 rows the weight stream (6 rows x 3584 x 152064 53 us, 5.4 TB/s, what a
+// large copy moves; a bf16 head 163); above, the trips through LDS and registers between the products: 144 x 4096 x 128256 166-176 us, 0.9
+// PFLOP/s, where the products alone take 95 and the weights 55; a bf16 head takes 172 there and 900 for 1017 rows, this one 1217.  With parts
+// of the work left out (timing only): LDS reads 35 us less, staging 24, dequantisation 4, scaling 0.  Wavefronts of 64 columns, one per SIMD,
+// with 32 x 32 x 16 products took 314 us, two blocks of 128 per barrier at nine row tiles 185.  Other ways to c - 7.5 of the same accuracy:
+// sizes looked up as fp8 numbers by byte permutations 59 us for the 6 rows, bf16 halves looked up and put together 62.
 #include <algorithm>
 
 #include "device_math.h"
