@@ -389,7 +389,7 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
   typedef float f32x4 __attribute__((ext_vector_type(4)));
   constexpr int kVec = Draft<T>::kElems, kEach = kVecs * kVec, kPairs = 8;
   extern __shared__ __attribute__((aligned(16))) float s_z[];   // [shift + id]: the target's logit at the id's image, then r
-  __shared__ double s_term[4][16];
+  __shared__ double s_term[5][16];                       // a row for each sum: nothing is written again before the totals
   __shared__ int s_last, s_far;
   __shared__ float s_top;                                // the target's logit at the likeliest id's image
   const int drow = blockIdx.x, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
@@ -513,12 +513,12 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
     kl = wave_sum(kl);
     mass = wave_sum(mass);
     double rest = wave_sum((double)rest_own);
-    if (lane == 0) { s_term[0][wave] = kl; s_term[1][wave] = mass; s_term[2][wave] = rest; }
+    if (lane == 0) { s_term[0][wave] = kl; s_term[1][wave] = mass; s_term[4][wave] = rest; }
     __syncthreads();
     wide = s_far != 0;
     kl = wave_sum(lane < 16 ? s_term[0][lane] : 0.0);
     mass = wave_sum(lane < 16 ? s_term[1][lane] : 0.0);
-    rest = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
+    rest = wave_sum(lane < 16 ? s_term[4][lane] : 0.0);
     kl += R.dlnS * mass;                                 // sum over ordinary ids of q (ln q - ln p)
     double A_rest = kl + mass + (R.pre == R.top ? 0.0 : R.A_more), a_top = 0.0;
     if (R.top >= 0) {
@@ -553,9 +553,9 @@ __global__ __launch_bounds__(kRowThreads) void loss_row_kernel(LossGradArgs a) {
       rest_own += q_of(first(i / kVec) + i % kVec == R.top ? -INFINITY : x[i], &tq);
     }
     double rest = wave_sum((double)rest_own);
-    if (lane == 0) s_term[2][wave] = rest;
+    if (lane == 0) s_term[4][wave] = rest;
     __syncthreads();
-    rest = wave_sum(lane < 16 ? s_term[2][lane] : 0.0);
+    rest = wave_sum(lane < 16 ? s_term[4][lane] : 0.0);
     out_top = (float)(R.D * (double)scale * (R.top == R.sub ? rest : rest - 1.0));
     if (tid == 0) count_in();
   } else if (!wide && tid == 0) {
