@@ -209,6 +209,13 @@ def _ptr(x) -> Optional[int]:
     return address()
 
 
+def _on_gpu(x) -> Optional[int]:
+    """_ptr of what the device reads or writes: a tensor or array in host memory is refused, whose address a kernel would take for its own."""
+    if x is not None and not isinstance(x, int) and not getattr(x, "is_cuda", False):
+        raise ValueError(f"device memory is needed, not {type(x).__name__} in host memory")
+    return _ptr(x)
+
+
 def _check(rc: int):
     if rc != OT_OK:
         raise OtError(rc, ot_last_error())
@@ -236,7 +243,7 @@ def ot_verify_init_quantized(*, d, V_t, V_d, max_batch, max_k, max_ngram_len, co
     """codes [d / 2, V_t], scales and (or None) zeros [ceil(d / group), V_t]: device tensors or addresses.  Returns the context handle."""
     dm = None if direct_map is None else np.ascontiguousarray(direct_map, dtype=np.int32)
     cfg = ot_verify_config(d, V_t, V_d, max_batch, max_k, dtype, max_ngram_len, int(draft_side), None, _ptr(dm), _ptr(stream))
-    w = ot_quant_weights(int(group), int(scale_dtype), _ptr(codes), _ptr(scales), _ptr(zeros))
+    w = ot_quant_weights(int(group), int(scale_dtype), _on_gpu(codes), _on_gpu(scales), _on_gpu(zeros))
     ctx = C.c_void_p()
     _check(load_library().ot_verify_init_quantized(C.byref(cfg), C.byref(w), C.byref(ctx)))
     return ctx
@@ -244,7 +251,7 @@ def ot_verify_init_quantized(*, d, V_t, V_d, max_batch, max_k, max_ngram_len, co
 
 def ot_lm_head(ctx, M: int, hidden, logits, ld: int):
     """logits: device tensor or address; rows may be ld elements apart (a tensor that is not contiguous: pass its address)."""
-    _check(load_library().ot_lm_head(ctx, M, _ptr(hidden), _ptr(logits), ld))
+    _check(load_library().ot_lm_head(ctx, M, _on_gpu(hidden), _on_gpu(logits), ld))
 
 
 def ot_verify_destroy(ctx):
@@ -346,18 +353,18 @@ def ot_distill_loss_grad(ctx, step_in: ot_step_in, step_out: ot_step_out, target
     cfg = ot_loss_config(float(lam), int(lambda_mode), int(ngram_term), 1 if accepted_only else 0)
     out = ot_loss_out(*[_ptr(buffers.get(n)) for n in LOSS_OUT])
     _check(load_library().ot_distill_loss_grad(ctx, C.byref(step_in), C.byref(step_out), _ptr(target_logits), C.byref(cfg), C.byref(out),
-                                               _ptr(grad_loss), _ptr(grad)))
+                                               _on_gpu(grad_loss), _on_gpu(grad)))
 
 
 def make_logprob_in(*, M, V, dtype, logits, ld, tokens, n_tok, n_top=0, temperature=None, row_off=None, B=0, given_rows_only=False,
                     reserved=0) -> ot_logprob_in:
-    return ot_logprob_in(M, V, dtype, n_tok, n_top, 1 if given_rows_only else 0, B, reserved, ld, _ptr(logits), _ptr(tokens), _ptr(temperature),
-                         _ptr(row_off))
+    return ot_logprob_in(M, V, dtype, n_tok, n_top, 1 if given_rows_only else 0, B, reserved, ld, _on_gpu(logits), _on_gpu(tokens),
+                         _on_gpu(temperature), _on_gpu(row_off))
 
 
 def make_logprob_out(buffers: dict) -> ot_logprob_out:
     """buffers: name -> device tensor/address for the fields of ot_logprob_out (those not wanted may be absent)."""
-    return ot_logprob_out(*[_ptr(buffers.get(n)) for n in LOGPROB_OUT])
+    return ot_logprob_out(*[_on_gpu(buffers.get(n)) for n in LOGPROB_OUT])
 
 
 def ot_token_logprobs(ctx, given: ot_logprob_in, out: ot_logprob_out):
@@ -365,7 +372,8 @@ def ot_token_logprobs(ctx, given: ot_logprob_in, out: ot_logprob_out):
 
 
 def ot_token_logprobs_grad(ctx, given: ot_logprob_in, forward: ot_logprob_out, grad_logprob, grad_entropy, grad, ld_grad: int):
-    _check(load_library().ot_token_logprobs_grad(ctx, C.byref(given), C.byref(forward), _ptr(grad_logprob), _ptr(grad_entropy), _ptr(grad), ld_grad))
+    _check(load_library().ot_token_logprobs_grad(ctx, C.byref(given), C.byref(forward), _on_gpu(grad_logprob), _on_gpu(grad_entropy),
+                                                 _on_gpu(grad), ld_grad))
 
 
 def ot_adaptive_drafting(ctx, *, B, gamma, w_accept=1.0, w_reject=1.0, row_off, row_off_host, head_logits, labels=None,

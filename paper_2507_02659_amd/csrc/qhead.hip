@@ -1,7 +1,7 @@
 // A target head of 4-bit weights with group scales: z[m][v] = sum over groups g of s[g][v] * sum_{k in g} h[m][k] (c[k][v] - zp[g][v]).
 //
-// The codes c (0..15) become bf16 operands c - 7.5 of v_mfma_f32_16x16x32_bf16: with c's range in the middle of the format's, so that what
-// a group's product sums is of the size of the weights.  (With 16 + c, one instruction less per word, the sums were 24 times the hidden states
+// The codes c (0..15) become bf16 operands c - 7.5 of v_mfma_f32_16x16x32_bf16: centred, so that what
+// a group's product sums is of the size of the weights.  (With 16 + c, by as many instructions, the sums were 24 times the hidden states
 // and their rounding 2 to 5 times as large in the logits, without end where c = zp.)  A group's product is sum h (c - 7.5), and the sum of the
 // group's hidden states, the same for every column, takes (zp - 7.5) times itself off it; then the group's scale multiplies 16 rows x 16 columns
 // in four instructions.  Products of a bf16 number and c - 7.5 are exact in fp32, so what is rounded is the sums alone, 2^-24 of each: a group's

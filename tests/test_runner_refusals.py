@@ -104,3 +104,41 @@ def test_weights_elsewhere(v, monkeypatch, away):
         Verifier.quantized(QuantWeights(**w), **args)
     with pytest.raises(ValueError, match=away + " is on meta"):
         Verifier.quantized(QuantWeights(**dict(w, **{away: w[away].to("meta")})), **args)
+
+
+def test_the_binding_takes_no_host_memory(monkeypatch):
+    """The entry points' mirrors: a tensor or an array in host memory is refused wherever the device reads or writes, before the library is called."""
+    import numpy as np
+
+    class Library:
+        def __getattr__(self, name):
+            return lambda *args: pytest.fail("reached the library")
+
+    monkeypatch.setattr(ot, "load_library", Library)
+    for host in (torch.zeros(4), np.zeros(4, np.float32)):
+        for args in ((None, 1, host, 0x1000, 4), (None, 1, 0x1000, host, 4)):
+            with pytest.raises(ValueError, match="host memory"):
+                ot.ot_lm_head(*args)
+        given = dict(M=1, V=4, dtype=ot.OT_F32, logits=0x1000, ld=4, tokens=0x1000, n_tok=1, temperature=0x1000, row_off=0x1000, B=1)
+        for name in ("logits", "tokens", "temperature", "row_off"):
+            with pytest.raises(ValueError, match="host memory"):
+                ot.make_logprob_in(**dict(given, **{name: host}))
+        for name in ot.LOGPROB_OUT:
+            with pytest.raises(ValueError, match="host memory"):
+                ot.make_logprob_out({name: host})
+        for at in (3, 4, 5):
+            args = [None, ot.make_logprob_in(**given), ot.make_logprob_out({}), 0x1000, 0x1000, 0x1000, 4]
+            args[at] = host
+            with pytest.raises(ValueError, match="host memory"):
+                ot.ot_token_logprobs_grad(*args)
+        weights = dict(codes=0x1000, scales=0x1000, zeros=None)
+        for name in weights:
+            with pytest.raises(ValueError, match="host memory"):
+                ot.ot_verify_init_quantized(d=8, V_t=4, V_d=1, max_batch=1, max_k=0, max_ngram_len=2, group=32, scale_dtype=ot.OT_BF16, direct_map=None,
+                                            **dict(weights, **{name: host}))
+        for name in ("grad_loss", "grad"):
+            sin = ot.make_step_in(B=0, step=0, seed=0, **{n: None for n in ("row_off", "row_off_host", "hidden", "draft_logits", "draft_ids", "temperature",
+                                                                            "draft_temperature", "seq_id")})
+            with pytest.raises(ValueError, match="host memory"):
+                ot.ot_distill_loss_grad(None, sin, ot.make_step_out({}), None, lam=0.2, lambda_mode=0, ngram_term=0, accepted_only=False, buffers={},
+                                        **dict(dict(grad_loss=None, grad=0x1000), **{name: host}))
