@@ -26,6 +26,9 @@ namespace {
 // 0, or NaN where the row's sum is.
 __device__ inline double nan_of(double lnS) { return lnS != lnS ? lnS : 0.0; }
 
+// A drafter is sure of a row's likeliest id where the others' sum of exponentials is below an eighth of its own.
+constexpr double kSureSum = 1.125;
+
 struct RowGrad {
   double mxq, invTd, lnSq;      // ln q(i) = (zq_i - mxq) * invTd - lnSq
   double mx, invT, lnS;         // ln p(v) = (z_v - mx) * invT - lnS
@@ -34,6 +37,7 @@ struct RowGrad {
   int32_t kind;                 // 0: zeros, 1: the KL part, 2: D alone, 3: both
   int32_t row, sub;             // the token's target row; the draft row's drafted id
   int32_t out, pre;             // draft ids whose a is 0 / a_pre, or -1
+  int32_t top;                  // the likeliest id of a sure drafter, or -1
 };
 
 template <typename T> struct Draft;
@@ -83,6 +87,7 @@ __device__ inline RowGrad make_row(const LossGradArgs& a, int drow, int lane) {
   const int m = a.n_mapped[b], s_l = a.span_start[r], len_l = a.span_len[r], kind_l = a.kind[r], t_l = a.mapped_ids[r], id_l = a.draft_ids[q];
   const float T_b = a.temperature[b], Td_b = a.draft_temperature ? a.draft_temperature[b] : T_b;
   const double kl_l = a.kl[r], mass_l = a.mass[r], weight_l = a.weight[r], sum_l = a.row_sum[r], dsum_l = a.drow_sum[q];
+  const int arg_l = a.drow_arg[q];
   const float mx_l = a.row_max[r], dmx_l = a.drow_max[q], up = a.grad_loss ? *a.grad_loss : 1.f;
   const double n = fmax(1.0, a.totals[2] + a.totals[3]);
   const unsigned long long who = __ballot(lane < m && s_l <= at && at < s_l + len_l);
@@ -95,6 +100,9 @@ __device__ inline RowGrad make_row(const LossGradArgs& a, int drow, int lane) {
   const double lnSq_l = log(dsum_l);
   R.mxq = (double)__shfl(dmx_l, at); R.lnSq = __shfl(lnSq_l, at);
   R.none = nan_of(R.lnSq);
+  const int arg = __shfl(arg_l, at);
+  const double Sq = __shfl(dsum_l, at);
+  R.top = Sq > 0.0 && Sq < kSureSum ? arg : -1;
   R.mx = (double)__shfl(mx_l, j); R.lnS = log(__shfl(sum_l, j));
   R.c = (double)up / n * R.invTd;
   R.kind = 1;
@@ -146,6 +154,48 @@ __device__ inline float grad_at(const RowGrad& R, int i, float x, int image, flo
   return (float)g;
 }
 
+// The gradient at a sure drafter's likeliest id, by a workgroup: what loss_row_kernel says of it, with the others' mass summed here.  q a of that
+// id comes off A as the loss's launch put it there, in 64 bits.  s_sum: 4 numbers of shared memory.
+template <typename T>
+__device__ inline float grad_at_top(const LossGradArgs& a, const RowGrad& R, const T* zq, int shift, int tid, double* s_sum) {
+  constexpr int kVec = Draft<T>::kElems, kAtOnce = 32 / kVec;
+  const float mxq = (float)R.mxq, s2 = (float)(R.invTd * 1.4426950408889634);
+  auto q_of = [&](float x) { return __builtin_amdgcn_exp2f(fmaxf(x - mxq, -1e30f) * s2); };   // times the row's sum
+  double rest = 0.0;
+  const int vecs = (a.V_d + shift) / kVec;               // whole ones, from the 16-byte boundary at or before the row's start; its ends one by one
+  for (int v = tid + 1; v < vecs; v += 256 * kAtOnce) {
+    float x[kAtOnce][kVec];
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) Draft<T>::load(zq - shift + min(v + 256 * j, vecs - 1) * kVec, x[j]);
+#pragma unroll
+    for (int j = 0; j < kAtOnce; ++j) {
+      float part = 0.f;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) part += (v + 256 * j) * kVec - shift + e != R.top ? q_of(x[j][e]) : 0.f;
+      if (v + 256 * j < vecs) rest += (double)part;
+    }
+  }
+  const int first = min(kVec - shift, a.V_d), last = max(vecs * kVec - shift, first), i = tid < first ? tid : last + tid - first;
+  if (i < a.V_d && i != R.top) rest += (double)q_of(Draft<T>::one(zq + i));
+  rest = wave_sum(rest);
+  if ((tid & 63) == 0) s_sum[tid >> 6] = rest;
+  __syncthreads();
+  const double others = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), mass = others / (1.0 + others), q_top = 1.0 - mass;
+  const double pull = R.kind & 2 ? R.D * (R.top == R.sub ? mass : -q_top) : 0.0;
+  if (!(R.kind & 1)) return (float)pull;
+  const double lq = -R.lnSq;
+  const int image = a.dmap[R.top];
+  double a_top = 0.0, A_rest = R.A;
+  if (R.top == R.pre) {
+    a_top = R.a_pre;
+    A_rest -= exp(lq) * a_top;
+  } else if (image >= 0 && R.top != R.out) {
+    a_top = lq - ln_p(R, a.Z[(int64_t)R.row * a.ldz + image]) + 1.0;
+    A_rest -= exp_neg_fast(lq) * a_top;
+  }
+  return (float)(pull + R.c * q_top * (a_top * mass - A_rest));
+}
+
 // Grid = groups of draft ids x draft rows, the groups of a row on one XCD back to back, so that its L2 holds the target row that they gather
 // from (across all of them: 58 us for 128 rows of 32000 ids with the loss in front).  A thread has whole vectors of its row, laid out from
 // the 16-byte boundary at or before the row's start; the row's ends go element by element.
@@ -157,6 +207,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
   constexpr int kVec = Draft<T>::kElems, kEach = kGradVecs * kVec;
   typedef int image_t __attribute__((ext_vector_type(4), aligned(4)));
   __shared__ RowGrad s_row;
+  __shared__ double s_sum[4];
   const int slot = (int)(blockIdx.x >> 3), drow = slot / groups * 8 + (int)(blockIdx.x & 7u), tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   if (drow >= a.K) return;                               // padding of the id space
   const T* zq = static_cast<const T*>(a.draft_logits) + (int64_t)drow * a.V_d;
@@ -205,6 +256,12 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 #pragma unroll
     for (int e = 0; e < kEach; ++e) out[e] = R.kind ? grad_at<false>(R, first(e / kVec) + e % kVec, x[e], -1, 0.f) : 0.f;
   }
+  const int first_id = slot % groups * kGradIds<T> - shift;
+  if (R.kind != 0 && R.top >= max(first_id, 0) && R.top < first_id + kGradIds<T>) {   // the same in the whole workgroup
+    const float g = grad_at_top(a, R, zq, shift, tid, s_sum);
+#pragma unroll
+    for (int e = 0; e < kEach; ++e) out[e] = first(e / kVec) + e % kVec == R.top ? g : out[e];
+  }
 #pragma unroll
   for (int i = 0; i < kGradVecs; ++i) {
     if (whole(i)) {
@@ -231,7 +288,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 // The likeliest id, of which a sure drafter has nearly all of q, is left out of the sums: with `rest` the mass of the others, its 1 - q is
 // rest, and a - A = a rest - (sum q a of the others).  Formed from q, both would be what is left of numbers next to each other: the rows'
 // sums, which the step leaves, know 1 - q to 2^-24 at best, and with float32 q nothing below that came out right (rows of 1 - q = 1e-8 were
-// off by 14 times their gradient; by 0.16 times with the other form, which has the step's sums alone).
+// off by 14 times their gradient).
 // Rows for which that arithmetic leaves float32's range are done as the other form does all of them, in 64 bits and from memory: those of
 // temperatures below 2.1e-8 (kMostScale), where exponents overflow; and those that propose an id which the target masks (with -inf, or with a
 // number as low as -1e20): its term is infinite or nearly, however small q is, and a q below 2^-126 is not there in float32.  An n-gram's
