@@ -285,7 +285,7 @@ __global__ __launch_bounds__(256) void loss_grad_kernel(LossGradArgs a, int grou
 // 2.6, arrival and totals 2.4, and the launch in front 4.
 // What the row kernel computes is float32 with the constants (maxima, ln S) apart: t = (zq - mxq)/Td - (z - mx)/T is formed without them, and
 // sum q t gets the constants' part as their 64-bit difference times the mass of q.
-// The likeliest id, of which a sure drafter has nearly all of q, is left out of the sums: with `rest` the mass of the others, its 1 - q is
+// The likeliest id of a row of which it has nearly all of q (kSureSum) is left out of the sums: with `rest` the mass of the others, its 1 - q is
 // rest, and a - A = a rest - (sum q a of the others).  Formed from q, both would be what is left of numbers next to each other: the rows'
 // sums, which the step leaves, know 1 - q to 2^-24 at best, and with float32 q nothing below that came out right (rows of 1 - q = 1e-8 were
 // off by 14 times their gradient).
@@ -304,7 +304,7 @@ struct alignas(16) GradRow {
   double invTd, lnSq, invT, lnS;   // for rows in 64 bits
   int32_t kind;                 // RowGrad's, and 4: in 64 bits
   int32_t row, sub, out, pre;
-  int32_t top;                  // the row's likeliest id, or -1
+  int32_t top;                  // the likeliest id of a sure drafter, or -1
 };
 static_assert(sizeof(GradRow) % 16 == 0, "read as 16-byte units");
 
@@ -328,7 +328,7 @@ __global__ __launch_bounds__(256) void loss_prepare_kernel(LossGradArgs a) {
     id = a.draft_ids[q];
     mxq = a.drow_max[q];
     Sq = a.drow_sum[q];
-    if (Sq > 0.0) top = a.drow_arg[q];
+    if (Sq > 0.0 && Sq < kSureSum) top = a.drow_arg[q];
     lq = ((double)Draft<T>::one(static_cast<const T*>(a.draft_logits) + (int64_t)q * a.V_d + id) - (double)mxq) * invTd - log(Sq);
   }
   const double lnSq = log(Sq);
