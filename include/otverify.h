@@ -114,13 +114,14 @@ void ot_verify_destroy(ot_ctx* ctx);          /* synchronises the stream, frees 
 
 /* ---- a target head of 4-bit weights --------------------------------------------------------------------- */
 /* W[k][v] = scale[k / group][v] * (code[k][v] - zero[k / group][v]) with codes of 0..15: a quarter of the OT_BF16 weights'
- * bytes.  Up to 16 rows that stream is what bounds the head, above it more and more the products: against 128256 columns of 4096 a
- * step takes 68 us instead of an OT_BF16 head's 176 with 6 rows, 74 / 180 with 24, 86 / 186 with 48, 118 / 197 with 80, as long with
- * 144 (192 / 191), and longer from there on (288 rows 358 / 312, 1017 1320 / 963): for prompts the OT_BF16 head is the faster one.  The hidden states are not rounded, products with
- * codes less 7.5 are exact, and what is summed in fp32 is h (code - 7.5), of which (zero - 7.5) times the sum of h is taken off, per group, then the
- * scaled groups: a logit is that of the weights above but for the roundings, 2^-24 each, of these sums' partial ones.  (A column whose codes
- * equal its zero point leaves what that rounds off and not exactly 0.)  Scales are finite.  A hidden row with an infinity or a NaN has NaN
- * logits, and so is a logit that float32 does not hold; hidden states are taken to stay below 2^100.                                          */
+ * bytes.  Up to 16 rows that stream is what bounds the head, above it more and more the products.  A step against 128256
+ * columns of 4096 takes 68 us with 6 rows (through an OT_BF16 head 176), 74 (180) with 24, 86 (186) with 48, 118 (197) with
+ * 80, 192 (191) with 144, 358 (312) with 288 and 1320 (963) with 1017: for prompts the OT_BF16 head is the faster one.
+ * The hidden states are not rounded, and products with codes less 7.5 are exact.  Summed in fp32 are h (code - 7.5), of which
+ * (zero - 7.5) times the sum of h is taken off, per group, then the scaled groups: a logit is that of the weights above but
+ * for the roundings, 2^-24 each, of these sums' partial ones.  (A column whose codes equal its zero point leaves what that
+ * rounds off and not exactly 0.)  Scales are finite.  A hidden row with an infinity or a NaN has NaN logits, and so is a
+ * logit that float32 does not hold; hidden states are taken to stay below 2^100.                                  */
 typedef struct ot_quant_weights {
   int32_t        group;        /* 32, 64 or 128: so many consecutive hidden indices share a scale and a zero point; d may end
                                   inside a group                                                              */

@@ -228,9 +228,10 @@ __global__ __launch_bounds__(1024) void qhead_rows16_kernel(const uint16_t* __re
   }
 }
 
-// More than 16 rows: blocks of RT tiles of 16 rows, so that weights are read and dequantised once for up to 144 rows.  A wavefront owns S tiles of 16 columns over the whole hidden dimension; the block's
-// hidden rows come through LDS in chunks of kBlocks * 128 hidden indices, two buffers, one barrier per chunk.  A wavefront stages whole
-// (row tile, block) units, in the order of the matrix instruction's operand, and forms their groups' sums on the way (a product with ones).
+// More than 16 rows: blocks of RT tiles of 16 rows, so that weights are read and dequantised once for up to 144 rows.  A wavefront owns S tiles
+// of 16 columns over the whole hidden dimension; the block's hidden rows come through LDS in chunks of kBlocks * 128 hidden indices, two buffers,
+// one barrier per chunk.  A wavefront stages whole (row tile, block) units, in the order of the matrix instruction's operand, and forms their
+// groups' sums on the way (a product with ones).
 constexpr int kTallWaves = 8;
 // Blocks per chunk: as many as registers and LDS hold (36 rows x 128256 with two instead of one 78.5 us instead of 82.2).
 constexpr int tall_blocks(int RT, int S) { return S > 2 ? (RT <= 4 ? 2 : 1) : RT <= 2 ? 4 : RT <= 4 ? 2 : 1; }

@@ -286,7 +286,8 @@ class Verifier:
         if row_off is not None and row_off.dtype != torch.int32:
             raise ValueError("row_off is int32")
         dev = self.device                           # (a call of one row is bound by the host)
-        if self.stream is not None or logits.device != dev or (tokens is not None and tokens.device != dev) or (temperature is not None and temperature.device != dev) or row_off is not None:
+        if (self.stream is not None or row_off is not None or logits.device != dev or (tokens is not None and tokens.device != dev)
+                or (temperature is not None and temperature.device != dev)):
             self._here(logits=logits, tokens=tokens, temperature=temperature, row_off=row_off)
         # rows may lie further apart than V, and overlap nothing: one row alone may have any stride
         return ot.ot_logprob_in(M, V, ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, n_tok, n_top, 1 if given_rows_only else 0, B, 0,
