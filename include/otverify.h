@@ -41,8 +41,9 @@ extern "C" {
 #define OT_ERR_DTYPE         -3   /* a type that the call does not take                                      */
 #define OT_ERR_MAP           -4   /* direct map entry out of range, or two draft ids share a target id       */
 #define OT_ERR_NGRAM         -5   /* n-gram entry length or id out of range                                  */
-#define OT_ERR_CTX_MISMATCH  -6   /* the n-gram cache was built for another context; of ot_lm_head, ot_token_logprobs, their
-                                     gradients and ot_distill_loss_grad: another HIP device than the context's is current */
+#define OT_ERR_CTX_MISMATCH  -6   /* the n-gram cache was built for another context; of ot_lm_head, ot_token_logprobs, ot_adapter_logits,
+                                     ot_adjust_logits, ot_top_distill_loss, their gradients and ot_distill_loss_grad: another HIP device
+                                     than the context's is current */
 #define OT_ERR_HIP           -7   /* a HIP call failed; ot_last_error() carries hipGetErrorString            */
 #define OT_ERR_NOMEM         -8   /* host or device allocation failed                                        */
 
@@ -331,6 +332,120 @@ int ot_token_logprobs(ot_ctx* ctx, const ot_logprob_in* in, ot_logprob_out* out)
  * share no byte with their rows.                                                                                 */
 int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logprob_out* forward, const float* grad_logprob_or_null,
                            const float* grad_entropy_or_null, void* grad, int64_t ld_grad);
+
+/* ---- low-rank adapters of many requests beside the head ------------------------------------------------------ */
+/* out[m][v] = logits[m][v] + scale[a] * sum_r up[a][v][r] * (sum_k hidden[m][k] * down[a][r][k]),  a = adapter[m]: every row through
+ * the adapter of its own request, in one call, beside the projection that they share.
+ *   - adapter[m] = -1: the row has none, out[m] = logits[m].  Outside [-1, n_adapters): the row is NaN.
+ *   - Both matrices lie as linear layers keep them, [outputs, inputs].  Adapters of a lower rank are padded with zeros.
+ *   - Sums are fp32; the inner one enters the outer one whole (OT_BF16: as three bfloat16 parts).  A row whose inner sum is not
+ *     finite is NaN.
+ *   - Rows of one adapter that lie within 64 rows of each other share what is read of it: keep a request's rows together.
+ * Work is enqueued on the context's stream; calls on one context share its workspace.  Any head's logits may be given: the target's
+ * (ot_lm_head), the drafter's or another model's.                                                                 */
+#define OT_MAX_ADAPTER_RANK 256
+typedef struct ot_adapter_in {
+  int32_t        M, d, V;             /* rows; hidden size (OT_BF16: a multiple of 8); ids per row                 */
+  int32_t        rank;                /* 1..OT_MAX_ADAPTER_RANK; a multiple of 8 (OT_F32: of 4)                     */
+  int32_t        n_adapters;
+  int32_t        dtype;               /* OT_BF16 or OT_F32: type of hidden, down and up                             */
+  int32_t        logits_dtype;        /* OT_BF16 or OT_F32: type of logits and out                                  */
+  int32_t        reserved;            /* must be 0                                                              */
+  int64_t        ld;                  /* elements from a row of logits to the next, at least V                      */
+  const void*    hidden;              /* DEVICE [M, d] row-major; this and the matrices from a multiple of 16 bytes on */
+  const void*    down;                /* DEVICE [n_adapters, rank, d]                                               */
+  const void*    up;                  /* DEVICE [n_adapters, V, rank]                                               */
+  const float*   scale;               /* DEVICE [n_adapters], or NULL: 1                                            */
+  const int32_t* adapter;             /* DEVICE [M]                                                             */
+  const void*    logits;              /* DEVICE, row m at logits + m * ld elements, or NULL: 0                      */
+} ot_adapter_in;
+/* out: DEVICE, row m at out + m * ld_out elements, ld_out >= V, written whole up to V; it may be the logits themselves (with the same
+ * ld), or share no byte with their rows.                                                                          */
+int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t ld_out);
+
+/* ---- what requests ask of their logits: penalties, biases, masks ------------------------------------------------- */
+/* For the rows of a batch of windows (or single tokens), before a step or ot_token_logprobs reads them.  Of row j of sequence b, for
+ * every id v, in this order, in 64 bits and rounded once:
+ *   1. repetition: v occurs in the sequence's history or among the j tokens of its window in front of the row: z = z / repetition[b]
+ *      where z > 0, else z * repetition[b];
+ *   2. n = how often v occurs in the history behind the prompt and among those j tokens:
+ *      z = z - frequency[b] * n - (n > 0 ? presence[b] : 0);
+ *   3. z = z + bias of v (of an id that the list names more than once the last entry counts);
+ *   4. the row's mask leaves v out: z = -inf.
+ * An id at -inf stays there.  What nothing of this names keeps its bits.  A mask that leaves no id makes a row without a distribution.
+ * Ids outside [0, V) in history, window and bias lists are none (so -1 pads them).  A mask_of_row outside [-1, n_masks) makes the
+ * row NaN.  Penalties are finite, repetition above 0.
+ * Without row_off every row is a sequence of its own (B = M).  Rows that no sequence of row_off has are neither read nor written.    */
+typedef struct ot_adjust_in {
+  int32_t         M, V, B;            /* rows; ids per row; sequences                                              */
+  int32_t         dtype;              /* OT_BF16 or OT_F32: type of logits and out                                  */
+  int32_t         n_bias, n_masks;    /* entries of a sequence's bias list; masks                                   */
+  int32_t         reserved[2];        /* must be 0                                                              */
+  int64_t         ld;                 /* elements from a row of logits to the next, at least V                      */
+  int64_t         ld_history;         /* ids from a sequence's history to the next: as many it holds at most         */
+  int64_t         ld_mask;            /* words from a mask to the next, at least ceil(V / 32)                       */
+  const void*     logits;             /* DEVICE, row m at logits + m * ld elements, any alignment of its type       */
+  const int32_t*  row_off;            /* DEVICE [B+1] first rows of the sequences, ascending, or NULL               */
+  const int32_t*  history;            /* DEVICE [B, ld_history] prompt, then output, of each sequence; NULL: none (ld_history = 0) */
+  const int32_t*  n_history;          /* DEVICE [B] their lengths, or NULL: ld_history                              */
+  const int32_t*  n_prompt;           /* DEVICE [B] how many of these are the prompt's, or NULL: 0                  */
+  const int32_t*  window;             /* DEVICE [M] proposed tokens in the layout of ot_step_out.mapped_ids: entry row_off[b] + j is
+                                         sequence b's j-th; NULL: none.  Needs row_off                              */
+  const float    *repetition, *frequency, *presence;   /* DEVICE [B], or NULL: 1, 0, 0                              */
+  const int32_t*  bias_ids;           /* DEVICE [B, n_bias]                                                     */
+  const float*    bias;               /* DEVICE [B, n_bias]; -inf bans an id                                        */
+  const uint32_t* masks;              /* DEVICE, mask i at masks + i * ld_mask: bit v % 32 of word v / 32 set: id v may come */
+  const int32_t*  mask_of_row;        /* DEVICE [M], -1: none; or NULL: row m has mask m (n_masks >= M)             */
+} ot_adjust_in;
+/* out: DEVICE, row m at out + m * ld_out elements, ld_out >= V; it may be the logits themselves (with the same ld: then only what
+ * changes is written), or share no byte with their rows.                                                           */
+int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_out);
+
+/* ---- distillation from a teacher's top logits --------------------------------------------------------------- */
+/* Of every row: a teacher's most likely ids with their log-probabilities (what ot_token_logprobs leaves of its rows, or what was stored
+ * of them), and a student's logits z with q = softmax(z / T).  With p_i = exp(top_logprobs_i), P = sum p_i, and Q = the student's
+ * probability of the ids that are kept:
+ *   OT_REST_DROP         loss = sum p_i (ln p_i - ln q(id_i)):  the kept terms of the teacher's KL divergence
+ *   OT_REST_RENORMALISE  the same with p_i / P
+ *   OT_REST_BUCKET       + (1 - P) (ln(1 - P) - ln(1 - Q)):  what is not kept as one token more (P above 1 by rounding counts as 1)
+ *   - An id of -1 is none, and so is with through_map a target id without a draft id.  A row without ids adds nothing: loss 0, kept 0,
+ *     zero gradient; it is not read.  An id outside [-1, V) (through_map: [-1, V_t)) makes loss, kept and gradient of its row NaN.
+ *   - An id that is named twice has both terms (and counts once in Q).
+ *   - A log-probability of -inf is one of p = 0 and adds no term.  NaN or +inf make the row's loss, kept and gradient NaN.
+ *   - An id that the student masks (-inf) gets a zero gradient; with p above 0 the row's loss is +inf.  A row that the student masks
+ *     whole adds nothing.  A NaN or +inf among a row's logits makes its loss and gradient NaN.
+ *   - temperature is the student's, as in ot_token_logprobs: not above 0 counts as 1, below 2^-126 as that.
+ * Work is enqueued on the context's stream.                                                                     */
+#define OT_MAX_TEACHER_TOP 256
+#define OT_MAX_STUDENT_V (1 << 20)
+#define OT_REST_DROP         0
+#define OT_REST_RENORMALISE  1
+#define OT_REST_BUCKET       2
+typedef struct ot_top_distill_in {
+  int32_t        M, V;                /* rows; ids per row, 1..OT_MAX_STUDENT_V                                     */
+  int32_t        dtype;               /* OT_BF16 or OT_F32: type of the student's logits                            */
+  int32_t        n_top;               /* ids per row, 1..OT_MAX_TEACHER_TOP                                         */
+  int32_t        rest;                /* OT_REST_*                                                              */
+  int32_t        through_map;         /* != 0: top_ids are target ids, the logits the drafter's (V = V_d): each becomes the draft id
+                                         that the context's direct map takes to it                                  */
+  int32_t        B;                   /* sequences, with row_off                                                   */
+  int32_t        reserved;            /* must be 0                                                              */
+  int64_t        ld;                  /* elements from a row of logits to the next, at least V                      */
+  const void*    logits;              /* DEVICE, row m at logits + m * ld elements, any alignment of its type       */
+  const int32_t* top_ids;             /* DEVICE [M, n_top]                                                      */
+  const float*   top_logprobs;        /* DEVICE [M, n_top]                                                      */
+  const float*   temperature;         /* DEVICE [M], or [B] with row_off, or NULL: 1                                */
+  const int32_t* row_off;             /* DEVICE [B+1] first rows of the sequences that the temperatures belong to, or NULL */
+} ot_top_distill_in;
+/* loss: DEVICE [M].  kept: DEVICE [M] or NULL: P of each row.                                                       */
+int ot_top_distill_loss(ot_ctx* ctx, const ot_top_distill_in* in, float* loss, float* kept_or_null);
+/* The same values, and the gradient of sum grad_loss * loss with respect to the student's logits, in their type:
+ *   dz_v = (grad_loss / T) (P q_v - sum of the p_i of v)      OT_REST_BUCKET: q_v - (p_i of v) for kept ids,
+ *                                                             q_v (1 - (1 - P) / (1 - Q)) for the others.
+ * grad_loss: DEVICE [M], or NULL: 1.  grad: DEVICE, row m at grad + m * ld_grad elements, ld_grad >= V, written whole up to V; it may
+ * be the logits themselves (with the same ld), or share no byte with their rows.                                    */
+int ot_top_distill_loss_grad(ot_ctx* ctx, const ot_top_distill_in* in, float* loss, float* kept_or_null, const float* grad_loss_or_null,
+                             void* grad, int64_t ld_grad);
 
 /* ---- adaptive drafting: stop rule and the acceptance head's loss value -------------------------------- */
 /* Section "Online Adaptive Drafting": a head f_phi gives, for proposed token i, the logit of

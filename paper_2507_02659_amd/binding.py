@@ -22,6 +22,9 @@ OT_FLAG_UNMAPPABLE, OT_FLAG_RESID_ZERO, OT_FLAG_BAD_ID = 1, 2, 4
 OT_MAX_NGRAM_LEN, OT_MAX_K = 8, 63
 OT_STATIC_MAX_BATCH = 4096
 OT_MAX_TOP = 64
+OT_MAX_ADAPTER_RANK = 256
+OT_MAX_TEACHER_TOP, OT_MAX_STUDENT_V = 256, 1 << 20
+OT_REST_DROP, OT_REST_RENORMALISE, OT_REST_BUCKET = 0, 1, 2
 OT_N_STAGES = 4
 STAGE_NAMES = ("lm_head", "softmax_stats", "translate_accept", "residual_draw")
 
@@ -35,6 +38,7 @@ EXPORTS = (
     "ot_verify_init", "ot_verify_init_quantized", "ot_verify_destroy", "ot_lm_head", "ot_ngram_cache_build", "ot_ngram_cache_create", "ot_ngram_cache_insert",
     "ot_ngram_cache_size", "ot_ngram_cache_export", "ot_ngram_cache_import", "ot_ngram_cache_destroy", "ot_verify_step",
     "ot_verify_step_from_logits", "ot_distill_loss", "ot_distill_loss_grad", "ot_token_logprobs", "ot_token_logprobs_grad",
+    "ot_adapter_logits", "ot_adjust_logits", "ot_top_distill_loss", "ot_top_distill_loss_grad",
     "ot_adaptive_drafting", "ot_adaptive_drafting_static", "ot_verify_workspace", "ot_verify_structure",
     "ot_verify_profile",
     "ot_verify_profile_read", "ot_last_error", "ot_version",
@@ -100,6 +104,28 @@ LOGPROB_OUT = ("logprob", "entropy", "row_max", "row_sumexp", "top_logprobs", "t
 
 class ot_logprob_out(C.Structure):
     _fields_ = [(n, C.c_void_p) for n in LOGPROB_OUT]
+
+
+class ot_adapter_in(C.Structure):
+    _fields_ = [("M", C.c_int32), ("d", C.c_int32), ("V", C.c_int32), ("rank", C.c_int32), ("n_adapters", C.c_int32), ("dtype", C.c_int32),
+                ("logits_dtype", C.c_int32), ("reserved", C.c_int32), ("ld", C.c_int64), ("hidden", C.c_void_p), ("down", C.c_void_p),
+                ("up", C.c_void_p), ("scale", C.c_void_p), ("adapter", C.c_void_p), ("logits", C.c_void_p)]
+
+
+ADJUST_ARRAYS = ("logits", "row_off", "history", "n_history", "n_prompt", "window", "repetition", "frequency", "presence", "bias_ids", "bias",
+                 "masks", "mask_of_row")
+
+
+class ot_adjust_in(C.Structure):
+    _fields_ = [("M", C.c_int32), ("V", C.c_int32), ("B", C.c_int32), ("dtype", C.c_int32), ("n_bias", C.c_int32), ("n_masks", C.c_int32),
+                ("reserved", C.c_int32 * 2), ("ld", C.c_int64), ("ld_history", C.c_int64), ("ld_mask", C.c_int64)] + \
+               [(n, C.c_void_p) for n in ADJUST_ARRAYS]
+
+
+class ot_top_distill_in(C.Structure):
+    _fields_ = [("M", C.c_int32), ("V", C.c_int32), ("dtype", C.c_int32), ("n_top", C.c_int32), ("rest", C.c_int32), ("through_map", C.c_int32),
+                ("B", C.c_int32), ("reserved", C.c_int32), ("ld", C.c_int64), ("logits", C.c_void_p), ("top_ids", C.c_void_p),
+                ("top_logprobs", C.c_void_p), ("temperature", C.c_void_p), ("row_off", C.c_void_p)]
 
 
 class ot_adapt_in(C.Structure):
@@ -169,6 +195,14 @@ def load_library() -> C.CDLL:
     lib.ot_token_logprobs_grad.argtypes = [C.c_void_p, C.POINTER(ot_logprob_in), C.POINTER(ot_logprob_out), C.c_void_p, C.c_void_p,
                                            C.c_void_p, C.c_int64]
     lib.ot_token_logprobs_grad.restype = C.c_int
+    lib.ot_adapter_logits.argtypes = [C.c_void_p, C.POINTER(ot_adapter_in), C.c_void_p, C.c_int64]
+    lib.ot_adapter_logits.restype = C.c_int
+    lib.ot_adjust_logits.argtypes = [C.c_void_p, C.POINTER(ot_adjust_in), C.c_void_p, C.c_int64]
+    lib.ot_adjust_logits.restype = C.c_int
+    lib.ot_top_distill_loss.argtypes = [C.c_void_p, C.POINTER(ot_top_distill_in), C.c_void_p, C.c_void_p]
+    lib.ot_top_distill_loss.restype = C.c_int
+    lib.ot_top_distill_loss_grad.argtypes = [C.c_void_p, C.POINTER(ot_top_distill_in), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int64]
+    lib.ot_top_distill_loss_grad.restype = C.c_int
     lib.ot_adaptive_drafting.argtypes = [C.c_void_p, C.POINTER(ot_adapt_in), C.POINTER(ot_adapt_out)]
     lib.ot_adaptive_drafting.restype = C.c_int
     lib.ot_adaptive_drafting_static.argtypes = [C.POINTER(ot_adapt_in), C.POINTER(ot_adapt_out), C.c_void_p]
@@ -374,6 +408,41 @@ def ot_token_logprobs(ctx, given: ot_logprob_in, out: ot_logprob_out):
 def ot_token_logprobs_grad(ctx, given: ot_logprob_in, forward: ot_logprob_out, grad_logprob, grad_entropy, grad, ld_grad: int):
     _check(load_library().ot_token_logprobs_grad(ctx, C.byref(given), C.byref(forward), _on_gpu(grad_logprob), _on_gpu(grad_entropy),
                                                  _on_gpu(grad), ld_grad))
+
+
+def make_adapter_in(*, M, d, V, rank, n_adapters, dtype, hidden, down, up, adapter, scale=None, logits=None, logits_dtype=OT_F32, ld=0,
+                    reserved=0) -> ot_adapter_in:
+    return ot_adapter_in(M, d, V, rank, n_adapters, dtype, logits_dtype, reserved, ld, _on_gpu(hidden), _on_gpu(down), _on_gpu(up), _on_gpu(scale),
+                         _on_gpu(adapter), _on_gpu(logits))
+
+
+def ot_adapter_logits(ctx, given: ot_adapter_in, out, ld_out: int):
+    """out: device tensor or address; rows may be ld_out elements apart (a tensor that is not contiguous: pass its address)."""
+    _check(load_library().ot_adapter_logits(ctx, C.byref(given), _on_gpu(out), ld_out))
+
+
+def make_adjust_in(*, M, V, B, dtype, ld, n_bias=0, n_masks=0, ld_history=0, ld_mask=0, reserved=(0, 0), **arrays) -> ot_adjust_in:
+    """arrays: name -> device tensor/address for the pointers of ot_adjust_in (those not wanted may be absent)."""
+    return ot_adjust_in(M, V, B, dtype, n_bias, n_masks, (C.c_int32 * 2)(*reserved), ld, ld_history, ld_mask,
+                        *[_on_gpu(arrays.get(n)) for n in ADJUST_ARRAYS])
+
+
+def ot_adjust_logits(ctx, given: ot_adjust_in, out, ld_out: int):
+    _check(load_library().ot_adjust_logits(ctx, C.byref(given), _on_gpu(out), ld_out))
+
+
+def make_top_distill_in(*, M, V, dtype, n_top, logits, ld, top_ids, top_logprobs, rest=OT_REST_DROP, through_map=False, temperature=None,
+                        row_off=None, B=0, reserved=0) -> ot_top_distill_in:
+    return ot_top_distill_in(M, V, dtype, n_top, rest, 1 if through_map else 0, B, reserved, ld, _on_gpu(logits), _on_gpu(top_ids),
+                             _on_gpu(top_logprobs), _on_gpu(temperature), _on_gpu(row_off))
+
+
+def ot_top_distill_loss(ctx, given: ot_top_distill_in, loss, kept=None):
+    _check(load_library().ot_top_distill_loss(ctx, C.byref(given), _on_gpu(loss), _on_gpu(kept)))
+
+
+def ot_top_distill_loss_grad(ctx, given: ot_top_distill_in, loss, kept, grad_loss, grad, ld_grad: int):
+    _check(load_library().ot_top_distill_loss_grad(ctx, C.byref(given), _on_gpu(loss), _on_gpu(kept), _on_gpu(grad_loss), _on_gpu(grad), ld_grad))
 
 
 def ot_adaptive_drafting(ctx, *, B, gamma, w_accept=1.0, w_reject=1.0, row_off, row_off_host, head_logits, labels=None,

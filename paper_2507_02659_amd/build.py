@@ -17,7 +17,7 @@ CSRC = os.path.join(PKG, "csrc")
 OUT_DIR = os.path.join(PKG, "_build")
 LIB_PATH = os.path.join(PKG, "libotverify.so")
 SOURCES = ["api.hip", "cache.hip", "ngram_table.cpp", "lmhead.hip", "stats.hip", "resid.hip", "loss.hip", "loss_grad.hip",
-           "logprobs.hip", "qhead.hip", "adapt.hip"]
+           "logprobs.hip", "qhead.hip", "adapt.hip", "adapters.hip", "adjust.hip", "top_distill.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -39,6 +39,15 @@ int ot_check_device(const ot_ctx* ctx, const char* who) {
   return OT_OK;
 }
 
+bool ot_rows_overlap(const void* from_rows, int64_t ld_from, const void* to_rows, int64_t ld_to, int64_t M, int64_t V, int64_t size) {
+  const int64_t row = V * size, step = ld_from * size;
+  const uintptr_t from = reinterpret_cast<uintptr_t>(from_rows), to = reinterpret_cast<uintptr_t>(to_rows);
+  if (to == from || to >= from + (uintptr_t)((M - 1) * step + row) || from >= to + (uintptr_t)((M - 1) * ld_to * size + row)) return false;
+  if (ld_to != ld_from) return true;
+  const int64_t apart = (int64_t)(to > from ? (to - from) % (uintptr_t)step : step - (int64_t)((from - to) % (uintptr_t)step));
+  return apart < row || apart > step - row;              // (a row's end, and the next row's start)
+}
+
 #define fail ot_fail
 #define fail_hip ot_fail_hip
 
@@ -168,6 +177,7 @@ static int init_impl(const char* who, const ot_verify_config* cfg, const ot_quan
   c->grad_rows = grad_rows;
   ok = ok && dev_alloc(c, &lp_part, kLogprobSegments * logprob_segment_bytes());
   c->lp_part = lp_part;
+  ok = ok && dev_alloc(c, &c->adapter_u, (size_t)kAdapterRows * OT_MAX_ADAPTER_RANK * 6);
   const size_t n_counters = 1 + (R + 1) + kLogprobSegments + 2;   // of adaptive drafting, the loss, the log-probabilities, the gradient
   ok = ok && dev_alloc(c, &c->counters, n_counters);
   if (!ok) { free_ctx(c); return fail(OT_ERR_NOMEM, "%s: device allocation failed", who); }

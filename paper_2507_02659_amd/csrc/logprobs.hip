@@ -9,12 +9,10 @@
 
 #include "device_math.h"
 #include "otv_host.h"
+#include "rows.h"
 
 namespace otv {
 namespace {
-
-constexpr float kLog2e = 1.4426950408889634f;
-constexpr float kNan = __builtin_nanf("");
 
 struct LogprobArgs {
   ot_logprob_in in;
@@ -24,11 +22,8 @@ struct LogprobArgs {
 __device__ inline const void* row_of(const ot_logprob_in& in, int64_t row) {
   return static_cast<const char*>(in.logits) + row * in.ld * (in.dtype == OT_BF16 ? 2 : 4);
 }
-// Temperature of a row, of which log2(e) / T is finite; by a whole wavefront.
 __device__ inline float row_temperature(const ot_logprob_in& in, int row, int lane) {
-  if (!in.temperature) return 1.f;
-  const float T = in.temperature[in.row_off ? find_sequence(in.row_off, in.B, row, 0, lane) : row];
-  return T > 0.f ? fmaxf(T, 0x1p-126f) : 1.f;
+  return otv::row_temperature(in.temperature, in.row_off, in.B, row, lane);
 }
 __device__ inline bool any_given(const ot_logprob_in& in, int64_t row) {
   for (int i = 0; i < in.n_tok; ++i)
@@ -129,33 +124,6 @@ struct Segment {
   float mx, pad;
   key_t top[OT_MAX_TOP];
 };
-
-template <typename T> struct Vec;
-template <> struct Vec<float> {
-  static constexpr int kElems = 4;
-  typedef float Raw __attribute__((ext_vector_type(4)));
-  __device__ static void unpack(const Raw& x, float* v) { v[0] = x.x; v[1] = x.y; v[2] = x.z; v[3] = x.w; }
-  __device__ static float one(const float* p) { return *p; }
-};
-template <> struct Vec<uint16_t> {
-  static constexpr int kElems = 8;
-  typedef uint32_t Raw __attribute__((ext_vector_type(4)));
-  __device__ static void unpack(const Raw& x, float* v) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(x[i] << 16);
-      v[2 * i + 1] = __uint_as_float(x[i] & 0xFFFF0000u);
-    }
-  }
-  __device__ static float one(const uint16_t* p) { return bf16_to_f32(*p); }
-};
-
-// Sum of n values, the deepest of them log2 n additions deep.
-template <int n>
-__device__ inline float tree_sum(const float* x) {
-  if constexpr (n == 1) return x[0];
-  else return tree_sum<n / 2>(x) + tree_sum<n - n / 2>(x + n / 2);
-}
 
 // kPer logits per lane into the lane's running sums (-inf: none); returns the largest.  The sums' reference is one for the wavefront and
 // moves, in 64 bits, only when a logit is more than 4 above it in the exponent: with a lane's own maximum for it nearly every tile moved one
@@ -422,22 +390,6 @@ struct LogprobGradArgs {
   int64_t ld_grad;
 };
 
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-typedef float f32x2 __attribute__((ext_vector_type(2)));
-__device__ inline void store_one(float* p, float x) { *p = x; }
-__device__ inline void store_one(uint16_t* p, float x) { *reinterpret_cast<__bf16*>(p) = (__bf16)x; }   // to nearest
-__device__ inline void store_vec(float* p, const float* x) {
-  typedef float raw_t __attribute__((ext_vector_type(4)));
-  __builtin_nontemporal_store(raw_t{x[0], x[1], x[2], x[3]}, reinterpret_cast<raw_t*>(p));
-}
-__device__ inline void store_vec(uint16_t* p, const float* x) {
-  typedef uint32_t raw_t __attribute__((ext_vector_type(4)));
-  raw_t r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{x[2 * i], x[2 * i + 1]}, bf16x2));
-  __builtin_nontemporal_store(r, reinterpret_cast<raw_t*>(p));
-}
-
 // Grid = chunks x rows: four vectors of logits per thread, all asked for at once, whole where the rows of the logits and of the gradient start
 // at the same place of a 16-byte unit, else one by one.  Bound by memory: a logit is read once, a gradient written once (512 x 128256
 // float32 91.7 us, 5.7 TB/s; a copy of the logits takes 98).  Two vectors per thread: bf16 66 us instead of 48; eight: float32 170.
@@ -569,16 +521,6 @@ int check_in(const ot_ctx* ctx, const ot_logprob_in* in, const char* who) {
   return ot_check_device(ctx, who);
 }
 
-// Whether rows of the gradient share memory with rows of the logits and are not those rows themselves.
-bool overlaps(const ot_logprob_in& in, const void* grad, int64_t ld_grad) {
-  const int64_t size = in.dtype == OT_BF16 ? 2 : 4, row = in.V * size, step = in.ld * size;
-  const uintptr_t from = reinterpret_cast<uintptr_t>(in.logits), to = reinterpret_cast<uintptr_t>(grad);
-  if (to == from || to >= from + (uintptr_t)((in.M - 1) * step + row) || from >= to + (uintptr_t)((in.M - 1) * ld_grad * size + row)) return false;
-  if (ld_grad != in.ld) return true;
-  const int64_t apart = (int64_t)(to > from ? (to - from) % (uintptr_t)step : step - (int64_t)((from - to) % (uintptr_t)step));
-  return apart < row || apart > step - row;              // (a row's end, and the next row's start)
-}
-
 }  // namespace
 
 size_t logprob_segment_bytes() { return sizeof(Segment); }
@@ -614,7 +556,7 @@ int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logpro
   if (reinterpret_cast<uintptr_t>(grad) % (in->dtype == OT_BF16 ? 2 : 4))
     return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: grad is not aligned to its type");
   if (grad == in->logits && ld_grad != in->ld) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: in place, ld_grad must be ld");
-  if (overlaps(*in, grad, ld_grad)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: rows of grad overlap other places of the logits' rows");
+  if (ot_rows_overlap(in->logits, in->ld, grad, ld_grad, in->M, in->V, in->dtype == OT_BF16 ? 2 : 4)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: rows of grad overlap other places of the logits' rows");
   const int chunks = ceil_div((int64_t)in->V + 7, in->dtype == OT_BF16 ? kGradChunk<uint16_t> : kGradChunk<float>);   // a row starts up to 7 elements into its first vector
   if (!grid_fits((int64_t)chunks * in->M, 256)) return ot_fail(OT_ERR_SHAPE, "ot_token_logprobs_grad: %d rows of %d ids are too many for a launch", in->M, in->V);
   const LogprobGradArgs a{*in, fwd->row_max, fwd->row_sumexp, fwd->entropy, grad_logprob, grad_entropy, grad, ld_grad};

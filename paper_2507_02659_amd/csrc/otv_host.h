@@ -14,6 +14,10 @@ int ot_static_scratch_prepare();
 // OT_OK if the context's device is the current one, else OT_ERR_CTX_MISMATCH with a message that names `who`.
 int ot_check_device(const struct ot_ctx* ctx, const char* who);
 
+// Whether M rows of V elements of `size` bytes that lie ld_to elements apart share memory with rows that lie ld_from apart, and are not those
+// rows themselves.
+bool ot_rows_overlap(const void* from_rows, int64_t ld_from, const void* to_rows, int64_t ld_to, int64_t M, int64_t V, int64_t size);
+
 struct ot_ctx {
   int32_t d = 0, V_t = 0, V_d = 0, max_batch = 0, max_k = 0, dtype = 0, max_ngram_len = 0, draft_side = 0;
   int32_t max_rows = 0, max_K = 0, Kp = 0, Vp = 0, ncht = 0, nchd = 0, max_units = 0;
@@ -51,6 +55,7 @@ struct ot_ctx {
   double* adapt_part = nullptr;       // [max_batch, 2] per-sequence partials of the acceptance head's loss
   void* lp_part = nullptr;            // [kLogprobSegments] what the workgroups of a row of log-probabilities hand to the last of them
   int32_t* lp_count = nullptr;        // [kLogprobSegments] their arrival counters, 0 between launches
+  uint8_t* adapter_u = nullptr;       // [kAdapterRows, OT_MAX_ADAPTER_RANK] of 6 bytes: hidden rows through their adapters' first matrix
   // profiling
   bool profiling = false;
   std::vector<hipEvent_t> events;   // OT_N_STAGES + 1 per pending step

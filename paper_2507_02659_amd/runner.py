@@ -56,6 +56,25 @@ class QuantWeights:
             raise TypeError("zeros are uint8")
 
 
+@dataclass
+class Adapters:
+    """Low-rank adapters of a head as device tensors: adapter a adds scale[a] * (hidden @ down[a].T) @ up[a].T to the logits."""
+
+    down: torch.Tensor                              # bfloat16 or float32 [n, rank, d]
+    up: torch.Tensor                                # the same type [n, V, rank]
+    scale: Optional[torch.Tensor] = None            # float32 [n]; None: 1
+
+    def check(self):
+        if self.down.dtype not in (torch.bfloat16, torch.float32) or self.up.dtype != self.down.dtype:
+            raise TypeError("adapters are bfloat16 or float32, both matrices alike")
+        if self.down.dim() != 3 or self.up.dim() != 3 or self.up.shape[0] != self.down.shape[0] or self.up.shape[2] != self.down.shape[1]:
+            raise ValueError(f"adapters are [n, rank, d] and [n, V, rank], not {tuple(self.down.shape)} and {tuple(self.up.shape)}")
+        if not self.down.is_contiguous() or not self.up.is_contiguous():
+            raise ValueError("adapters are contiguous")
+        if self.scale is not None and (self.scale.dtype != torch.float32 or tuple(self.scale.shape) != (self.down.shape[0],) or not self.scale.is_contiguous()):
+            raise ValueError(f"scale is float32 [{self.down.shape[0]}]")
+
+
 class Verifier:
     """One library context plus (optionally) one n-gram cache, for batches of a fixed model shape.
 
@@ -260,8 +279,13 @@ class Verifier:
                 if self.stream is not None:
                     t.record_stream(self.stream)
 
-    def lm_head(self, hidden: torch.Tensor) -> torch.Tensor:
-        """Logits [M, V_t] (float32) of hidden rows [M, d] through the verifier's head (ot_lm_head)."""
+    def lm_head(self, hidden: torch.Tensor, *, adapters: Optional[Adapters] = None, adapter_of_row: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Logits [M, V_t] (float32) of hidden rows [M, d] through the verifier's head (ot_lm_head), and with adapters what each row's adds to
+        them (adapter_logits)."""
+        if adapters is not None and (adapters.up.dim() != 3 or adapters.up.shape[1] != self.V_t):
+            raise ValueError(f"the head's adapters are [n, rank, {self.d}] and [n, {self.V_t}, rank]")
+        if (adapters is None) != (adapter_of_row is None):
+            raise ValueError("adapters and adapter_of_row come together")
         if hidden.dtype != self._type() or hidden.dim() != 2 or hidden.shape[1] != self.d:
             raise ValueError(f"hidden rows are [M, {self.d}] of the verifier's type, not {tuple(hidden.shape)} {hidden.dtype}")
         if self.stream is not None or hidden.device != self.device:
@@ -269,7 +293,98 @@ class Verifier:
         M = hidden.shape[0]
         logits = self._empty((M, self.V_t), torch.float32)
         ot.ot_lm_head(self.ctx, M, hidden, logits, self.V_t)
-        return logits
+        return logits if adapters is None else self.adapter_logits(hidden, adapters, adapter_of_row, logits, out=logits)
+
+    def _rows(self, name, logits):
+        """Type, rows, ids and distance of rows of logits."""
+        M, V = logits.shape
+        if logits.dtype not in (torch.bfloat16, torch.float32) or (V > 1 and logits.stride(1) != 1):
+            raise ValueError(f"{name} are [M, V] bfloat16 or float32 with neighbouring ids next to each other")
+        return ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, M, V, logits.stride(0) if M > 1 else V
+
+    def _array(self, name, t, dtype, shape):
+        """Address of an argument that is an array of this type and shape, or None."""
+        if t is None:
+            return None
+        if t.dtype != dtype or t.shape != shape or not t.is_contiguous():
+            raise ValueError(f"{name} is {dtype} {list(shape)}, contiguous, not {t.dtype} {list(t.shape)}")
+        if self.stream is not None or t.device != self.device:
+            self._here(**{name: t})
+        return t.data_ptr()
+
+    def adapter_logits(self, hidden: torch.Tensor, adapters: Adapters, adapter_of_row: torch.Tensor, logits: Optional[torch.Tensor] = None, *,
+                       out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Rows of logits [M, V] plus what each row's adapter makes of its hidden row [M, d] (ot_adapter_logits); without logits that alone, in
+        float32.  adapter_of_row: int32 [M], -1: none.  out: where to, shaped and typed like the logits (these themselves: in place)."""
+        adapters.check()
+        n, rank, d = adapters.down.shape
+        V = adapters.up.shape[1]
+        if hidden.dim() != 2 or hidden.shape[1] != d or hidden.dtype != adapters.down.dtype or not hidden.is_contiguous():
+            raise ValueError(f"hidden rows are [M, {d}] of the adapters' type, contiguous, not {tuple(hidden.shape)} {hidden.dtype}")
+        M = hidden.shape[0]
+        if logits is not None and tuple(logits.shape) != (M, V):
+            raise ValueError(f"logits are [{M}, {V}], not {tuple(logits.shape)}")
+        code, _, _, ld = (ot.OT_F32, M, V, 0) if logits is None else self._rows("logits", logits)
+        out, ld_out = self._out(out, (M, V), torch.float32 if logits is None else logits.dtype)
+        dev = self.device
+        if self.stream is not None or hidden.device != dev or adapters.down.device != dev or adapters.up.device != dev or (logits is not None and logits.device != dev):
+            self._here(hidden=hidden, down=adapters.down, up=adapters.up, logits=logits)
+        given = ot.ot_adapter_in(M, d, V, rank, n, ot.OT_BF16 if hidden.dtype == torch.bfloat16 else ot.OT_F32, code, 0, ld, hidden.data_ptr(),
+                                 adapters.down.data_ptr(), adapters.up.data_ptr(), self._array("scale", adapters.scale, torch.float32, (n,)),
+                                 self._array("adapter_of_row", adapter_of_row, torch.int32, (M,)), None if logits is None else logits.data_ptr())
+        ot.ot_adapter_logits(self.ctx, given, out.data_ptr(), ld_out)
+        return out
+
+    def _out(self, out, shape, dtype):
+        """The given output, or a new one, and the distance of its rows."""
+        if out is None:
+            return self._empty(shape, dtype), shape[1]
+        if tuple(out.shape) != tuple(shape) or out.dtype != dtype or (shape[1] > 1 and out.stride(1) != 1) or (shape[0] > 1 and out.stride(0) < shape[1]):
+            raise ValueError(f"out is {list(shape)} {dtype} with neighbouring ids next to each other")
+        if self.stream is not None or out.device != self.device:
+            self._here(out=out)
+        return out, out.stride(0) if shape[0] > 1 else shape[1]
+
+    def adjust_logits(self, logits: torch.Tensor, *, row_off: Optional[torch.Tensor] = None, history: Optional[torch.Tensor] = None,
+                      n_history: Optional[torch.Tensor] = None, n_prompt: Optional[torch.Tensor] = None, window: Optional[torch.Tensor] = None,
+                      repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
+                      bias_ids: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, masks: Optional[torch.Tensor] = None,
+                      mask_of_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
+        """Penalties for repeated tokens, biases and masks on rows of logits [M, V] (ot_adjust_logits), in 64 bits and rounded once.
+
+        row_off: int32 [B + 1] first rows of the sequences (None: every row is one).  history: int32 [B, L], the first n_history of a row count
+        (int32 [B]; None: all) and of these the first n_prompt are its prompt (int32 [B]; None: none).  window: int32 [M] proposed tokens (a step's
+        mapped_ids), those in front of a row count for it.  repetition, frequency, presence: float32 [B].  bias_ids, bias: int32 and float32 [B, n].
+        masks: int32 [n, words], bit v % 32 of word v / 32 set where id v may come; mask_of_row: int32 [M], -1: none (None: row m has mask m).
+        Ids outside the vocabulary are none.  out: where to (None: new; the logits themselves: in place)."""
+        code, M, V, ld = self._rows("logits", logits)
+        B = M if row_off is None else max(0, row_off.numel() - 1)
+        out, ld_out = self._out(out, (M, V), logits.dtype)
+        if self.stream is not None or logits.device != self.device:
+            self._here(logits=logits)
+        L = n_bias = n_masks = words = 0
+        if history is not None:
+            if history.dim() != 2:
+                raise ValueError(f"history is int32 [{B}, L]")
+            L = history.shape[1]
+        if bias_ids is not None or bias is not None:
+            if bias_ids is None or bias is None or bias_ids.dim() != 2:
+                raise ValueError(f"bias_ids and bias come together, [{B}, n]")
+            n_bias = bias_ids.shape[1]
+        if masks is not None:
+            if masks.dim() != 2 or masks.shape[1] < (V + 31) // 32:
+                raise ValueError(f"masks are int32 [n, at least {(V + 31) // 32}]")
+            n_masks, words = masks.shape
+            if mask_of_row is None and n_masks < M:
+                raise ValueError(f"without mask_of_row every row has its own mask ({n_masks} for {M} rows)")
+        i32, f32, at = torch.int32, torch.float32, self._array
+        given = ot.ot_adjust_in(M, V, B, code, n_bias, n_masks, (C.c_int32 * 2)(), ld, L, words, logits.data_ptr(), at("row_off", row_off, i32, (B + 1,)),
+                                at("history", history, i32, (B, L)), at("n_history", n_history, i32, (B,)), at("n_prompt", n_prompt, i32, (B,)),
+                                at("window", window, i32, (M,)), at("repetition", repetition, f32, (B,)), at("frequency", frequency, f32, (B,)),
+                                at("presence", presence, f32, (B,)), at("bias_ids", bias_ids, i32, (B, n_bias)), at("bias", bias, f32, (B, n_bias)),
+                                at("masks", masks, i32, (n_masks, words)), at("mask_of_row", mask_of_row, i32, (M,)))
+        ot.ot_adjust_logits(self.ctx, given, out.data_ptr(), ld_out)
+        return out
 
     def _logprob_in(self, logits, tokens, temperature, row_off, n_top, given_rows_only):
         M, V = logits.shape
@@ -345,6 +460,43 @@ class Verifier:
         grad = self._empty(logits.shape, logits.dtype)
         ot.ot_token_logprobs_grad(self.ctx, given, stats, grad_logprob, grad_entropy, grad, given.V)
         return grad
+
+    def _top_distill_in(self, logits, top_ids, top_logprobs, rest, temperature, row_off, through_map):
+        code, M, V, ld = self._rows("logits", logits)
+        if top_ids.dim() != 2 or top_ids.shape[0] != M or top_ids.shape != top_logprobs.shape:
+            raise ValueError(f"top_ids and top_logprobs are [{M}, n]")
+        if through_map and V != self.V_d:
+            raise ValueError(f"through the direct map the logits are the drafter's, [M, {self.V_d}]")
+        B = M if row_off is None else max(0, row_off.numel() - 1)
+        if self.stream is not None or logits.device != self.device:
+            self._here(logits=logits)
+        shape, at = tuple(top_ids.shape), self._array
+        return ot.ot_top_distill_in(M, V, code, shape[1], rest, 1 if through_map else 0, B, 0, ld, logits.data_ptr(), at("top_ids", top_ids, torch.int32, shape),
+                                    at("top_logprobs", top_logprobs, torch.float32, shape), at("temperature", temperature, torch.float32, (B,)),
+                                    at("row_off", row_off, torch.int32, (B + 1,)))
+
+    def top_distill_loss(self, logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, *, rest: int = ot.OT_REST_DROP,
+                         temperature: Optional[torch.Tensor] = None, row_off: Optional[torch.Tensor] = None, through_map: bool = False) -> dict:
+        """Distillation loss of rows of a student's logits [M, V] against a teacher's most likely ids (int32 [M, n], -1: none) and their
+        log-probabilities (float32 [M, n]), as token_logprobs leaves them (ot_top_distill_loss).  rest: OT_REST_*, what becomes of the teacher's
+        probability of the other ids.  temperature: the student's, one per row, or per sequence of row_off.  through_map: the ids are the target's and
+        become draft ids by the verifier's direct map.  Returns device tensors [M]: loss, and kept, the probability that the teacher's ids have."""
+        given = self._top_distill_in(logits, top_ids, top_logprobs, rest, temperature, row_off, through_map)
+        out = {"loss": self._empty((given.M,), torch.float32), "kept": self._empty((given.M,), torch.float32)}
+        ot.ot_top_distill_loss(self.ctx, given, out["loss"], out["kept"])
+        return out
+
+    def top_distill_loss_grad(self, logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, *, rest: int = ot.OT_REST_DROP,
+                              temperature: Optional[torch.Tensor] = None, row_off: Optional[torch.Tensor] = None, through_map: bool = False,
+                              grad_loss: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> dict:
+        """top_distill_loss, and "grad": the gradient of sum grad_loss * loss (float32 [M]; None: 1) with respect to the logits, in their type
+        (ot_top_distill_loss_grad).  out: where the gradient goes (None: new; the logits themselves: in place)."""
+        given = self._top_distill_in(logits, top_ids, top_logprobs, rest, temperature, row_off, through_map)
+        grad, ld_grad = self._out(out, tuple(logits.shape), logits.dtype)
+        at = self._array("grad_loss", grad_loss, torch.float32, (given.M,))
+        got = {"loss": self._empty((given.M,), torch.float32), "kept": self._empty((given.M,), torch.float32), "grad": grad}
+        ot.ot_top_distill_loss_grad(self.ctx, given, got["loss"], got["kept"], at, grad.data_ptr(), ld_grad)
+        return got
 
     def step_logprobs(self, inp: dict, *, from_logits: bool = False, n_top: int = 0, at_temperature: bool = True) -> dict:
         """Log-probabilities of the tokens that the last step on `inp` emitted, with entropy and alternatives, from the logits it left
