@@ -24,22 +24,7 @@ struct AdapterArgs {
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
-// four neighbouring logits, from any element on
-typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));
-typedef uint16_t u16x4_any __attribute__((ext_vector_type(4), aligned(2)));
-
-__device__ inline f32x4 load4(const float* p) { return __builtin_nontemporal_load(reinterpret_cast<const f32x4_any*>(p)); }
-__device__ inline f32x4 load4(const uint16_t* p) {
-  const u16x4_any x = __builtin_nontemporal_load(reinterpret_cast<const u16x4_any*>(p));
-  return f32x4{bf16_to_f32(x.x), bf16_to_f32(x.y), bf16_to_f32(x.z), bf16_to_f32(x.w)};
-}
-__device__ inline void store4(float* p, f32x4 x) { __builtin_nontemporal_store(f32x4_any(x), reinterpret_cast<f32x4_any*>(p)); }
-__device__ inline void store4(uint16_t* p, f32x4 x) {
-  u16x4_any r;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint16_t, (__bf16)x[i]);
-  __builtin_nontemporal_store(r, reinterpret_cast<u16x4_any*>(p));
-}
+typedef float f32x4_any __attribute__((ext_vector_type(4), aligned(4)));   // from any element on
 
 // Operands of the matrix instructions: of 16 rows (lane & 15) the kDepth products' indices from k0 on, those past K as 0.  Which of the block's
 // indices a lane's element stands for is the same on both sides, so any order will do.
@@ -104,7 +89,7 @@ struct Block {
 
 // Grid = blocks of 64 rows x 16s of the rank x kSlots.  A workgroup takes every kSlots-th tile of its block; its 16 wavefronts share the hidden
 // indices and add their sums in LDS, in one order.
-constexpr int kDownWaves = 16;
+constexpr int kDownWaves = 16, kDownSteps = 4;
 template <typename W>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterArgs a, int slots) {
   typedef Operand<W> Op;
@@ -124,8 +109,17 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
       const W* hidden = static_cast<const W*>(in.hidden) + (int64_t)(a.row0 + m) * in.d;
       const int K = r < in.rank ? in.d : 0;
       f32x4 sum{};
-      for (int k0 = wave * Op::kDepth; k0 < in.d; k0 += kDownWaves * Op::kDepth)
-        sum = Op::product(Op::load(down, k0, K, lane), Op::load(hidden, k0, in.d, lane), sum);
+      for (int k0 = wave * Op::kDepth; k0 < in.d; k0 += kDownSteps * kDownWaves * Op::kDepth) {
+        typename Op::Frag x[kDownSteps], y[kDownSteps];
+#pragma unroll
+        for (int i = 0; i < kDownSteps; ++i) {
+          const int k = k0 + i * kDownWaves * Op::kDepth;
+          x[i] = Op::load(down, k, K, lane);
+          y[i] = Op::load(hidden, k, in.d, lane);
+        }
+#pragma unroll
+        for (int i = 0; i < kDownSteps; ++i) sum = Op::product(x[i], y[i], sum);
+      }
       // lane: of row (lane & 15) the ranks (lane >> 4) * 4 ..
 #pragma unroll
       for (int i = 0; i < 4; ++i) s_part[wave][lane * 4 + i] = sum[i];
@@ -156,104 +150,204 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
   }
 }
 
-// Grid = strips of 256 ids x blocks of 64 rows; a wavefront has 64 ids of all of the block's rows.  The matrix of the ids is the first operand, so
-// that a lane ends up with four neighbouring ids of one row.
+// Grid = strips of ids x blocks of 64 rows.  A tile's sums are formed with the matrix of the ids as the first operand, 64 ids a wavefront, and go
+// through LDS to the logits, which a wavefront reads and writes row by row in whole 16-byte vectors, wherever the row starts: a strip has the
+// vectors that begin in its kStride ids, and computes the kVec - 1 ids more that the last of them may reach.  In LDS a row is shifted so that
+// its vectors are whole there too.  The next tile's logits are on their way while one is taken.
+constexpr int kUpWaves = 8, kStrip = 64 * kUpWaves, kFront = 8;
+constexpr int kPitch = kStrip + kFront + 4;              // four rows on another quarter of the 64 banks than the next four
+template <typename T>
+constexpr int kStride = kStrip - Vec<T>::kElems;
 template <typename W, typename T, int kBlocks>
-__global__ __launch_bounds__(256) void adapter_up_kernel(AdapterArgs a, int strips) {
+__global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_up_kernel(AdapterArgs a, int strips) {
   typedef Operand<W> Op;
   typedef typename Op::Frag Frag;
-  constexpr int kParts = sizeof(W) == 2 ? 3 : 1;
+  typedef typename Vec<T>::Raw Raw;
+  constexpr int kParts = sizeof(W) == 2 ? 3 : 1, kVec = Vec<T>::kElems, kTurns = kStrip / (64 * kVec), kRows = 16 / kUpWaves;
+  constexpr bool kLargest = kBlocks == 4;
   const ot_adapter_in& in = a.in;
   const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int strip = (int)(blockIdx.x % (unsigned)strips), block = (int)(blockIdx.x / (unsigned)strips);
-  const int v0 = strip * 256 + wave * 64;
-  if (v0 >= in.V) return;
+  __shared__ float s_sum[2][16][kPitch];
+  const int v0 = strip * kStride<T>, own = wave * 64;
+  const bool edges = strip == 0 || v0 + kStrip >= in.V;
+  const int row_at = a.row0 + block * 64;                // first row of the block
+  auto out_of = [&](int row) { return static_cast<T*>(a.out) + (row_at + (int64_t)row) * a.ld_out; };
+  auto logits_of = [&](int row) { return in.logits ? static_cast<const T*>(in.logits) + (row_at + (int64_t)row) * in.ld : nullptr; };
+  // ids of the strip in front of a row's first vector: modulo kVec, so 32 bits will do
+  const uint32_t at_v0 = (uint32_t)(reinterpret_cast<uintptr_t>(a.out) / sizeof(T)) + (uint32_t)v0 + (uint32_t)row_at * (uint32_t)a.ld_out;
+  auto first_of = [&](int row) { return (int)(0u - (at_v0 + (uint32_t)row * (uint32_t)a.ld_out) & (uint32_t)(kVec - 1)); };
+  // whether the logits' rows have their vectors where the output's do
+  const bool vectors = ((reinterpret_cast<uintptr_t>(in.logits) ^ reinterpret_cast<uintptr_t>(a.out)) & 15) == 0 && (((uint32_t)in.ld - (uint32_t)a.ld_out) & (kVec - 1)) == 0;
+  // first id of the lane's t-th vector, or -1
+  auto id_of = [&](int first, int t) {
+    const int at = first + (t * 64 + lane) * kVec;
+    return at < kStride<T> && v0 + at + kVec <= in.V ? v0 + at : -1;
+  };
   Block rows(a, block, lane);
-  while (rows.next()) {
-    if (rows.now == -1 && a.out == in.logits) continue;
-    Frag up[kBlocks][4];
-    if (rows.now >= 0) {
+  // the tile: its adapter, the adapter's rows in the block, which they are, the tile's first; false: none is left
+  int adapter = -3, n = 0, order = 0, q = 0;
+  auto advance = [&]() {
+    q += 16;
+    if (q < n) return true;
+    do {
+      if (!rows.next()) return false;
+    } while (rows.now == -1 && a.out == in.logits);      // in place there is nothing to do for rows without an adapter
+    adapter = rows.now;
+    n = rows.n;
+    order = rows.order;
+    q = 0;
+    return true;
+  };
+  auto load_base = [&](Raw (&base)[kRows][kTurns]) {
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const W* row = static_cast<const W*>(in.up) + ((int64_t)rows.now * in.V + min(v0 + c * 16 + (lane & 15), in.V - 1)) * in.rank;
+    for (int j = 0; j < kRows; ++j) {
+      const int i = q + wave + kUpWaves * j;
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) up[kb][c] = Op::load(row, kb * Op::kDepth, in.rank, lane);
+      for (int t = 0; t < kTurns; ++t) base[j][t] = Raw{};
+      if (i >= n || !in.logits) continue;
+      const int row = __builtin_amdgcn_readlane(order, i);
+      const T* z = logits_of(row);
+      const int first = first_of(row);
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        const int id = id_of(first, t);
+        if (id < 0) continue;
+        if (vectors) {
+          base[j][t] = __builtin_nontemporal_load(reinterpret_cast<const Raw*>(z + id));
+        } else {
+          float x[kVec];
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x[e] = Vec<T>::one(z + id + e);
+          base[j][t] = pack_vec(x);
+        }
       }
     }
-    for (int q = 0; q < rows.n; q += 16) {
-      const int m = block * 64 + rows.row(q + (lane & 15));
-      const bool mine = q + (lane & 15) < rows.n;
-      const int64_t row = a.row0 + m;
-      const T* z = static_cast<const T*>(in.logits) + row * in.ld;
-      T* out = static_cast<T*>(a.out) + row * a.ld_out;
-      f32x4 base[4], sum[4];
+  };
+  constexpr int kChunk = kBlocks * Op::kDepth;            // of the rank: so much of the operands is held; a larger rank reads them in turn for every tile
+  Frag up[kBlocks][4], u[kBlocks][kParts];
+  Raw base[kRows][kTurns], next[kRows][kTurns];
+  int loaded = -1, turn = 0;
+  auto load_operands = [&](int of, int of_n, int of_order, int of_q, int k0) {
+    if (of < 0) return;
+    const int i = of_q + (lane & 15);
+    const uint32_t at = (uint32_t)((block * 64 + __shfl(of_order, i < of_n ? i : 0)) * a.depth + (lane >> 4) * (Op::kDepth / 4));
 #pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int v = v0 + c * 16 + (lane >> 4) * 4;
-        base[c] = f32x4{};
-        sum[c] = f32x4{};
-        if (!in.logits || !mine) continue;
-        if (v + 4 <= in.V) {
-          base[c] = load4(z + v);
-        } else {
+    for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (v + i < in.V) base[c][i] = Vec<T>::one(z + v + i);
+      for (int part = 0; part < kParts; ++part)
+        if (kBlocks <= 2 || k0 + kb * Op::kDepth < a.depth)   // (depth: whole 32s, zeros behind the rank)
+          u[kb][part] = *reinterpret_cast<const Frag*>(reinterpret_cast<const W*>(a.u) + (size_t)(uint32_t)(part * a.rows * a.depth + k0 + kb * Op::kDepth) + at);
+        else
+          u[kb][part] = Frag{};
+    if (of == loaded && in.rank <= kChunk) return;
+#pragma unroll
+    for (int c = 0; c < 4; ++c) {
+      const W* row = static_cast<const W*>(in.up) + ((int64_t)of * in.V + min(v0 + own + c * 16 + (lane & 15), in.V - 1)) * in.rank;
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb) up[kb][c] = Op::load(row, k0 + kb * Op::kDepth, in.rank, lane);
+    }
+    loaded = of;
+  };
+  bool more = advance();
+  if (more) {
+    load_operands(adapter, n, order, q, 0);
+    load_base(base);
+  }
+  while (more) {
+    const int now = adapter, now_n = n, now_order = order, now_q = q;
+    more = advance();
+    if (more) load_base(next);
+    float (*sums)[kPitch] = s_sum[turn];
+    f32x4 sum[4] = {};
+    auto add_products = [&]() {
+#pragma unroll
+      for (int kb = 0; kb < kBlocks; ++kb)
+#pragma unroll
+        for (int part = kParts - 1; part >= 0; --part)
+#pragma unroll
+          for (int c = 0; c < 4; ++c) sum[c] = Op::product(u[kb][part], up[kb][c], sum[c]);
+    };
+    if (now >= 0) {
+      add_products();
+      if constexpr (kLargest)
+        for (int k0 = kChunk; k0 < in.rank; k0 += kChunk) {
+          load_operands(now, now_n, now_order, now_q, k0);
+          add_products();
+        }
+    }
+    // asked for in front of this tile's stores, which a wait for what was asked for behind them would wait for too
+    if (more) load_operands(adapter, n, order, q, 0);
+    if (now >= 0) {
+      // lane: of the rows (lane >> 4) * 4 .. the id (lane & 15) of each 16
+      const int i = now_q + (lane & 15), shift = kFront - first_of(__shfl(now_order, i < now_n ? i : 0));
+#pragma unroll
+      for (int e = 0; e < 4; ++e) {
+        const int row = (lane >> 4) * 4 + e;
+        float* to = &sums[row][own + (lane & 15) + __shfl(shift, row)];
+#pragma unroll
+        for (int c = 0; c < 4; ++c) to[c * 16] = sum[c][e];
+      }
+      __syncthreads();
+      turn ^= 1;                                         // (the other half is written next: one barrier per tile)
+    }
+#pragma unroll
+    for (int j = 0; j < kRows; ++j) {
+      const int i = wave + kUpWaves * j;
+      if (now_q + i >= now_n) break;
+      const int row = __builtin_amdgcn_readlane(now_order, now_q + i);
+      T* out = out_of(row);
+      const int first = first_of(row);
+#pragma unroll
+      for (int t = 0; t < kTurns; ++t) {
+        const int id = id_of(first, t);
+        if (id < 0) continue;
+        if (now != -1) {
+          float x[kVec];
+          Vec<T>::unpack(base[j][t], x);
+#pragma unroll
+          for (int e = 0; e < kVec; ++e) x[e] += now >= 0 ? sums[i][kFront + (t * 64 + lane) * kVec + e] : kNan;
+          base[j][t] = pack_vec(x);
+        }
+        __builtin_nontemporal_store(base[j][t], reinterpret_cast<Raw*>(out + id));
+      }
+      if (edges) {                                       // in front of the row's first vector, behind its last one: one id a lane
+        const T* z = logits_of(row);
+        const RowSplit<T> split(out, in.V);
+        const int tail = split.head + split.vecs * kVec, v = lane < kVec ? lane : tail + lane - kVec;
+        if (lane < kVec ? strip == 0 && v < split.head : lane < 2 * kVec && v < in.V && tail >= v0 && tail < v0 + kStride<T>) {
+          if (now == -1) out[v] = z ? z[v] : T{};
+          else store_one(out + v, (z ? Vec<T>::one(z + v) : 0.f) + (now >= 0 ? sums[i][kFront + v - v0 - first] : kNan));
         }
       }
-      if (rows.now >= 0) {
+    }
+    if (more) {
 #pragma unroll
-        for (int kb = 0; kb < kBlocks; ++kb) {
+      for (int j = 0; j < kRows; ++j)
 #pragma unroll
-          for (int part = kParts - 1; part >= 0; --part) {
-            const W* u = reinterpret_cast<const W*>(a.u) + ((int64_t)part * a.rows + m) * a.depth;
-            const Frag x = Op::load(u, kb * Op::kDepth, a.depth, lane);
-#pragma unroll
-            for (int c = 0; c < 4; ++c) sum[c] = Op::product(up[kb][c], x, sum[c]);
-          }
-        }
-      } else if (rows.now == -2) {
-#pragma unroll
-        for (int c = 0; c < 4; ++c) sum[c] = f32x4{kNan, kNan, kNan, kNan};
-      }
-      if (!mine) continue;
-#pragma unroll
-      for (int c = 0; c < 4; ++c) {
-        const int v = v0 + c * 16 + (lane >> 4) * 4;
-        const f32x4 x = base[c] + sum[c];
-        if (v + 4 <= in.V) {
-          store4(out + v, x);
-        } else {
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (v + i < in.V) store_one(out + v + i, x[i]);
-        }
-      }
+        for (int t = 0; t < kTurns; ++t) base[j][t] = next[j][t];
     }
   }
 }
 
 template <typename W, typename T>
-hipError_t launch_up(const AdapterArgs& a, dim3 grid, int strips, hipStream_t stream) {
-  const int blocks = ceil_div(a.in.rank, Operand<W>::kDepth);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, stream, a, strips); return hipGetLastError(); };
+hipError_t launch_up(const AdapterArgs& a, hipStream_t stream) {
+  const int blocks = ceil_div(a.in.rank, Operand<W>::kDepth), strips = ceil_div(a.in.V, kStride<T>), of_rows = ceil_div(a.rows, 64);
+  const dim3 grid((unsigned)strips * (unsigned)of_rows);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kUpWaves), 0, stream, a, strips); return hipGetLastError(); };
   if (blocks <= 1) return go(adapter_up_kernel<W, T, 1>);
   if (blocks <= 2) return go(adapter_up_kernel<W, T, 2>);
-  if (blocks <= 4) return go(adapter_up_kernel<W, T, 4>);
-  if constexpr (sizeof(W) == 4)
-    if (blocks > 8) return go(adapter_up_kernel<W, T, 16>);
-  return go(adapter_up_kernel<W, T, 8>);
+  return go(adapter_up_kernel<W, T, 4>);                 // also of more
 }
 
 template <typename W>
 hipError_t launch_adapters(const AdapterArgs& a, hipStream_t stream) {
-  const int blocks = ceil_div(a.rows, 64), strips = ceil_div(a.in.V, 256);
+  const int blocks = ceil_div(a.rows, 64);
   const int slots = std::min({a.rows, 16, std::min(a.in.n_adapters, 64) + 3});
   hipLaunchKernelGGL(adapter_down_kernel<W>, dim3((unsigned)(blocks * (a.depth / 16) * slots)), dim3(64 * kDownWaves), 0, stream, a, slots);
-  hipError_t e = hipGetLastError();
+  const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  const dim3 grid((unsigned)strips * (unsigned)blocks);
-  return a.in.logits_dtype == OT_BF16 ? launch_up<W, uint16_t>(a, grid, strips, stream) : launch_up<W, float>(a, grid, strips, stream);
+  return a.in.logits_dtype == OT_BF16 ? launch_up<W, uint16_t>(a, stream) : launch_up<W, float>(a, stream);
 }
 
 }  // namespace
@@ -288,7 +382,7 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
   if (in->logits && ot_rows_overlap(in->logits, in->ld, out, ld_out, in->M, in->V, size))
     return ot_fail(OT_ERR_SHAPE, "ot_adapter_logits: rows of out overlap other places of the logits' rows");
   const int most = std::min(in->M, kAdapterRows);
-  if (!grid_fits((int64_t)ceil_div(in->V, 256) * ceil_div(most, 64), 256))
+  if (!grid_fits((int64_t)ceil_div(in->V, kStride<uint16_t>) * ceil_div(most, 64), 64 * kUpWaves))
     return ot_fail(OT_ERR_SHAPE, "ot_adapter_logits: %d ids are too many for a launch of %d rows", in->V, most);
   if (const int bad = ot_check_device(ctx, "ot_adapter_logits")) return bad;
   for (int row0 = 0; row0 < in->M; row0 += kAdapterRows) {
