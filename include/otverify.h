@@ -376,6 +376,8 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
  * Ids outside [0, V) in history, window and bias lists are none (so -1 pads them).  A mask_of_row outside [-1, n_masks) makes the
  * row NaN.  Penalties are finite, repetition above 0.
  * Without row_off every row is a sequence of its own (B = M).  Rows that no sequence of row_off has are neither read nor written.    */
+#define OT_MAX_BIAS    4096            /* entries of a sequence's bias list at most (longer bans: masks)             */
+#define OT_MAX_HISTORY (1 << 29)       /* ids of a sequence's history at most                                       */
 typedef struct ot_adjust_in {
   int32_t         M, V, B;            /* rows; ids per row; sequences                                              */
   int32_t         dtype;              /* OT_BF16 or OT_F32: type of logits and out                                  */
@@ -409,7 +411,7 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
  *   OT_REST_RENORMALISE  the same with p_i / P
  *   OT_REST_BUCKET       + (1 - P) (ln(1 - P) - ln(1 - Q)):  what is not kept as one token more (P above 1 by rounding counts as 1)
  *   - An id of -1 is none, and so is with through_map a target id without a draft id.  A row without ids adds nothing: loss 0, kept 0,
- *     zero gradient; it is not read.  An id outside [-1, V) (through_map: [-1, V_t)) makes loss, kept and gradient of its row NaN.
+ *     zero gradient, whatever its logits.  An id outside [-1, V) (through_map: [-1, V_t)) makes loss, kept and gradient of its row NaN.
  *   - An id that is named twice has both terms (and counts once in Q).
  *   - A log-probability of -inf is one of p = 0 and adds no term.  NaN or +inf make the row's loss, kept and gradient NaN.
  *   - An id that the student masks (-inf) gets a zero gradient; with p above 0 the row's loss is +inf.  A row that the student masks

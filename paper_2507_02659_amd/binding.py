@@ -23,6 +23,7 @@ OT_MAX_NGRAM_LEN, OT_MAX_K = 8, 63
 OT_STATIC_MAX_BATCH = 4096
 OT_MAX_TOP = 64
 OT_MAX_ADAPTER_RANK = 256
+OT_MAX_BIAS, OT_MAX_HISTORY = 4096, 1 << 29
 OT_MAX_TEACHER_TOP, OT_MAX_STUDENT_V = 256, 1 << 20
 OT_REST_DROP, OT_REST_RENORMALISE, OT_REST_BUCKET = 0, 1, 2
 OT_N_STAGES = 4

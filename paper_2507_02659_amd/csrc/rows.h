@@ -58,6 +58,28 @@ __device__ inline void store_vec(uint16_t* p, const float* x) {
   __builtin_nontemporal_store(r, reinterpret_cast<raw_t*>(p));
 }
 
+// A vector of these values, as the row's type rounds them.
+__device__ inline Vec<float>::Raw pack_vec(const float (&v)[4]) { return {v[0], v[1], v[2], v[3]}; }
+__device__ inline Vec<uint16_t>::Raw pack_vec(const float (&v)[8]) {
+  Vec<uint16_t>::Raw r;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{v[2 * i], v[2 * i + 1]}, bf16x2));
+  return r;
+}
+
+// The elements of a vector whose bit is clear become -inf.
+__device__ inline void mask_vector(Vec<float>::Raw* x, uint32_t allowed) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) (*x)[e] = allowed >> e & 1 ? (*x)[e] : -INFINITY;
+}
+__device__ inline void mask_vector(Vec<uint16_t>::Raw* x, uint32_t allowed) {
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t keep = (allowed >> (2 * e) & 1 ? 0xFFFFu : 0u) | (allowed >> (2 * e + 1) & 1 ? 0xFFFF0000u : 0u);
+    (*x)[e] = ((*x)[e] & keep) | (0xFF80FF80u & ~keep);
+  }
+}
+
 // A row's elements as whole vectors from the first 16-byte boundary on, and those in front of it and behind the last whole one (fewer than
 // two vectors' worth), which go one by one.
 template <typename T>

@@ -25,63 +25,59 @@ struct TopDistillArgs {
   int64_t ld_grad;
 };
 
-// What the first wavefront hands to the others.
-struct RowCoef {
-  float rest;               // of exp((z - mx) / T), mx the others' largest logit, in a gradient outside K
-  int32_t zero;             // the row adds nothing
-};
-
 // Grid = rows.  A workgroup holds the vectors of its row that fit its registers (kHeld per thread) from the sums to the gradient and reads what is
-// beyond them twice.  The kept ids, of which the first wavefront has up to four per lane, are taken in 64 bits; the others through a bitmap in
-// LDS that tells them apart, in float32 exponentials of their distance to their largest.
+// beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie among the others a bitmap in LDS
+// says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of their distance to their largest.
+constexpr int kEntryWaves = OT_MAX_TEACHER_TOP / 64;
+constexpr int kGradWaves = 4;
 template <typename T, int kThreads, int kHeld, bool kGrad>
-__global__ __launch_bounds__(kThreads) void top_distill_kernel(TopDistillArgs a) {
+__global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) void top_distill_kernel(TopDistillArgs a) {
   typedef typename Vec<T>::Raw Raw;
-  constexpr int kVec = Vec<T>::kElems, kWaves = kThreads / 64, kEach = OT_MAX_TEACHER_TOP / 64;
+  constexpr int kVec = Vec<T>::kElems, kWaves = kThreads / 64;
   constexpr uint32_t kAll = (1u << kVec) - 1;
   extern __shared__ uint32_t s_keep[];                   // [V / 32 + 2]
-  __shared__ int s_id[OT_MAX_TEACHER_TOP];
-  __shared__ double s_p[OT_MAX_TEACHER_TOP], s_sum[kWaves];
-  __shared__ float s_max[kWaves];
-  __shared__ int s_state;
-  __shared__ RowCoef s_coef;
+  __shared__ volatile int s_id[OT_MAX_TEACHER_TOP];
+  __shared__ volatile double s_p[OT_MAX_TEACHER_TOP];
+  __shared__ double s_sum[kWaves], s_P[kEntryWaves], s_E[kEntryWaves], s_L[kEntryWaves];
+  __shared__ float s_max[kWaves], s_top[kEntryWaves];
+  __shared__ int s_twice;
   const ot_top_distill_in& in = a.in;
   const int row = (int)blockIdx.x, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, V = in.V;
   const T* z = static_cast<const T*>(in.logits) + (int64_t)row * in.ld;
   T* grad = kGrad ? static_cast<T*>(a.grad) + (int64_t)row * a.ld_grad : nullptr;
   const RowSplit<T> split(z, V);
   const Raw* zv = reinterpret_cast<const Raw*>(z + split.head);
-  const float temperature = row_temperature(in.temperature, in.row_off, in.B, row, lane), scale = kLog2e / temperature;
 
-  // the teacher's entries, entry lane + 64 j of the first wavefront's lanes
-  for (int i = tid; i < V / 32 + 2; i += kThreads) s_keep[i] = 0;
-  int id[kEach];
-  float lp[kEach], zk[kEach];
-  bool broken = false;
-  if (wave == 0) {
-    bool any = false;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      const int i = lane + 64 * j;
-      id[j] = -1;
-      lp[j] = -INFINITY;
-      if (i < in.n_top) {
-        int v = in.top_ids[(int64_t)row * in.n_top + i];
-        lp[j] = in.top_logprobs[(int64_t)row * in.n_top + i];
-        const bool inside = v >= -1 && v < (in.through_map ? a.V_t : V);
-        broken |= !inside;
-        if (in.through_map && inside && v >= 0) v = a.tmap[v];
-        id[j] = inside && v >= 0 && v < V ? v : -1;
-        if (id[j] >= 0) broken |= isnan(lp[j]) || lp[j] == INFINITY;
-      }
-      any |= id[j] >= 0;
-    }
-    broken = __any(broken);
-    const int state = (__any(any) || broken) ? 1 : 0;
-    if (lane == 0) s_state = state;
+  // the teacher's entries; the row's vectors behind them on their way
+  const bool entries = wave < kEntryWaves;
+  int id = -1;
+  float lp = -INFINITY;
+  if (tid < in.n_top) {
+    id = in.top_ids[(int64_t)row * in.n_top + tid];
+    lp = in.top_logprobs[(int64_t)row * in.n_top + tid];
   }
-  __syncthreads();
-  if (s_state == 0) {                                    // no ids: nothing is read
+  Raw raw[kHeld];
+#pragma unroll
+  for (int k = 0; k < kHeld; ++k) {
+    const int at = k * kThreads + tid;
+    raw[k] = Raw{};
+    if (at < split.vecs) raw[k] = __builtin_nontemporal_load(zv + at);
+  }
+  const bool has_edge = tid < split.head + split.tail;
+  const int edge_id = has_edge ? split.edge(tid) : 0;
+  float edge = has_edge ? Vec<T>::one(z + edge_id) : -INFINITY;
+  const float temperature = row_temperature(in.temperature, in.row_off, in.B, row, lane), scale = kLog2e / temperature;
+  const double temp = (double)temperature;
+  for (int i = tid; i < V / 32 + 2; i += kThreads) s_keep[i] = 0;
+  if (tid == 0) s_twice = 0;
+  const bool inside = id >= -1 && id < (in.through_map ? a.V_t : V);
+  if (in.through_map && inside && id >= 0) id = a.tmap[id];
+  if (!inside || id >= V) id = -1;
+  const bool wrong = !inside || (id >= 0 && (isnan(lp) || lp == INFINITY));
+  float zk = -INFINITY;
+  if (id >= 0) zk = Vec<T>::one(z + id);
+  const bool broken = __syncthreads_or(wrong);           // (the bitmap is clear from here on)
+  if (!__syncthreads_or(id >= 0) && !broken) {           // no ids: the row's logits do not matter
     if (tid == 0) {
       a.loss[row] = 0.f;
       if (a.kept) a.kept[row] = 0.f;
@@ -94,172 +90,154 @@ __global__ __launch_bounds__(kThreads) void top_distill_kernel(TopDistillArgs a)
     }
     return;
   }
-  Raw raw[kHeld];
-#pragma unroll
-  for (int k = 0; k < kHeld; ++k) {
-    const int at = k * kThreads + tid;
-    raw[k] = Raw{};
-    if (at < split.vecs) raw[k] = kGrad ? zv[at] : __builtin_nontemporal_load(zv + at);
-  }
-  const bool has_edge = tid < split.head + split.tail;
-  const int edge_id = has_edge ? split.edge(tid) : 0;
-  const float edge = has_edge ? Vec<T>::one(z + edge_id) : -INFINITY;
-  bool twice = false;
-  if (wave == 0) {
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      zk[j] = -INFINITY;
-      if (id[j] < 0) continue;
-      zk[j] = Vec<T>::one(z + id[j]);
-      const uint32_t bit = 1u << (id[j] & 31);
-      twice |= (atomicOr(&s_keep[id[j] >> 5], bit) & bit) != 0;
+  double p = 0.0;
+  if (entries) {
+    if (id >= 0) {
+      const uint32_t bit = 1u << (id & 31);
+      if (atomicOr(&s_keep[id >> 5], bit) & bit) s_twice = 1;
+      p = exp((double)lp);
     }
+    s_id[tid] = id;
+    s_p[tid] = p;
+    const double P = wave_sum(p);
+    const float top = wave_max(zk);
+    if (lane == 0) { s_P[wave] = P; s_top[wave] = top; }
   }
   __syncthreads();
 
-  auto keep_at = [&](int v) { return (uint32_t)((((uint64_t)s_keep[(v >> 5) + 1] << 32) | s_keep[v >> 5]) >> (v & 31)) & kAll; };
+  auto keep_at = [&](int v) { return __builtin_amdgcn_alignbit(s_keep[(v >> 5) + 1], s_keep[v >> 5], v & 31) & kAll; };
   const bool edge_kept = has_edge && (keep_at(edge_id) & 1);
-  // the others' largest logit
-  float mx = has_edge && !edge_kept ? edge : -INFINITY;
-  auto vector_max = [&](const Raw& x, int v0) {
-    float v[kVec];
+  if (edge_kept) edge = -INFINITY;
+  // of a vector from id v0 on: its values, -inf in the places of kept ids
+  auto others = [&](Raw x, int v0, float* v) {
+    if (const uint32_t keep = keep_at(v0)) mask_vector(&x, ~keep);
     Vec<T>::unpack(x, v);
-    const uint32_t keep = keep_at(v0);
-#pragma unroll
-    for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, keep >> e & 1 ? -INFINITY : v[e]);
   };
+  float mx = edge;                                       // their largest
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
-    if (const int at = k * kThreads + tid; at < split.vecs) vector_max(raw[k], split.head + at * kVec);
-  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) vector_max(zv[at], split.head + at * kVec);
+  for (int k = 0; k < kHeld; ++k) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int at = k * kThreads + tid;
+    if (at >= split.vecs) continue;
+    if (const uint32_t keep = keep_at(split.head + at * kVec)) mask_vector(&raw[k], ~keep);
+    float v[kVec];
+    Vec<T>::unpack(raw[k], v);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, v[e]);
+  }
+  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) {
+    float v[kVec];
+    others(zv[at], split.head + at * kVec, v);
+#pragma unroll
+    for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, v[e]);
+  }
   mx = wave_max(mx);
   if (lane == 0) s_max[wave] = mx;
   __syncthreads();
   mx = wave_max(lane < kWaves ? s_max[lane] : -INFINITY);
+  const float top = fmaxf(mx, wave_max(lane < kEntryWaves ? s_top[lane] : -INFINITY));
   const float ref = mx == -INFINITY ? 0.f : mx;
+  const double ref_top = top == -INFINITY ? 0.0 : (double)top;
   // and the sum of their exponentials
-  double sum = 0.0;
-  auto vector_sum = [&](const Raw& x, int v0) {
-    float v[kVec];
-    Vec<T>::unpack(x, v);
-    const uint32_t keep = keep_at(v0);
+  double sum = (double)__builtin_amdgcn_exp2f((edge - ref) * scale);
+  auto add = [&](float* v) {
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) v[e] = keep >> e & 1 ? 0.f : __builtin_amdgcn_exp2f((v[e] - ref) * scale);
+    for (int e = 0; e < kVec; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - ref) * scale);
     sum += (double)tree_sum<kVec>(v);
   };
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
-    if (const int at = k * kThreads + tid; at < split.vecs) vector_sum(raw[k], split.head + at * kVec);
-  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) vector_sum(zv[at], split.head + at * kVec);
-  if (has_edge && !edge_kept) sum += (double)__builtin_amdgcn_exp2f((edge - ref) * scale);
+  for (int k = 0; k < kHeld; ++k) {
+    __builtin_amdgcn_sched_barrier(0);                   // (one vector at a time: together they take twice the registers)
+    if (k * kThreads + tid >= split.vecs) continue;
+    float v[kVec];
+    Vec<T>::unpack(raw[k], v);
+    add(v);
+  }
+  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) {
+    float v[kVec];
+    others(zv[at], split.head + at * kVec, v);
+    add(v);
+  }
   sum = wave_sum(sum);
   if (lane == 0) s_sum[wave] = sum;
+  // entries of the same id: the first of them has the id's part in Q and its gradient
+  bool first = id >= 0;
+  double p_id = p, e = 0.0;
+  if (entries) {
+    if (s_twice) {
+      for (int i = 0; i < in.n_top; ++i) {
+        if (id < 0 || s_id[i] != id) continue;
+        if (i < tid) first = false;
+        if (i > tid) p_id += s_p[i];
+      }
+    }
+    const double x = ((double)zk - ref_top) / temp;
+    if (id >= 0) e = exp(x);
+    const double E = wave_sum(first ? e : 0.0), L = wave_sum(p != 0.0 ? p * ((double)lp - x) : 0.0);
+    if (lane == 0) { s_E[wave] = E; s_L[wave] = L; }
+  }
   __syncthreads();
 
-  if (wave == 0) {
-    const double S_rest = wave_sum(lane < kWaves ? s_sum[lane] : 0.0), temp = (double)temperature;
-    // entries of the same id: the first of them has the id's part in Q and its gradient
-    bool first[kEach];
-    double p[kEach], p_id[kEach];
-    double P = 0.0;
-    float top = mx;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      first[j] = id[j] >= 0;
-      p_id[j] = p[j] = id[j] >= 0 ? exp((double)lp[j]) : 0.0;
-      P += p[j];
-      top = fmaxf(top, zk[j]);
-    }
-    P = wave_sum(P);
-    top = wave_max(top);
-    if (__any(twice)) {
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        *(volatile int*)&s_id[lane + 64 * j] = id[j];
-        *(volatile double*)&s_p[lane + 64 * j] = p[j];
-      }
-      __builtin_amdgcn_wave_barrier();
-      for (int i = 0; i < in.n_top; ++i) {
-        const int other = *(volatile int*)&s_id[i];
-        const double more = *(volatile double*)&s_p[i];
-#pragma unroll
-        for (int j = 0; j < kEach; ++j) {
-          if (id[j] < 0 || other != id[j]) continue;
-          if (i < lane + 64 * j) first[j] = false;
-          if (i > lane + 64 * j) p_id[j] += more;
-        }
-      }
-    }
-    const double ref_top = top == -INFINITY ? 0.0 : (double)top;
-    const double rest = mx == -INFINITY && !isnan(S_rest) ? 0.0 : S_rest * exp(((double)mx - ref_top) / temp);   // of exp((z - top) / T)
-    double e[kEach], S = 0.0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j) {
-      e[j] = id[j] >= 0 ? exp(((double)zk[j] - ref_top) / temp) : 0.0;
-      if (first[j]) S += e[j];
-    }
-    S = wave_sum(S) + rest;
-    const double lnS = log(S), norm = in.rest == OT_REST_RENORMALISE ? P : 1.0, ln_norm = log(norm);
-    double loss = 0.0;
-#pragma unroll
-    for (int j = 0; j < kEach; ++j)
-      if (id[j] >= 0 && p[j] != 0.0 && norm > 0.0) loss += p[j] / norm * ((double)lp[j] - ln_norm - (((double)zk[j] - ref_top) / temp - lnS));
-    loss = wave_sum(loss);
-    const double left = in.rest == OT_REST_BUCKET && P < 1.0 ? 1.0 - P : 0.0;
-    if (left > 0.0) loss += left * (log(left) - (S_rest == 0.0 ? -INFINITY : log(S_rest) + ((double)mx - ref_top) / temp - lnS));
-    const bool nothing = S == 0.0 && top == -INFINITY && !broken;       // masked whole
-    if (broken) loss = (double)kNan;
-    if (lane == 0) {
-      a.loss[row] = nothing ? 0.f : (float)loss;
-      if (a.kept) a.kept[row] = broken ? kNan : (float)P;
-    }
-    if (kGrad) {
-      const double each = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;
-      const double mass = in.rest == OT_REST_BUCKET ? 1.0 : in.rest == OT_REST_RENORMALISE ? (P > 0.0 ? 1.0 : 0.0) : P;   // in front of q_v
-      if (lane == 0) {
-        double c = mx == -INFINITY && !isnan(S) ? 0.0 : each * mass * exp(((double)mx - ref_top) / temp) / S;
-        if (left > 0.0 && S_rest > 0.0) c -= each * left / S_rest;
-        s_coef.rest = broken ? kNan : (float)c;
-        s_coef.zero = nothing;
-      }
-#pragma unroll
-      for (int j = 0; j < kEach; ++j) {
-        if (!first[j]) continue;
-        double g = each * (mass * e[j] / S - (norm > 0.0 ? p_id[j] / norm : 0.0));
-        if (nothing || (zk[j] == -INFINITY && !isnan(S))) g = 0.0;
-        if (broken) g = (double)kNan;
-        store_one(grad + id[j], (float)g);
-      }
-    }
+  const double S_rest = wave_sum(lane < kWaves ? s_sum[lane] : 0.0);
+  const double P = (s_P[0] + s_P[1]) + (s_P[2] + s_P[3]);
+  const double shift = ((double)mx - ref_top) / temp;    // (-inf: there are no others)
+  const double down = mx == -INFINITY && !isnan(S_rest) ? 0.0 : exp(shift);
+  const double S = ((s_E[0] + s_E[1]) + (s_E[2] + s_E[3])) + S_rest * down;
+  const double left = in.rest == OT_REST_BUCKET && P < 1.0 ? 1.0 - P : 0.0;
+  const bool nothing = S == 0.0 && top == -INFINITY && !broken;         // masked whole
+  const double norm = in.rest == OT_REST_RENORMALISE ? P : 1.0;
+  if (tid == 0) {
+    const double lnS = log(S);
+    double loss = norm > 0.0 ? ((s_L[0] + s_L[1]) + (s_L[2] + s_L[3]) + P * (lnS - log(norm))) / norm : 0.0;
+    if (left > 0.0) loss += left * (log(left) - (S_rest == 0.0 ? -INFINITY : log(S_rest) + shift - lnS));
+    if (nothing) loss = 0.0;
+    a.loss[row] = broken || isnan(P) ? kNan : (float)loss;
+    if (a.kept) a.kept[row] = broken ? kNan : (float)P;
   }
   if (!kGrad) return;
-  __syncthreads();
-  const float c = s_coef.zero ? 0.f : s_coef.rest;
-  const bool zero = s_coef.zero;
-  const bool vectors = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0;
+  const double scaled = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;
+  const double mass = in.rest == OT_REST_BUCKET ? 1.0 : in.rest == OT_REST_RENORMALISE ? (P > 0.0 ? 1.0 : 0.0) : P;   // in front of q_v
+  if (first) {
+    double g = scaled * (mass * e / S - (norm > 0.0 ? p_id / norm : 0.0));
+    if (nothing || (zk == -INFINITY && !isnan(S))) g = 0.0;
+    store_one(grad + id, broken ? kNan : (float)g);
+  }
+  // of exp((z - mx) / T) in the others' gradients
+  double factor = down == 0.0 ? 0.0 : scaled * mass * down / S;
+  if (left > 0.0 && S_rest > 0.0) factor -= scaled * left / S_rest;
+  const float c = nothing ? 0.f : broken || isnan(S) ? kNan : (float)factor;
   const float none = isnan(c) ? c : 0.f;                 // where the exponential is 0, also beside an infinite factor
+  const bool vectors = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0;
   auto gradient = [&](float x) {
-    const float e = __builtin_amdgcn_exp2f((x - ref) * scale);
-    return zero ? 0.f : e == 0.f ? none : c * e;
+    const float y = __builtin_amdgcn_exp2f((x - ref) * scale);
+    return y == 0.f ? none : c * y;
   };
-  auto vector_grad = [&](const Raw& x, int v0) {
-    float v[kVec];
-    Vec<T>::unpack(x, v);
+  auto put = [&](float* v, int v0) {
     const uint32_t keep = keep_at(v0);
 #pragma unroll
     for (int e = 0; e < kVec; ++e) v[e] = gradient(v[e]);
     if (vectors && keep == 0) {
       store_vec(grad + v0, v);
-    } else {                                             // the kept ids' are there already
+    } else {                                             // the kept ids' are the entries' business
 #pragma unroll
       for (int e = 0; e < kVec; ++e)
         if (!(keep >> e & 1)) store_one(grad + v0 + e, v[e]);
     }
   };
 #pragma unroll
-  for (int k = 0; k < kHeld; ++k)
-    if (const int at = k * kThreads + tid; at < split.vecs) vector_grad(raw[k], split.head + at * kVec);
-  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) vector_grad(zv[at], split.head + at * kVec);
+  for (int k = 0; k < kHeld; ++k) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int at = k * kThreads + tid;
+    if (at >= split.vecs) continue;
+    float v[kVec];
+    Vec<T>::unpack(raw[k], v);
+    put(v, split.head + at * kVec);
+  }
+  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) {
+    float v[kVec];
+    others(zv[at], split.head + at * kVec, v);
+    put(v, split.head + at * kVec);
+  }
   if (has_edge && !edge_kept) store_one(grad + edge_id, gradient(edge));
 }
 
@@ -268,7 +246,7 @@ hipError_t launch(const TopDistillArgs& a, hipStream_t stream) {
   constexpr int kVec = Vec<T>::kElems;
   const size_t lds = sizeof(uint32_t) * ((size_t)a.in.V / 32 + 2);
   auto go = [&](auto kernel, int threads) {
-    if (lds > (60 << 10)) {
+    if (lds > (56 << 10)) {
       const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
       if (e != hipSuccess) return e;
     }
@@ -276,6 +254,7 @@ hipError_t launch(const TopDistillArgs& a, hipStream_t stream) {
     return hipGetLastError();
   };
   if (a.in.V <= 256 * 4 * kVec) return go(top_distill_kernel<T, 256, 4, kGrad>, 256);
+  if (a.in.V <= 512 * 8 * kVec) return go(top_distill_kernel<T, 512, 8, kGrad>, 512);
   if (a.in.V <= 1024 * 8 * kVec) return go(top_distill_kernel<T, 1024, 8, kGrad>, 1024);
   return go(top_distill_kernel<T, 1024, 16, kGrad>, 1024);
 }

@@ -97,6 +97,15 @@ def test_lengths(v, V, dtype):
     _check(v, _logits(rng, M, V, dtype), **kw)
 
 
+@pytest.mark.parametrize("V", [1, 33, 4095, 16383, 16385, 40003])
+def test_long_histories(v, V):
+    """The larger workgroups: slices of 16384 ids, of ragged windows."""
+    rng = np.random.default_rng(V)
+    M, kw = _all(rng, 3, [2, 70, 1], V, L=4500, n_bias=9)
+    _check(v, _logits(rng, M, V), **kw)
+    _check(v, _logits(rng, M, V, torch.bfloat16), **kw)
+
+
 @pytest.mark.parametrize("rows", [[1], [64], [1] * 70, [5, 0, 9, 1, 64, 2], [200], [3] * 300])
 @pytest.mark.parametrize("V", [300, 5000])
 def test_numbers_of_rows(v, rows, V):
@@ -171,6 +180,19 @@ def test_masks_and_special_values(v, dtype):
     _check(v, z, **kw)
     kw["repetition"] = np.full(12, 2.0, np.float32)       # products past the type's range
     _check(v, z, **kw)
+
+
+@pytest.mark.parametrize("n_bias", [1, 2, 3, 64, 300, 4096])
+@pytest.mark.parametrize("L", [3, 6000])
+def test_bias_lists(v, n_bias, L):
+    """Lists up to the longest, of ids in one place and all over, with both sizes of workgroups."""
+    rng = np.random.default_rng(n_bias)
+    V = 20011
+    M, kw = _all(rng, 3, [2, 1, 2], V, L=L, n_bias=n_bias)
+    kw["bias_ids"][0] = 5000 + rng.permutation(n_bias)
+    kw["bias_ids"][1] = rng.permutation(V)[:n_bias]
+    _check(v, _logits(rng, M, V), **kw)
+    _check(v, _logits(rng, M, V, torch.bfloat16), **kw)
 
 
 def test_an_id_that_the_bias_list_names_twice(v):

@@ -52,7 +52,7 @@ def _adjust(out=AT + (1 << 40), ld_out=100, **kw):
 def test_adjusted_logits():
     S, N, D = ot.OT_ERR_SHAPE, ot.OT_ERR_NULL, ot.OT_ERR_DTYPE
     for kw in (dict(M=-1), dict(V=0), dict(V=2 ** 30 + 1, ld=2 ** 31, ld_out=2 ** 31), dict(ld=99), dict(ld_out=99), dict(B=3), dict(B=5), dict(B=-1, row_off=AT),
-               dict(reserved=(1, 0)), dict(reserved=(0, 1)), dict(n_bias=-1), dict(n_masks=-1), dict(ld_history=-1), dict(masks=AT, n_masks=4, ld_mask=3),
+               dict(reserved=(1, 0)), dict(reserved=(0, 1)), dict(n_bias=-1), dict(n_bias=4097, bias=AT, bias_ids=AT), dict(history=AT, ld_history=2 ** 29 + 1), dict(n_masks=-1), dict(ld_history=-1), dict(masks=AT, n_masks=4, ld_mask=3),
                dict(window=AT), dict(masks=AT, n_masks=3, ld_mask=4), dict(logits=AT + 2), dict(out=AT + 2), dict(out=AT, ld_out=101),
                dict(out=AT + 4 * 99), dict(V=2 ** 30, ld=2 ** 30, ld_out=2 ** 30, M=100, B=100, out=1 << 50)):
         assert _adjust(**kw) == S, kw
