@@ -168,7 +168,7 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
   const ot_adapter_in& in = a.in;
   const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
   const int strip = (int)(blockIdx.x % (unsigned)strips), block = (int)(blockIdx.x / (unsigned)strips);
-  __shared__ float s_sum[2][16][kPitch];
+  __shared__ alignas(16) float s_sum[2][16][kPitch];
   const int v0 = strip * kStride<T>, own = wave * 64;
   const bool edges = strip == 0 || v0 + kStrip >= in.V;
   const int row_at = a.row0 + block * 64;                // first row of the block
@@ -185,28 +185,23 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
     return at < kStride<T> && v0 + at + kVec <= in.V ? v0 + at : -1;
   };
   Block rows(a, block, lane);
-  // the tile: its adapter, the adapter's rows in the block, which they are, the tile's first; false: none is left
-  int adapter = -3, n = 0, order = 0, q = 0;
-  auto advance = [&]() {
-    q += 16;
-    if (q < n) return true;
+  // A tile: its adapter (-3: none is left), the adapter's rows in the block, which they are, the tile's first.
+  struct Tile { int adapter, n, order, q; };
+  auto after = [&](const Tile& t) {
+    if (t.q + 16 < t.n) return Tile{t.adapter, t.n, t.order, t.q + 16};
     do {
-      if (!rows.next()) return false;
+      if (!rows.next()) return Tile{-3, 0, 0, 0};
     } while (rows.now == -1 && a.out == in.logits);      // in place there is nothing to do for rows without an adapter
-    adapter = rows.now;
-    n = rows.n;
-    order = rows.order;
-    q = 0;
-    return true;
+    return Tile{rows.now, rows.n, rows.order, 0};
   };
-  auto load_base = [&](Raw (&base)[kRows][kTurns]) {
+  auto load_base = [&](const Tile& of, Raw (&base)[kRows][kTurns]) {
 #pragma unroll
     for (int j = 0; j < kRows; ++j) {
-      const int i = q + wave + kUpWaves * j;
+      const int i = of.q + wave + kUpWaves * j;
 #pragma unroll
       for (int t = 0; t < kTurns; ++t) base[j][t] = Raw{};
-      if (i >= n || !in.logits) continue;
-      const int row = __builtin_amdgcn_readlane(order, i);
+      if (i >= of.n || !in.logits) continue;
+      const int row = __builtin_amdgcn_readlane(of.order, i);
       const T* z = logits_of(row);
       const int first = first_of(row);
 #pragma unroll
@@ -226,12 +221,14 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
   };
   constexpr int kChunk = kBlocks * Op::kDepth;            // of the rank: so much of the operands is held; a larger rank reads them in turn for every tile
   Frag up[kBlocks][4], u[kBlocks][kParts];
-  Raw base[kRows][kTurns], next[kRows][kTurns];
+  constexpr int kAhead = kTurns == 1 ? 2 : 1;            // tiles whose logits are on their way while one is taken
+  Raw base[kAhead + 1][kRows][kTurns];
+  Tile tile[kAhead + 1];
   int loaded = -1, turn = 0;
-  auto load_operands = [&](int of, int of_n, int of_order, int of_q, int k0) {
-    if (of < 0) return;
-    const int i = of_q + (lane & 15);
-    const uint32_t at = (uint32_t)((block * 64 + __shfl(of_order, i < of_n ? i : 0)) * a.depth + (lane >> 4) * (Op::kDepth / 4));
+  auto load_operands = [&](const Tile& of, int k0) {
+    if (of.adapter < 0) return;
+    const int i = of.q + (lane & 15);
+    const uint32_t at = (uint32_t)((block * 64 + __shfl(of.order, i < of.n ? i : 0)) * a.depth + (lane >> 4) * (Op::kDepth / 4));
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
@@ -240,24 +237,27 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
           u[kb][part] = *reinterpret_cast<const Frag*>(reinterpret_cast<const W*>(a.u) + (size_t)(uint32_t)(part * a.rows * a.depth + k0 + kb * Op::kDepth) + at);
         else
           u[kb][part] = Frag{};
-    if (of == loaded && in.rank <= kChunk) return;
+    if (of.adapter == loaded && in.rank <= kChunk) return;
 #pragma unroll
     for (int c = 0; c < 4; ++c) {
-      const W* row = static_cast<const W*>(in.up) + ((int64_t)of * in.V + min(v0 + own + c * 16 + (lane & 15), in.V - 1)) * in.rank;
+      const W* row = static_cast<const W*>(in.up) + ((int64_t)of.adapter * in.V + min(v0 + own + c * 16 + (lane & 15), in.V - 1)) * in.rank;
 #pragma unroll
       for (int kb = 0; kb < kBlocks; ++kb) up[kb][c] = Op::load(row, k0 + kb * Op::kDepth, in.rank, lane);
     }
-    loaded = of;
+    loaded = of.adapter;
   };
-  bool more = advance();
-  if (more) {
-    load_operands(adapter, n, order, q, 0);
-    load_base(base);
+  tile[0] = after(Tile{-3, 0, 0, 0});
+  load_operands(tile[0], 0);
+  load_base(tile[0], base[0]);
+#pragma unroll
+  for (int i = 1; i < kAhead; ++i) {
+    tile[i] = after(tile[i - 1]);
+    load_base(tile[i], base[i]);
   }
-  while (more) {
-    const int now = adapter, now_n = n, now_order = order, now_q = q;
-    more = advance();
-    if (more) load_base(next);
+  while (tile[0].adapter != -3) {
+    const int now = tile[0].adapter, now_n = tile[0].n, now_order = tile[0].order, now_q = tile[0].q;
+    tile[kAhead] = after(tile[kAhead - 1]);
+    load_base(tile[kAhead], base[kAhead]);
     float (*sums)[kPitch] = s_sum[turn];
     f32x4 sum[4] = {};
     auto add_products = [&]() {
@@ -272,12 +272,12 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
       add_products();
       if constexpr (kLargest)
         for (int k0 = kChunk; k0 < in.rank; k0 += kChunk) {
-          load_operands(now, now_n, now_order, now_q, k0);
+          load_operands(tile[0], k0);
           add_products();
         }
     }
     // asked for in front of this tile's stores, which a wait for what was asked for behind them would wait for too
-    if (more) load_operands(adapter, n, order, q, 0);
+    load_operands(tile[1], 0);
     if (now >= 0) {
       // lane: of the rows (lane >> 4) * 4 .. the id (lane & 15) of each 16
       const int i = now_q + (lane & 15), shift = kFront - first_of(__shfl(now_order, i < now_n ? i : 0));
@@ -304,12 +304,15 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
         if (id < 0) continue;
         if (now != -1) {
           float x[kVec];
-          Vec<T>::unpack(base[j][t], x);
+          Vec<T>::unpack(base[0][j][t], x);
 #pragma unroll
-          for (int e = 0; e < kVec; ++e) x[e] += now >= 0 ? sums[i][kFront + (t * 64 + lane) * kVec + e] : kNan;
-          base[j][t] = pack_vec(x);
+          for (int e = 0; e < kVec; e += 4) {
+            const f32x4 y = now >= 0 ? *reinterpret_cast<const f32x4*>(&sums[i][kFront + (t * 64 + lane) * kVec + e]) : f32x4{kNan, kNan, kNan, kNan};
+            x[e] += y.x; x[e + 1] += y.y; x[e + 2] += y.z; x[e + 3] += y.w;
+          }
+          base[0][j][t] = pack_vec(x);
         }
-        __builtin_nontemporal_store(base[j][t], reinterpret_cast<Raw*>(out + id));
+        __builtin_nontemporal_store(base[0][j][t], reinterpret_cast<Raw*>(out + id));
       }
       if (edges) {                                       // in front of the row's first vector, behind its last one: one id a lane
         const T* z = logits_of(row);
@@ -321,11 +324,13 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
         }
       }
     }
-    if (more) {
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      tile[i] = tile[i + 1];
 #pragma unroll
       for (int j = 0; j < kRows; ++j)
 #pragma unroll
-        for (int t = 0; t < kTurns; ++t) base[j][t] = next[j][t];
+        for (int t = 0; t < kTurns; ++t) base[i][j][t] = base[i + 1][j][t];
     }
   }
 }
