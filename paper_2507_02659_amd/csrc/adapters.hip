@@ -107,9 +107,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
       const int r = r0 + (lane & 15), m = block * 64 + rows.row(q + (lane & 15));
       const W* down = static_cast<const W*>(in.down) + ((int64_t)rows.now * in.rank + min(r, in.rank - 1)) * in.d;
       const W* hidden = static_cast<const W*>(in.hidden) + (int64_t)(a.row0 + m) * in.d;
-      const int K = r < in.rank ? in.d : 0;
+      const int K = r < in.rank ? in.d : 0, end = r0 < in.rank ? in.d : 0;   // (behind the rank: zeros)
       f32x4 sum{};
-      for (int k0 = wave * Op::kDepth; k0 < in.d; k0 += kDownSteps * kDownWaves * Op::kDepth) {
+      for (int k0 = wave * Op::kDepth; k0 < end; k0 += kDownSteps * kDownWaves * Op::kDepth) {
         typename Op::Frag x[kDownSteps], y[kDownSteps];
 #pragma unroll
         for (int i = 0; i < kDownSteps; ++i) {
