@@ -35,9 +35,9 @@ __device__ inline uint32_t bits_at(uint32_t lo, uint32_t hi, int at) { return __
 // the history into a table in LDS, once for all of its rows (whole numbers: the order of the additions does not matter), puts the slice's biases
 // into a small hash table and marks the ids of both in a bitmap; a row then costs one pass over its logits, of which a vector without a marked or
 // masked id is only copied (in place: not even read).  The window's tokens join the table row by row.  The first row's logits are on their
-// way while the table is built, the next row's while one is taken.
+// way while the table is built.
 template <typename T, int kThreads, bool kInPlace>
-__global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
+__global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
   typedef typename Vec<T>::Raw Raw;
   constexpr int kVec = Vec<T>::kElems, kLoads = 16 / kVec, kSlice = kThreads * 16;
   constexpr uint32_t kAll = (1u << kVec) - 1;
@@ -75,7 +75,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
       if (!kInPlace) f->raw[i] = Raw{};
       f->lo[i] = f->hi[i] = kNoKey;
       if (k >= split.vecs) continue;
-      if (!kInPlace) f->raw[i] = __builtin_nontemporal_load(zv + k);
+      if (!kInPlace) f->raw[i] = zv[k];
       if (mask) { f->lo[i] = mask[v >> 5]; f->hi[i] = mask[(v + kVec - 1) >> 5]; }
     }
   };
@@ -105,7 +105,7 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
     const int n = (int)min((int64_t)(in.n_history ? max(0, in.n_history[b]) : 0x7FFFFFFF), in.ld_history);
     const int n_prompt = in.n_prompt ? in.n_prompt[b] : 0;
     const int32_t* ids = in.history + (int64_t)b * in.ld_history;
-    constexpr int kBatch = 4;                            // vectors of four ids per thread that are on their way together
+    constexpr int kBatch = 2;                            // vectors of four ids per thread that are on their way together
     for (int i0 = 0; i0 < n; i0 += kBatch * 4 * kThreads) {
       i32x4_any got[kBatch];
 #pragma unroll
@@ -167,12 +167,6 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
 
   for (int row = first; row < last; ++row) {
     const int token = __builtin_amdgcn_readlane(tokens, row - rows_at), m = m_now;
-    Fetched next;
-    if (row + 1 < last) {
-      if (row + 1 - rows_at == 64) { rows_at += 64; fetch_rows(); }
-      m_now = __builtin_amdgcn_readlane(masks, row + 1 - rows_at);
-      fetch(row + 1, m_now, &next);
-    }
     const T* z = logits_of(row);
     T* out = out_of(row);
     const uint32_t* mask = mask_of(m);
@@ -221,7 +215,9 @@ __global__ __launch_bounds__(kThreads) void adjust_kernel(AdjustArgs a) {
       for (int o = tid; o < n_ids; o += kThreads) one(o);
     }
     if (row + 1 < last) {
-      now = next;
+      if (row + 1 - rows_at == 64) { rows_at += 64; fetch_rows(); }
+      m_now = __builtin_amdgcn_readlane(masks, row + 1 - rows_at);
+      fetch(row + 1, m_now, &now);
       if (mine(token)) {                                 // the same in every thread
         __syncthreads();
         if (tid == 0) { s_count[token - s0] += 1; s_mark[(token - s0) >> 5] |= 1u << ((token - s0) & 31); }
@@ -279,8 +275,9 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
   const int threads = in->ld_history > kFewIds ? 1024 : 256;
   AdjustArgs a{*in, out, ld_out, ceil_div(in->V, 16 * threads), 1, 0};
   const int64_t groups = (int64_t)a.slices * in->B;
-  // a sequence's rows in parts until there are enough workgroups for every compute unit
-  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(in->M, in->B), (1024 / threads) * ctx->n_cu / groups));
+  // a row a workgroup where the table is quickly made, else a sequence's rows in parts until there is a workgroup for every compute unit
+  a.parts = ceil_div(in->M, in->B);
+  if (threads == 1024) a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(a.parts, ctx->n_cu / groups));
   if (in->n_bias > 0)
     for (a.bias_slots = 2; a.bias_slots < 2 * in->n_bias;) a.bias_slots *= 2;
   if (!grid_fits(groups * a.parts, threads)) return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: %d sequences of %d ids are too many for a launch", in->B, in->V);
