@@ -239,7 +239,7 @@ hipError_t launch(const AdjustArgs& a, hipStream_t stream) {
   return hipGetLastError();
 }
 
-constexpr int kFewIds = 4096;       // history up to which a slice's workgroup is a small one
+constexpr int kFewIds = 8192;       // ids of a history up to which workgroups are small
 
 }  // namespace
 }  // namespace otv

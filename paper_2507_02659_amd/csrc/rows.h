@@ -70,12 +70,16 @@ __device__ inline Vec<uint16_t>::Raw pack_vec(const float (&v)[8]) {
 // The elements of a vector whose bit is clear become -inf.
 __device__ inline void mask_vector(Vec<float>::Raw* x, uint32_t allowed) {
 #pragma unroll
-  for (int e = 0; e < 4; ++e) (*x)[e] = allowed >> e & 1 ? (*x)[e] : -INFINITY;
+  for (int e = 0; e < 4; ++e) {
+    const uint32_t keep = (uint32_t)__builtin_amdgcn_sbfe((int)allowed, e, 1);
+    (*x)[e] = __uint_as_float((__float_as_uint((*x)[e]) & keep) | (0xFF800000u & ~keep));
+  }
 }
 __device__ inline void mask_vector(Vec<uint16_t>::Raw* x, uint32_t allowed) {
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    const uint32_t keep = (allowed >> (2 * e) & 1 ? 0xFFFFu : 0u) | (allowed >> (2 * e + 1) & 1 ? 0xFFFF0000u : 0u);
+    const uint32_t low = (uint32_t)__builtin_amdgcn_sbfe((int)allowed, 2 * e, 1), high = (uint32_t)__builtin_amdgcn_sbfe((int)allowed, 2 * e + 1, 1);
+    const uint32_t keep = (low & 0xFFFFu) | (high & 0xFFFF0000u);
     (*x)[e] = ((*x)[e] & keep) | (0xFF80FF80u & ~keep);
   }
 }

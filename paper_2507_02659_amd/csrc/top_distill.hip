@@ -25,13 +25,18 @@ struct TopDistillArgs {
   int64_t ld_grad;
 };
 
-// Grid = rows.  A workgroup holds the vectors of its row that fit its registers (kHeld per thread) from the sums to the gradient and reads what is
-// beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie among the others a bitmap in LDS
+// Grid = rows.  A workgroup holds the vectors of its row that fit its registers (kHeld per thread; kWhole: all of them) from the sums to the
+// gradient and reads what is beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie among the others a bitmap in LDS
 // says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of their distance to their largest.
+constexpr int kFar = 4;           // vectors of a row that a thread asks for together where it does not hold them
 constexpr int kEntryWaves = OT_MAX_TEACHER_TOP / 64;
-constexpr int kGradWaves = 4;
-template <typename T, int kThreads, int kHeld, bool kGrad>
-__global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) void top_distill_kernel(TopDistillArgs a) {
+struct RowCoef {
+  double q, p;              // a kept id's gradient: q exp((z - top) / T) - p (its probability with the teacher)
+  float rest;               // of exp((z - mx) / T), mx the others' largest logit, in the others' gradients
+  int32_t nothing;          // the row adds nothing
+};
+template <typename T, int kThreads, int kHeld, bool kGrad, bool kWhole>
+__global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distill_kernel(TopDistillArgs a) {
   typedef typename Vec<T>::Raw Raw;
   constexpr int kVec = Vec<T>::kElems, kWaves = kThreads / 64;
   constexpr uint32_t kAll = (1u << kVec) - 1;
@@ -41,6 +46,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
   __shared__ double s_sum[kWaves], s_P[kEntryWaves], s_E[kEntryWaves], s_L[kEntryWaves];
   __shared__ float s_max[kWaves], s_top[kEntryWaves];
   __shared__ int s_twice;
+  __shared__ RowCoef s_coef;
   const ot_top_distill_in& in = a.in;
   const int row = (int)blockIdx.x, tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63, V = in.V;
   const T* z = static_cast<const T*>(in.logits) + (int64_t)row * in.ld;
@@ -49,7 +55,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
   const Raw* zv = reinterpret_cast<const Raw*>(z + split.head);
 
   // the teacher's entries; the row's vectors behind them on their way
-  const bool entries = wave < kEntryWaves;
+  const bool entries = wave < kEntryWaves && wave * 64 < in.n_top;   // (the same for a wavefront)
   int id = -1;
   float lp = -INFINITY;
   if (tid < in.n_top) {
@@ -102,6 +108,9 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
     const double P = wave_sum(p);
     const float top = wave_max(zk);
     if (lane == 0) { s_P[wave] = P; s_top[wave] = top; }
+  } else if (wave < kEntryWaves && lane == 0) {
+    s_P[wave] = s_E[wave] = s_L[wave] = 0.0;
+    s_top[wave] = -INFINITY;
   }
   __syncthreads();
 
@@ -125,12 +134,39 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
 #pragma unroll
     for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, v[e]);
   }
-  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) {
-    float v[kVec];
-    others(zv[at], split.head + at * kVec, v);
+  // what is not held, in one pass: a sum of its own per lane, whose reference moves up with the lane's largest
+  float far_ref = -INFINITY;
+  double far_sum = 0.0;
+  auto far_vectors = [&](auto take) {                    // each in turn, a few on their way together
+    for (int at0 = kHeld * kThreads + tid; at0 < split.vecs; at0 += kFar * kThreads) {
+      Raw x[kFar];
 #pragma unroll
-    for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, v[e]);
-  }
+      for (int i = 0; i < kFar; ++i) x[i] = zv[min(at0 + i * kThreads, split.vecs - 1)];
+#pragma unroll
+      for (int i = 0; i < kFar; ++i) {
+        const int at = at0 + i * kThreads;
+        if (at >= split.vecs) continue;
+        float v[kVec];
+        others(x[i], split.head + at * kVec, v);
+        take(v, split.head + at * kVec);
+      }
+    }
+  };
+  if constexpr (!kWhole)
+    far_vectors([&](float* v, int) {
+      float top_v = -INFINITY;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) top_v = fmaxf(top_v, v[e]);
+      if (top_v > far_ref) {
+        far_sum *= far_ref == -INFINITY ? 0.0 : exp_neg_fast(((double)far_ref - (double)top_v) / temp);
+        far_ref = top_v;
+      }
+      const float r = far_ref == -INFINITY ? 0.f : far_ref;
+#pragma unroll
+      for (int e = 0; e < kVec; ++e) v[e] = __builtin_amdgcn_exp2f((v[e] - r) * scale);
+      far_sum += (double)tree_sum<kVec>(v);
+    });
+  if (!kWhole) mx = fmaxf(mx, far_ref);
   mx = wave_max(mx);
   if (lane == 0) s_max[wave] = mx;
   __syncthreads();
@@ -153,11 +189,8 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
     Vec<T>::unpack(raw[k], v);
     add(v);
   }
-  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) {
-    float v[kVec];
-    others(zv[at], split.head + at * kVec, v);
-    add(v);
-  }
+  if (!kWhole && far_ref != -INFINITY) sum += far_sum * (far_ref == mx ? 1.0 : exp(((double)far_ref - (double)mx) / temp));
+  else if (!kWhole) sum += far_sum;                                   // (0, or NaN)
   sum = wave_sum(sum);
   if (lane == 0) s_sum[wave] = sum;
   // entries of the same id: the first of them has the id's part in Q and its gradient
@@ -178,34 +211,42 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
   }
   __syncthreads();
 
-  const double S_rest = wave_sum(lane < kWaves ? s_sum[lane] : 0.0);
   const double P = (s_P[0] + s_P[1]) + (s_P[2] + s_P[3]);
-  const double shift = ((double)mx - ref_top) / temp;    // (-inf: there are no others)
-  const double down = mx == -INFINITY && !isnan(S_rest) ? 0.0 : exp(shift);
-  const double S = ((s_E[0] + s_E[1]) + (s_E[2] + s_E[3])) + S_rest * down;
-  const double left = in.rest == OT_REST_BUCKET && P < 1.0 ? 1.0 - P : 0.0;
-  const bool nothing = S == 0.0 && top == -INFINITY && !broken;         // masked whole
   const double norm = in.rest == OT_REST_RENORMALISE ? P : 1.0;
-  if (tid == 0) {
+  if (wave == 0) {
+    const double S_rest = wave_sum(lane < kWaves ? s_sum[lane] : 0.0);
+    const double shift = ((double)mx - ref_top) / temp;  // (-inf: there are no others)
+    const double down = mx == -INFINITY && !isnan(S_rest) ? 0.0 : exp(shift);
+    const double S = ((s_E[0] + s_E[1]) + (s_E[2] + s_E[3])) + S_rest * down;
+    const double left = in.rest == OT_REST_BUCKET && P < 1.0 ? 1.0 - P : 0.0;
+    const bool nothing = S == 0.0 && top == -INFINITY && !broken;       // masked whole
     const double lnS = log(S);
     double loss = norm > 0.0 ? ((s_L[0] + s_L[1]) + (s_L[2] + s_L[3]) + P * (lnS - log(norm))) / norm : 0.0;
     if (left > 0.0) loss += left * (log(left) - (S_rest == 0.0 ? -INFINITY : log(S_rest) + shift - lnS));
     if (nothing) loss = 0.0;
-    a.loss[row] = broken || isnan(P) ? kNan : (float)loss;
-    if (a.kept) a.kept[row] = broken ? kNan : (float)P;
+    if (lane == 0) {
+      a.loss[row] = broken || isnan(P) ? kNan : (float)loss;
+      if (a.kept) a.kept[row] = broken ? kNan : (float)P;
+      if (kGrad) {
+        const double scaled = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;
+        const double mass = in.rest == OT_REST_BUCKET ? 1.0 : in.rest == OT_REST_RENORMALISE ? (P > 0.0 ? 1.0 : 0.0) : P;   // in front of q_v
+        double factor = down == 0.0 ? 0.0 : scaled * mass * down / S;
+        if (left > 0.0 && S_rest > 0.0) factor -= scaled * left / S_rest;
+        s_coef.rest = nothing ? 0.f : broken || isnan(S) ? kNan : (float)factor;
+        s_coef.nothing = nothing;
+        s_coef.q = scaled * mass / S;
+        s_coef.p = norm > 0.0 ? scaled / norm : 0.0;
+      }
+    }
   }
   if (!kGrad) return;
-  const double scaled = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;
-  const double mass = in.rest == OT_REST_BUCKET ? 1.0 : in.rest == OT_REST_RENORMALISE ? (P > 0.0 ? 1.0 : 0.0) : P;   // in front of q_v
+  __syncthreads();
+  const float c = s_coef.rest;
   if (first) {
-    double g = scaled * (mass * e / S - (norm > 0.0 ? p_id / norm : 0.0));
-    if (nothing || (zk == -INFINITY && !isnan(S))) g = 0.0;
+    double g = s_coef.q * e - s_coef.p * p_id;
+    if (s_coef.nothing || (zk == -INFINITY && !isnan(s_coef.q))) g = 0.0;
     store_one(grad + id, broken ? kNan : (float)g);
   }
-  // of exp((z - mx) / T) in the others' gradients
-  double factor = down == 0.0 ? 0.0 : scaled * mass * down / S;
-  if (left > 0.0 && S_rest > 0.0) factor -= scaled * left / S_rest;
-  const float c = nothing ? 0.f : broken || isnan(S) ? kNan : (float)factor;
   const float none = isnan(c) ? c : 0.f;                 // where the exponential is 0, also beside an infinite factor
   const bool vectors = ((reinterpret_cast<uintptr_t>(z) ^ reinterpret_cast<uintptr_t>(grad)) & 15) == 0;
   auto gradient = [&](float x) {
@@ -233,11 +274,7 @@ __global__ __launch_bounds__(kThreads, kHeld > 8 ? 4 : kGrad ? kGradWaves : 8) v
     Vec<T>::unpack(raw[k], v);
     put(v, split.head + at * kVec);
   }
-  for (int at = kHeld * kThreads + tid; at < split.vecs; at += kThreads) {
-    float v[kVec];
-    others(zv[at], split.head + at * kVec, v);
-    put(v, split.head + at * kVec);
-  }
+  if constexpr (!kWhole) far_vectors(put);
   if (has_edge && !edge_kept) store_one(grad + edge_id, gradient(edge));
 }
 
@@ -253,10 +290,10 @@ hipError_t launch(const TopDistillArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)a.in.M), dim3(threads), lds, stream, a);
     return hipGetLastError();
   };
-  if (a.in.V <= 256 * 4 * kVec) return go(top_distill_kernel<T, 256, 4, kGrad>, 256);
-  if (a.in.V <= 512 * 8 * kVec) return go(top_distill_kernel<T, 512, 8, kGrad>, 512);
-  if (a.in.V <= 1024 * 8 * kVec) return go(top_distill_kernel<T, 1024, 8, kGrad>, 1024);
-  return go(top_distill_kernel<T, 1024, 16, kGrad>, 1024);
+  if (a.in.V <= 256 * 4 * kVec) return go(top_distill_kernel<T, 256, 4, kGrad, true>, 256);
+  if (a.in.V <= 512 * 8 * kVec) return go(top_distill_kernel<T, 512, 8, kGrad, true>, 512);
+  if (a.in.V <= 1024 * 8 * kVec) return go(top_distill_kernel<T, 1024, 8, kGrad, true>, 1024);
+  return go(top_distill_kernel<T, 1024, 12, kGrad, false>, 1024);   // (the loss alone holds as many: it has the same bits)
 }
 
 int run(const char* who, const ot_ctx* ctx, const ot_top_distill_in* in, float* loss, float* kept, const float* grad_loss, void* grad, int64_t ld_grad, bool with_grad) {
