@@ -345,7 +345,7 @@ int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logpro
  * (ot_lm_head), the drafter's or another model's.                                                                 */
 #define OT_MAX_ADAPTER_RANK 256
 typedef struct ot_adapter_in {
-  int32_t        M, d, V;             /* rows; hidden size (OT_BF16: a multiple of 8); ids per row                 */
+  int32_t        M, d, V;             /* rows; hidden size, up to 2^24 (OT_BF16: a multiple of 8); ids per row, up to 2^30 */
   int32_t        rank;                /* 1..OT_MAX_ADAPTER_RANK; a multiple of 8 (OT_F32: of 4)                     */
   int32_t        n_adapters;
   int32_t        dtype;               /* OT_BF16 or OT_F32: type of hidden, down and up                             */

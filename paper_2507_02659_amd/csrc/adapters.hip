@@ -369,8 +369,8 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
     return ot_fail(OT_ERR_DTYPE, "ot_adapter_logits: types are OT_BF16 or OT_F32 (%d, %d)", in->dtype, in->logits_dtype);
   const int64_t size = in->logits_dtype == OT_BF16 ? 2 : 4;
   const int unit = in->dtype == OT_BF16 ? 8 : 4;
-  if (in->M < 0 || in->d < 1 || in->V < 1 || in->V > (1 << 30) || in->n_adapters < 1 || (in->logits && in->ld < in->V) || ld_out < in->V)
-    return ot_fail(OT_ERR_SHAPE, "ot_adapter_logits: need M >= 0, d >= 1, 1 <= V <= 2^30, n_adapters >= 1, ld and ld_out >= V (M = %d, d = %d, V = %d, n_adapters = %d)",
+  if (in->M < 0 || in->d < 1 || in->d > (1 << 24) || in->V < 1 || in->V > (1 << 30) || in->n_adapters < 1 || (in->logits && in->ld < in->V) || ld_out < in->V)
+    return ot_fail(OT_ERR_SHAPE, "ot_adapter_logits: need M >= 0, 1 <= d <= 2^24, 1 <= V <= 2^30, n_adapters >= 1, ld and ld_out >= V (M = %d, d = %d, V = %d, n_adapters = %d)",
                    in->M, in->d, in->V, in->n_adapters);
   if (in->rank < 1 || in->rank > OT_MAX_ADAPTER_RANK || in->rank % unit != 0 || (in->dtype == OT_BF16 && in->d % 8 != 0))
     return ot_fail(OT_ERR_SHAPE, "ot_adapter_logits: the rank is a multiple of %d up to %d, d of bf16 a multiple of 8 (rank = %d, d = %d)", unit, OT_MAX_ADAPTER_RANK,

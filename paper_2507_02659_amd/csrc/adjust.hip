@@ -275,9 +275,9 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
   const int threads = in->ld_history > kFewIds ? 1024 : 256;
   AdjustArgs a{*in, out, ld_out, ceil_div(in->V, 16 * threads), 1, 0};
   const int64_t groups = (int64_t)a.slices * in->B;
-  // a row a workgroup where the table is quickly made, else a sequence's rows in parts until there is a workgroup for every compute unit
-  a.parts = ceil_div(in->M, in->B);
-  if (threads == 1024) a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(a.parts, ctx->n_cu / groups));
+  // a row a workgroup where the table is quickly made (up to as many workgroups as keep every compute unit busy), else a sequence's rows in parts
+  // until there is a workgroup for every compute unit
+  a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(in->M, in->B), threads == 1024 ? ctx->n_cu / groups : (1 << 22) / groups));
   if (in->n_bias > 0)
     for (a.bias_slots = 2; a.bias_slots < 2 * in->n_bias;) a.bias_slots *= 2;
   if (!grid_fits(groups * a.parts, threads)) return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: %d sequences of %d ids are too many for a launch", in->B, in->V);

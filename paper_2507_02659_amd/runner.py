@@ -482,9 +482,14 @@ class Verifier:
         probability of the other ids.  temperature: the student's, one per row, or per sequence of row_off.  through_map: the ids are the target's and
         become draft ids by the verifier's direct map.  Returns device tensors [M]: loss, and kept, the probability that the teacher's ids have."""
         given = self._top_distill_in(logits, top_ids, top_logprobs, rest, temperature, row_off, through_map)
-        out = {"loss": self._empty((given.M,), torch.float32), "kept": self._empty((given.M,), torch.float32)}
-        ot.ot_top_distill_loss(self.ctx, given, out["loss"], out["kept"])
+        out, at = self._loss_and_kept(given.M)
+        ot.ot_top_distill_loss(self.ctx, given, at, at + 4 * given.M)
         return out
+
+    def _loss_and_kept(self, M):
+        """Both in one allocation (a call of few rows is bound by the host), and its address."""
+        memory = self._empty((2 * M,), torch.float32)
+        return {"loss": memory.as_strided((M,), (1,), 0), "kept": memory.as_strided((M,), (1,), M)}, memory.data_ptr()
 
     def top_distill_loss_grad(self, logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, *, rest: int = ot.OT_REST_DROP,
                               temperature: Optional[torch.Tensor] = None, row_off: Optional[torch.Tensor] = None, through_map: bool = False,
@@ -493,10 +498,10 @@ class Verifier:
         (ot_top_distill_loss_grad).  out: where the gradient goes (None: new; the logits themselves: in place)."""
         given = self._top_distill_in(logits, top_ids, top_logprobs, rest, temperature, row_off, through_map)
         grad, ld_grad = self._out(out, tuple(logits.shape), logits.dtype)
-        at = self._array("grad_loss", grad_loss, torch.float32, (given.M,))
-        got = {"loss": self._empty((given.M,), torch.float32), "kept": self._empty((given.M,), torch.float32), "grad": grad}
-        ot.ot_top_distill_loss_grad(self.ctx, given, got["loss"], got["kept"], at, grad.data_ptr(), ld_grad)
-        return got
+        g = self._array("grad_loss", grad_loss, torch.float32, (given.M,))
+        got, at = self._loss_and_kept(given.M)
+        ot.ot_top_distill_loss_grad(self.ctx, given, at, at + 4 * given.M, g, grad.data_ptr(), ld_grad)
+        return dict(got, grad=grad)
 
     def step_logprobs(self, inp: dict, *, from_logits: bool = False, n_top: int = 0, at_temperature: bool = True) -> dict:
         """Log-probabilities of the tokens that the last step on `inp` emitted, with entropy and alternatives, from the logits it left

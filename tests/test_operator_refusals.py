@@ -28,7 +28,7 @@ def _adapter(out=AT + (1 << 40), ld_out=100, **kw):
 
 def test_adapters():
     S, N, D = ot.OT_ERR_SHAPE, ot.OT_ERR_NULL, ot.OT_ERR_DTYPE
-    for kw in (dict(M=-1), dict(d=0), dict(V=0), dict(V=2 ** 30 + 1, ld=2 ** 31, ld_out=2 ** 31), dict(n_adapters=0), dict(ld=99), dict(ld_out=99), dict(rank=0),
+    for kw in (dict(M=-1), dict(d=0), dict(d=2 ** 24 + 8), dict(V=0), dict(V=2 ** 30 + 1, ld=2 ** 31, ld_out=2 ** 31), dict(n_adapters=0), dict(ld=99), dict(ld_out=99), dict(rank=0),
                dict(rank=264), dict(rank=4), dict(rank=12), dict(d=12), dict(rank=6, dtype=ot.OT_F32), dict(reserved=1), dict(hidden=AT + 8), dict(down=AT + 4),
                dict(up=AT + 2), dict(logits=AT + 2), dict(out=AT + 1), dict(out=AT + 4), dict(out=AT, ld_out=101), dict(out=AT + 4 * 99), dict(out=AT - 4 * 350),
                dict(V=2 ** 30, ld=2 ** 30, ld_out=2 ** 30, M=2048, out=1 << 50)):
