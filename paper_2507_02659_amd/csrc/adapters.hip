@@ -17,7 +17,7 @@ struct AdapterArgs {
   ot_adapter_in in;
   void* out;
   int64_t ld_out;
-  uint8_t* u;              // OT_BF16: [3][rows][depth] bfloat16, else [rows][depth] float32, rows = those of the launch
+  uint8_t* u;              // OT_BF16: [rows][3][depth] bfloat16, else [rows][depth] float32, rows = those of the launch
   int32_t row0, rows;      // the launch's rows
   int32_t depth;           // rank in whole 32s
 };
@@ -134,12 +134,11 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
         const int at = block * 64 + rows.row(i);         // (whole wavefronts come here)
         if (i < rows.n) {
           if constexpr (sizeof(W) == 2) {                // three parts, whose sum is u
-            uint16_t* to = reinterpret_cast<uint16_t*>(a.u) + (int64_t)at * a.depth + rank;
-            const int64_t part = (int64_t)a.rows * a.depth;
+            uint16_t* to = reinterpret_cast<uint16_t*>(a.u) + (int64_t)at * 3 * a.depth + rank;
             const float hi = (float)(__bf16)u, mid = (float)(__bf16)(u - hi);
             store_one(to, hi);
-            store_one(to + part, mid);
-            store_one(to + 2 * part, u - hi - mid);
+            store_one(to + a.depth, mid);
+            store_one(to + 2 * a.depth, u - hi - mid);
           } else {
             reinterpret_cast<float*>(a.u)[(int64_t)at * a.depth + rank] = u;
           }
@@ -150,7 +149,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
   }
 }
 
-// Grid = strips of ids x blocks of 64 rows.  A tile's sums are formed with the matrix of the ids as the first operand, 64 ids a wavefront, and go
+// Grid = strips of ids x blocks of 64 rows.  A tile's sums are formed 64 ids a wavefront and go
 // through LDS to the logits, which a wavefront reads and writes row by row in whole 16-byte vectors, wherever the row starts: a strip has the
 // vectors that begin in its kStride ids, and computes the kVec - 1 ids more that the last of them may reach.  In LDS a row is shifted so that
 // its vectors are whole there too.  The next tile's logits are on their way while one is taken.
@@ -228,13 +227,15 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
   auto load_operands = [&](const Tile& of, int k0) {
     if (of.adapter < 0) return;
     const int i = of.q + (lane & 15);
-    const uint32_t at = (uint32_t)((block * 64 + __shfl(of.order, i < of.n ? i : 0)) * a.depth + (lane >> 4) * (Op::kDepth / 4));
+    // (depth: whole 32s, zeros behind the rank; of up to two blocks of 32 a constant, so that the loads share an address)
+    const int depth = kParts == 3 && kBlocks <= 2 ? kBlocks * 32 : a.depth;
+    const W* of_row = reinterpret_cast<const W*>(a.u) + (size_t)(uint32_t)((block * 64 + __shfl(of.order, i < of.n ? i : 0)) * kParts * depth + (lane >> 4) * (Op::kDepth / 4));
 #pragma unroll
     for (int kb = 0; kb < kBlocks; ++kb)
 #pragma unroll
       for (int part = 0; part < kParts; ++part)
-        if (kBlocks <= 2 || k0 + kb * Op::kDepth < a.depth)   // (depth: whole 32s, zeros behind the rank)
-          u[kb][part] = *reinterpret_cast<const Frag*>(reinterpret_cast<const W*>(a.u) + (size_t)(uint32_t)(part * a.rows * a.depth + k0 + kb * Op::kDepth) + at);
+        if (kBlocks <= 2 || k0 + kb * Op::kDepth < depth)
+          u[kb][part] = *reinterpret_cast<const Frag*>(of_row + part * depth + k0 + kb * Op::kDepth);
         else
           u[kb][part] = Frag{};
     if (of.adapter == loaded && in.rank <= kChunk) return;

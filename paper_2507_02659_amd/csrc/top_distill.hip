@@ -134,8 +134,9 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
 #pragma unroll
     for (int e = 0; e < kVec; ++e) mx = fmaxf(mx, v[e]);
   }
-  // what is not held, in one pass: a sum of its own per lane, whose reference moves up with the lane's largest
-  float far_ref = -INFINITY;
+  // what is not held, in one pass: a sum of its own per lane, whose reference starts at the wavefront's largest that is held, and moves up with
+  // the lane's largest (rarely: from -inf on, in every second vector of some lane, it cost 512 rows of 128256 ids 7 us)
+  float far_ref = kWhole ? -INFINITY : wave_max(mx);
   double far_sum = 0.0;
   auto far_vectors = [&](auto take) {                    // each in turn, a few on their way together
     for (int at0 = kHeld * kThreads + tid; at0 < split.vecs; at0 += kFar * kThreads) {
@@ -158,7 +159,7 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
 #pragma unroll
       for (int e = 0; e < kVec; ++e) top_v = fmaxf(top_v, v[e]);
       if (top_v > far_ref) {
-        far_sum *= far_ref == -INFINITY ? 0.0 : exp_neg_fast(((double)far_ref - (double)top_v) / temp);
+        far_sum *= far_ref == -INFINITY ? 0.0 : exp(((double)far_ref - (double)top_v) / temp);
         far_ref = top_v;
       }
       const float r = far_ref == -INFINITY ? 0.f : far_ref;
