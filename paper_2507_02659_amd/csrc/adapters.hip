@@ -149,7 +149,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
   }
 }
 
-// Grid = strips of ids x blocks of 64 rows.  A tile's sums are formed 64 ids a wavefront and go
+// Grid = strips of ids x slots x blocks of 64 rows; a workgroup takes every slots-th tile of its block.  A tile's sums are formed 64 ids a wavefront and go
 // through LDS to the logits, which a wavefront reads and writes row by row in whole 16-byte vectors, wherever the row starts: a strip has the
 // vectors that begin in its kStride ids, and computes the kVec - 1 ids more that the last of them may reach.  In LDS a row is shifted so that
 // its vectors are whole there too.  The next tile's logits are on their way while one is taken.
@@ -158,7 +158,7 @@ constexpr int kPitch = kStrip + kFront + 4;              // four rows on another
 template <typename T>
 constexpr int kStride = kStrip - Vec<T>::kElems;
 template <typename W, typename T, int kBlocks>
-__global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_up_kernel(AdapterArgs a, int strips) {
+__global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_up_kernel(AdapterArgs a, int strips, int slots) {
   typedef Operand<W> Op;
   typedef typename Op::Frag Frag;
   typedef typename Vec<T>::Raw Raw;
@@ -166,7 +166,7 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
   constexpr bool kLargest = kBlocks == 4;
   const ot_adapter_in& in = a.in;
   const int wave = uniform((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
-  const int strip = (int)(blockIdx.x % (unsigned)strips), block = (int)(blockIdx.x / (unsigned)strips);
+  const int strip = (int)(blockIdx.x % (unsigned)strips), t0 = (int)(blockIdx.x / (unsigned)strips), slot = t0 % slots, block = t0 / slots;
   __shared__ alignas(16) float s_sum[2][16][kPitch];
   const int v0 = strip * kStride<T>, own = wave * 64;
   const bool edges = strip == 0 || v0 + kStrip >= in.V;
@@ -186,12 +186,18 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
   Block rows(a, block, lane);
   // A tile: its adapter (-3: none is left), the adapter's rows in the block, which they are, the tile's first.
   struct Tile { int adapter, n, order, q; };
-  auto after = [&](const Tile& t) {
+  auto behind = [&](const Tile& t) {
     if (t.q + 16 < t.n) return Tile{t.adapter, t.n, t.order, t.q + 16};
     do {
       if (!rows.next()) return Tile{-3, 0, 0, 0};
     } while (rows.now == -1 && a.out == in.logits);      // in place there is nothing to do for rows without an adapter
     return Tile{rows.now, rows.n, rows.order, 0};
+  };
+  int seen = 0;
+  auto after = [&](Tile t) {                             // the next that is this workgroup's
+    do t = behind(t);
+    while (t.adapter != -3 && seen++ % slots != slot);
+    return t;
   };
   auto load_base = [&](const Tile& of, Raw (&base)[kRows][kTurns]) {
 #pragma unroll
@@ -337,23 +343,25 @@ __global__ __launch_bounds__(64 * kUpWaves, kBlocks <= 2 ? 4 : 2) void adapter_u
 }
 
 template <typename W, typename T>
-hipError_t launch_up(const AdapterArgs& a, hipStream_t stream) {
+hipError_t launch_up(const AdapterArgs& a, int n_cu, hipStream_t stream) {
   const int blocks = ceil_div(a.in.rank, Operand<W>::kDepth), strips = ceil_div(a.in.V, kStride<T>), of_rows = ceil_div(a.rows, 64);
-  const dim3 grid((unsigned)strips * (unsigned)of_rows);
-  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kUpWaves), 0, stream, a, strips); return hipGetLastError(); };
+  // a block's tiles one after the other, unless that leaves compute units without a workgroup
+  const int slots = std::max(1, std::min({a.rows, 16, (int)(n_cu / ((int64_t)strips * of_rows))}));
+  const dim3 grid((unsigned)strips * (unsigned)slots * (unsigned)of_rows);
+  auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(64 * kUpWaves), 0, stream, a, strips, slots); return hipGetLastError(); };
   if (blocks <= 1) return go(adapter_up_kernel<W, T, 1>);
   if (blocks <= 2) return go(adapter_up_kernel<W, T, 2>);
   return go(adapter_up_kernel<W, T, 4>);                 // also of more
 }
 
 template <typename W>
-hipError_t launch_adapters(const AdapterArgs& a, hipStream_t stream) {
+hipError_t launch_adapters(const AdapterArgs& a, int n_cu, hipStream_t stream) {
   const int blocks = ceil_div(a.rows, 64);
   const int slots = std::min({a.rows, 16, std::min(a.in.n_adapters, 64) + 3});
   hipLaunchKernelGGL(adapter_down_kernel<W>, dim3((unsigned)(blocks * (a.depth / 16) * slots)), dim3(64 * kDownWaves), 0, stream, a, slots);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  return a.in.logits_dtype == OT_BF16 ? launch_up<W, uint16_t>(a, stream) : launch_up<W, float>(a, stream);
+  return a.in.logits_dtype == OT_BF16 ? launch_up<W, uint16_t>(a, n_cu, stream) : launch_up<W, float>(a, n_cu, stream);
 }
 
 }  // namespace
@@ -393,7 +401,7 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
   if (const int bad = ot_check_device(ctx, "ot_adapter_logits")) return bad;
   for (int row0 = 0; row0 < in->M; row0 += kAdapterRows) {
     const AdapterArgs a{*in, out, ld_out, ctx->adapter_u, row0, std::min(in->M - row0, kAdapterRows), ceil_div(in->rank, 32) * 32};
-    const hipError_t e = in->dtype == OT_BF16 ? launch_adapters<uint16_t>(a, ctx->stream) : launch_adapters<float>(a, ctx->stream);
+    const hipError_t e = in->dtype == OT_BF16 ? launch_adapters<uint16_t>(a, ctx->n_cu, ctx->stream) : launch_adapters<float>(a, ctx->n_cu, ctx->stream);
     if (e != hipSuccess) return ot_fail_hip(e, "ot_adapter_logits: launch");
   }
   return OT_OK;
