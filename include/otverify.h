@@ -365,7 +365,7 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
 
 /* ---- what requests ask of their logits: penalties, biases, masks ------------------------------------------------- */
 /* For the rows of a batch of windows (or single tokens), before a step or ot_token_logprobs reads them.  Of row j of sequence b, for
- * every id v, in this order, in 64 bits and rounded once:
+ * every id v, in this order, in 64 bits, then rounded to the logits' type (bfloat16 through float32):
  *   1. repetition: v occurs in the sequence's history or among the j tokens of its window in front of the row: z = z / repetition[b]
  *      where z > 0, else z * repetition[b];
  *   2. n = how often v occurs in the history behind the prompt and among those j tokens:

@@ -27,7 +27,13 @@ struct TopDistillArgs {
 
 // Grid = rows.  A workgroup holds the vectors of its row that fit its registers (kHeld per thread; kWhole: all of them) from the sums to the
 // gradient and reads what is beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie among the others a bitmap in LDS
-// says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of their distance to their largest.
+// says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of their distance to their largest,
+// added in 64 bits.
+// 512 rows of 128256 float32 logits with 50 ids, gradient included, 116 to 119 us (525 MB, 4.5 TB/s; a copy of the logits takes 99): bound by memory,
+// and by the 60 % of a row that is read again, from a cache.  16 vectors held 119 to 133 us, 8 123, in workgroups of 512 threads that hold 32 149 (one
+// workgroup, 8 wavefronts, per compute unit).  2000 rows of 32003 in bfloat16 with 256 ids, the loss alone, 42 us (3.1 TB/s): bound by its
+// instructions, 19 per logit, a third of them for the entries and the sums' ends; 256 threads that hold 16 vectors 43.
+// 128 rows of 32000 in bfloat16 13 us: one chain of loads, four barriers and 64-bit exponentials.
 constexpr int kFar = 4;           // vectors of a row that a thread asks for together where it does not hold them
 constexpr int kEntryWaves = OT_MAX_TEACHER_TOP / 64;
 struct RowCoef {
@@ -291,6 +297,7 @@ hipError_t launch(const TopDistillArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)a.in.M), dim3(threads), lds, stream, a);
     return hipGetLastError();
   };
+  // the smallest workgroup that holds the row, else the largest
   if (a.in.V <= 256 * 4 * kVec) return go(top_distill_kernel<T, 256, 4, kGrad, true>, 256);
   if (a.in.V <= 512 * 8 * kVec) return go(top_distill_kernel<T, 512, 8, kGrad, true>, 512);
   if (a.in.V <= 1024 * 8 * kVec) return go(top_distill_kernel<T, 1024, 8, kGrad, true>, 1024);

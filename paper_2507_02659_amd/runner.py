@@ -350,7 +350,7 @@ class Verifier:
                       repetition: Optional[torch.Tensor] = None, frequency: Optional[torch.Tensor] = None, presence: Optional[torch.Tensor] = None,
                       bias_ids: Optional[torch.Tensor] = None, bias: Optional[torch.Tensor] = None, masks: Optional[torch.Tensor] = None,
                       mask_of_row: Optional[torch.Tensor] = None, out: Optional[torch.Tensor] = None) -> torch.Tensor:
-        """Penalties for repeated tokens, biases and masks on rows of logits [M, V] (ot_adjust_logits), in 64 bits and rounded once.
+        """Penalties for repeated tokens, biases and masks on rows of logits [M, V] (ot_adjust_logits).
 
         row_off: int32 [B + 1] first rows of the sequences (None: every row is one).  history: int32 [B, L], the first n_history of a row count
         (int32 [B]; None: all) and of these the first n_prompt are its prompt (int32 [B]; None: none).  window: int32 [M] proposed tokens (a step's
