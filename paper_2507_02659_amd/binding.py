@@ -246,7 +246,9 @@ def _ptr(x) -> Optional[int]:
 
 def _on_gpu(x) -> Optional[int]:
     """_ptr of what the device reads or writes: a tensor or array in host memory is refused, whose address a kernel would take for its own."""
-    if x is not None and not isinstance(x, int) and not getattr(x, "is_cuda", False):
+    if x is None or isinstance(x, int):
+        return x
+    if not getattr(x, "is_cuda", False):
         raise ValueError(f"device memory is needed, not {type(x).__name__} in host memory")
     return _ptr(x)
 

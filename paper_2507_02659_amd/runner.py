@@ -37,6 +37,10 @@ def read_device(ptr: int, count: int, np_dtype) -> np.ndarray:
     return out
 
 
+_CODES = {torch.bfloat16: ot.OT_BF16, torch.float32: ot.OT_F32}
+_NO_RESERVED = (C.c_int32 * 2)()
+
+
 @dataclass
 class QuantWeights:
     """A target head of 4-bit weights as device tensors: W[k, v] = scales[k // group, v] * (code[k, v] - zeros[k // group, v])."""
@@ -65,14 +69,17 @@ class Adapters:
     scale: Optional[torch.Tensor] = None            # float32 [n]; None: 1
 
     def check(self):
-        if self.down.dtype not in (torch.bfloat16, torch.float32) or self.up.dtype != self.down.dtype:
+        down, up, scale = self.down, self.up, self.scale
+        if down.dtype not in _CODES or up.dtype != down.dtype:
             raise TypeError("adapters are bfloat16 or float32, both matrices alike")
-        if self.down.dim() != 3 or self.up.dim() != 3 or self.up.shape[0] != self.down.shape[0] or self.up.shape[2] != self.down.shape[1]:
-            raise ValueError(f"adapters are [n, rank, d] and [n, V, rank], not {tuple(self.down.shape)} and {tuple(self.up.shape)}")
-        if not self.down.is_contiguous() or not self.up.is_contiguous():
+        a, b = down.shape, up.shape
+        if len(a) != 3 or len(b) != 3 or a[0] != b[0] or a[1] != b[2]:
+            raise ValueError(f"adapters are [n, rank, d] and [n, V, rank], not {tuple(a)} and {tuple(b)}")
+        if not down.is_contiguous() or not up.is_contiguous():
             raise ValueError("adapters are contiguous")
-        if self.scale is not None and (self.scale.dtype != torch.float32 or tuple(self.scale.shape) != (self.down.shape[0],) or not self.scale.is_contiguous()):
-            raise ValueError(f"scale is float32 [{self.down.shape[0]}]")
+        if scale is not None and (scale.dtype != torch.float32 or scale.shape != a[:1] or not scale.is_contiguous()):
+            raise ValueError(f"scale is float32 [{a[0]}]")
+        return a[0], a[1], a[2], b[1]
 
 
 class Verifier:
@@ -296,11 +303,13 @@ class Verifier:
         return logits if adapters is None else self.adapter_logits(hidden, adapters, adapter_of_row, logits, out=logits)
 
     def _rows(self, name, logits):
-        """Type, rows, ids and distance of rows of logits."""
+        """Type, rows, ids and distance of rows of logits.  (Calls of few rows are bound by the host: here and below nothing is asked for twice.)"""
         M, V = logits.shape
-        if logits.dtype not in (torch.bfloat16, torch.float32) or (V > 1 and logits.stride(1) != 1):
+        between, beside = logits.stride()
+        code = _CODES.get(logits.dtype)
+        if code is None or (beside != 1 and V > 1):
             raise ValueError(f"{name} are [M, V] bfloat16 or float32 with neighbouring ids next to each other")
-        return ot.OT_BF16 if logits.dtype == torch.bfloat16 else ot.OT_F32, M, V, logits.stride(0) if M > 1 else V
+        return code, M, V, between if M > 1 else V
 
     def _array(self, name, t, dtype, shape):
         """Address of an argument that is an array of this type and shape, or None."""
@@ -316,22 +325,22 @@ class Verifier:
                        out: Optional[torch.Tensor] = None) -> torch.Tensor:
         """Rows of logits [M, V] plus what each row's adapter makes of its hidden row [M, d] (ot_adapter_logits); without logits that alone, in
         float32.  adapter_of_row: int32 [M], -1: none.  out: where to, shaped and typed like the logits (these themselves: in place)."""
-        adapters.check()
-        n, rank, d = adapters.down.shape
-        V = adapters.up.shape[1]
-        if hidden.dim() != 2 or hidden.shape[1] != d or hidden.dtype != adapters.down.dtype or not hidden.is_contiguous():
-            raise ValueError(f"hidden rows are [M, {d}] of the adapters' type, contiguous, not {tuple(hidden.shape)} {hidden.dtype}")
-        M = hidden.shape[0]
-        if logits is not None and tuple(logits.shape) != (M, V):
-            raise ValueError(f"logits are [{M}, {V}], not {tuple(logits.shape)}")
-        code, _, _, ld = (ot.OT_F32, M, V, 0) if logits is None else self._rows("logits", logits)
+        n, rank, d, V = adapters.check()
+        down, up, dtype = adapters.down, adapters.up, hidden.dtype
+        if hidden.dim() != 2 or hidden.shape[1] != d or dtype != down.dtype or not hidden.is_contiguous():
+            raise ValueError(f"hidden rows are [M, {d}] of the adapters' type, contiguous, not {tuple(hidden.shape)} {dtype}")
+        M, dev, code, ld = hidden.shape[0], self.device, ot.OT_F32, 0
+        if logits is not None:
+            code, rows, ids, ld = self._rows("logits", logits)
+            if rows != M or ids != V:
+                raise ValueError(f"logits are [{M}, {V}], not {tuple(logits.shape)}")
         out, ld_out = self._out(out, (M, V), torch.float32 if logits is None else logits.dtype)
-        dev = self.device
-        if self.stream is not None or hidden.device != dev or adapters.down.device != dev or adapters.up.device != dev or (logits is not None and logits.device != dev):
-            self._here(hidden=hidden, down=adapters.down, up=adapters.up, logits=logits)
-        given = ot.ot_adapter_in(M, d, V, rank, n, ot.OT_BF16 if hidden.dtype == torch.bfloat16 else ot.OT_F32, code, 0, ld, hidden.data_ptr(),
-                                 adapters.down.data_ptr(), adapters.up.data_ptr(), self._array("scale", adapters.scale, torch.float32, (n,)),
-                                 self._array("adapter_of_row", adapter_of_row, torch.int32, (M,)), None if logits is None else logits.data_ptr())
+        if self.stream is not None or hidden.device != dev or down.device != dev or up.device != dev or (logits is not None and logits.device != dev):
+            self._here(hidden=hidden, down=down, up=up, logits=logits)
+        at = self._array
+        given = ot.ot_adapter_in(M, d, V, rank, n, _CODES[dtype], code, 0, ld, hidden.data_ptr(), down.data_ptr(), up.data_ptr(),
+                                 at("scale", adapters.scale, torch.float32, (n,)), at("adapter_of_row", adapter_of_row, torch.int32, (M,)),
+                                 None if logits is None else logits.data_ptr())
         ot.ot_adapter_logits(self.ctx, given, out.data_ptr(), ld_out)
         return out
 
@@ -377,12 +386,14 @@ class Verifier:
             n_masks, words = masks.shape
             if mask_of_row is None and n_masks < M:
                 raise ValueError(f"without mask_of_row every row has its own mask ({n_masks} for {M} rows)")
-        i32, f32, at = torch.int32, torch.float32, self._array
-        given = ot.ot_adjust_in(M, V, B, code, n_bias, n_masks, (C.c_int32 * 2)(), ld, L, words, logits.data_ptr(), at("row_off", row_off, i32, (B + 1,)),
-                                at("history", history, i32, (B, L)), at("n_history", n_history, i32, (B,)), at("n_prompt", n_prompt, i32, (B,)),
-                                at("window", window, i32, (M,)), at("repetition", repetition, f32, (B,)), at("frequency", frequency, f32, (B,)),
-                                at("presence", presence, f32, (B,)), at("bias_ids", bias_ids, i32, (B, n_bias)), at("bias", bias, f32, (B, n_bias)),
-                                at("masks", masks, i32, (n_masks, words)), at("mask_of_row", mask_of_row, i32, (M,)))
+        i32, f32, at, each = torch.int32, torch.float32, self._array, (B,)
+        given = ot.ot_adjust_in(M, V, B, code, n_bias, n_masks, _NO_RESERVED, ld, L, words, logits.data_ptr(), row_off if row_off is None else at("row_off", row_off, i32, (B + 1,)),
+                                at("history", history, i32, (B, L)), at("n_history", n_history, i32, each), at("n_prompt", n_prompt, i32, each),
+                                window if window is None else at("window", window, i32, (M,)), at("repetition", repetition, f32, each),
+                                at("frequency", frequency, f32, each), at("presence", presence, f32, each),
+                                *((None, None) if bias is None else (at("bias_ids", bias_ids, i32, (B, n_bias)), at("bias", bias, f32, (B, n_bias)))),
+                                masks if masks is None else at("masks", masks, i32, (n_masks, words)),
+                                mask_of_row if mask_of_row is None else at("mask_of_row", mask_of_row, i32, (M,)))
         ot.ot_adjust_logits(self.ctx, given, out.data_ptr(), ld_out)
         return out
 
@@ -463,17 +474,18 @@ class Verifier:
 
     def _top_distill_in(self, logits, top_ids, top_logprobs, rest, temperature, row_off, through_map):
         code, M, V, ld = self._rows("logits", logits)
-        if top_ids.dim() != 2 or top_ids.shape[0] != M or top_ids.shape != top_logprobs.shape:
-            raise ValueError(f"top_ids and top_logprobs are [{M}, n]")
+        shape = top_ids.shape
+        if len(shape) != 2 or shape[0] != M:
+            raise ValueError(f"top_ids is {[M, 'n']}")
         if through_map and V != self.V_d:
             raise ValueError(f"through the direct map the logits are the drafter's, [M, {self.V_d}]")
         B = M if row_off is None else max(0, row_off.numel() - 1)
         if self.stream is not None or logits.device != self.device:
             self._here(logits=logits)
-        shape, at = tuple(top_ids.shape), self._array
+        at = self._array
         return ot.ot_top_distill_in(M, V, code, shape[1], rest, 1 if through_map else 0, B, 0, ld, logits.data_ptr(), at("top_ids", top_ids, torch.int32, shape),
                                     at("top_logprobs", top_logprobs, torch.float32, shape), at("temperature", temperature, torch.float32, (B,)),
-                                    at("row_off", row_off, torch.int32, (B + 1,)))
+                                    None if row_off is None else at("row_off", row_off, torch.int32, (B + 1,)))
 
     def top_distill_loss(self, logits: torch.Tensor, top_ids: torch.Tensor, top_logprobs: torch.Tensor, *, rest: int = ot.OT_REST_DROP,
                          temperature: Optional[torch.Tensor] = None, row_off: Optional[torch.Tensor] = None, through_map: bool = False) -> dict:
@@ -497,11 +509,12 @@ class Verifier:
         """top_distill_loss, and "grad": the gradient of sum grad_loss * loss (float32 [M]; None: 1) with respect to the logits, in their type
         (ot_top_distill_loss_grad).  out: where the gradient goes (None: new; the logits themselves: in place)."""
         given = self._top_distill_in(logits, top_ids, top_logprobs, rest, temperature, row_off, through_map)
-        grad, ld_grad = self._out(out, tuple(logits.shape), logits.dtype)
+        grad, ld_grad = self._out(out, (given.M, given.V), logits.dtype)
         g = self._array("grad_loss", grad_loss, torch.float32, (given.M,))
         got, at = self._loss_and_kept(given.M)
         ot.ot_top_distill_loss_grad(self.ctx, given, at, at + 4 * given.M, g, grad.data_ptr(), ld_grad)
-        return dict(got, grad=grad)
+        got["grad"] = grad
+        return got
 
     def step_logprobs(self, inp: dict, *, from_logits: bool = False, n_top: int = 0, at_temperature: bool = True) -> dict:
         """Log-probabilities of the tokens that the last step on `inp` emitted, with entropy and alternatives, from the logits it left

@@ -93,6 +93,15 @@ def test_numbers_of_rows(v, M):
     _check(v, rng, M, 4, 8, 16, 70, torch.float32, adapter=np.repeat(np.arange(-1, 5), -(-M // 6))[:M] % 5 - 1)
 
 
+def test_few_strips_and_many_tiles(v):
+    """Blocks whose tiles are shared out over workgroups: few ids, many adapters, rows in any order."""
+    rng = np.random.default_rng(11)
+    for M, n, R, V in ((56, 5, 64, 2251), (64, 64, 16, 1100), (130, 20, 136, 700), (64, 1, 16, 513), (33, 7, 8, 9)):
+        for logits_type in (torch.float32, torch.bfloat16):
+            _check(v, rng, M, n, R, 48, V, torch.bfloat16, logits_type)
+            _check(v, rng, M, n, R, 48, V, torch.float32, logits_type)
+
+
 def test_many_adapters(v):
     """A row each, all in one block and in many; an adapter that no row has."""
     rng = np.random.default_rng(3)

@@ -101,7 +101,7 @@ def test_lengths(v, V, dtype):
 def test_long_histories(v, V):
     """The larger workgroups: slices of 16384 ids, of ragged windows."""
     rng = np.random.default_rng(V)
-    M, kw = _all(rng, 3, [2, 70, 1], V, L=4500, n_bias=9)
+    M, kw = _all(rng, 3, [2, 70, 1], V, L=8500, n_bias=9)
     _check(v, _logits(rng, M, V), **kw)
     _check(v, _logits(rng, M, V, torch.bfloat16), **kw)
 
@@ -183,7 +183,7 @@ def test_masks_and_special_values(v, dtype):
 
 
 @pytest.mark.parametrize("n_bias", [1, 2, 3, 64, 300, 4096])
-@pytest.mark.parametrize("L", [3, 6000])
+@pytest.mark.parametrize("L", [3, 8200])
 def test_bias_lists(v, n_bias, L):
     """Lists up to the longest, of ids in one place and all over, with both sizes of workgroups."""
     rng = np.random.default_rng(n_bias)
@@ -268,10 +268,10 @@ def test_from_graphs_and_on_another_stream():
                    max_batch=1, max_k=0, stream=stream)
     with torch.cuda.stream(stream):
         made = []
-        for rows, V in (([9] * 4, 32003), ([1], 9000)):
+        for rows, V, L in (([9] * 4, 32003, 40), ([1], 9000, 40), ([2, 3], 20011, 9000)):   # (the last: the larger workgroups)
             sets = []
             for _ in range(3):
-                M, kw = _all(rng, len(rows), rows, V, n_masks=3)
+                M, kw = _all(rng, len(rows), rows, V, L=L, n_masks=3)
                 sets.append((_logits(rng, M, V), {n: _put(x) for n, x in kw.items()}))
             eager = [ver.adjust_logits(z, **kw).clone() for z, kw in sets]
             z, kw = sets[0][0].clone(), {n: x.clone() for n, x in sets[0][1].items()}

@@ -319,7 +319,7 @@ def test_from_graphs_and_on_another_stream():
     ver = _verifier(stream=stream)
     with torch.cuda.stream(stream):
         made = []
-        for M, V, n in ((1, 50001, 20), (40, 9000, 256)):
+        for M, V, n in ((1, 50001, 20), (40, 9000, 256), (2, 600_000, 9)):
             sets = []
             for _ in range(3):
                 z, ids, lps = _case(rng, M, V, n)
