@@ -92,9 +92,9 @@ struct Block {
 };
 
 // Grid = slots x 16s of the rank x blocks of 64 rows.  A workgroup takes every slots-th tile of its block; its 16 wavefronts share the hidden
-// indices and add their sums in LDS, in one order.  Bound by what one compute unit reads, 16 rows of both sides: 1024 hidden indices 3.5 us, 4096
-// 11.4 (144 rows, rank 16).  Indices split over four workgroups, whose sums the last one adds, took 10.0 and for 2000 rows of 2056 indices 16.4
-// instead of 13.3; eight steps of loads ahead instead of four changed nothing.
+// indices and add their sums in LDS, in one order.  3.5 us with one row of 1024 indices, 11.4 with 144 of 4096 (rank 16), 13.4 with 2000 of 2056 (rank
+// 64): behind a launch that left many logits to write it waits for the memory (with every load from a cached line the times are the same).  Indices
+// split over four workgroups, whose sums the last one adds, took 10.0 and 16.4; eight steps of loads ahead instead of four changed nothing.
 constexpr int kDownWaves = 16, kDownSteps = 4;
 template <typename W>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterArgs a, int slots) {
