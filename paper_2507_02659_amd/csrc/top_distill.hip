@@ -26,9 +26,9 @@ struct TopDistillArgs {
 };
 
 // Grid = rows.  A workgroup holds the vectors of its row that fit its registers (kHeld per thread; kWhole: all of them) from the sums to the
-// gradient and reads what is beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie among the others a bitmap in LDS
-// says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of their distance to their largest,
-// added in 64 bits.
+// gradient and reads what is beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie
+// among the others a bitmap in LDS says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of
+// their distance to their largest, added in 64 bits.
 // 512 rows of 128256 float32 logits with 50 ids, gradient included, 116 to 119 us (525 MB, 4.5 TB/s; a copy of the logits takes 99): bound by memory,
 // and by the 60 % of a row that is read again, from a cache.  16 vectors held 119 to 133 us, 8 123, in workgroups of 512 threads that hold 32 149 (one
 // workgroup, 8 wavefronts, per compute unit).  2000 rows of 32003 in bfloat16 with 256 ids, the loss alone, 42 us (3.1 TB/s): bound by its
@@ -232,7 +232,7 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
     if (left > 0.0) loss += left * (log(left) - (S_rest == 0.0 ? -INFINITY : log(S_rest) + shift - lnS));
     if (nothing) loss = 0.0;
     if (lane == 0) {
-      a.loss[row] = broken || isnan(P) ? kNan : (float)loss;
+      a.loss[row] = broken || isnan(S) ? kNan : (float)loss;   // (S: also where no p is above 0)
       if (a.kept) a.kept[row] = broken ? kNan : (float)P;
       if (kGrad) {
         const double scaled = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;

@@ -165,6 +165,19 @@ def test_masks_and_special_values(v, V, dtype, rest):
 
 
 @pytest.mark.parametrize("rest", RESTS)
+def test_rows_that_hold_a_nan_and_no_probability(v, rest):
+    """The row is NaN whether its ids ask for it or not."""
+    rng = np.random.default_rng(2)
+    z, ids, lps = _case(rng, 4, 70, 5)
+    lps[:] = -np.inf
+    z[0, ids[0, 1]] = float("nan")
+    z[1, int((torch.arange(70, device=DEV)[:, None] != _put(ids[1])[None]).all(1).nonzero()[0])] = float("nan")
+    z[2, ids[2, 0]] = float("inf")
+    got = _check(v, z, ids, lps, None, rest)
+    assert got["loss"][:3].isnan().all() and not got["loss"][3].isnan()
+
+
+@pytest.mark.parametrize("rest", RESTS)
 def test_tiny_temperatures(v, rest):
     """Gradients past float32 and exponentials of 0 beside them: what is masked or too far to be reached stays 0."""
     rng = np.random.default_rng(1)
