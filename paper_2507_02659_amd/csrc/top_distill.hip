@@ -31,7 +31,7 @@ struct TopDistillArgs {
 // their distance to their largest, added in 64 bits.
 // 512 rows of 128256 float32 logits with 50 ids, gradient included, 116 to 119 us (525 MB, 4.5 TB/s; a copy of the logits takes 99): bound by memory,
 // and by the 60 % of a row that is read again, from a cache.  16 vectors held 119 to 133 us, 8 123, in workgroups of 512 threads that hold 32 149 (one
-// workgroup, 8 wavefronts, per compute unit).  2000 rows of 32003 in bfloat16 with 256 ids, the loss alone, 42 us (3.1 TB/s): bound by its
+// workgroup, 8 wavefronts, per compute unit).  2000 rows of 128256 in bfloat16, gradient included, 242 us (1.03 GB, 4.2 TB/s).  2000 rows of 32003 in bfloat16 with 256 ids, the loss alone, 42 us (3.1 TB/s): bound by its
 // instructions, 19 per logit, a third of them for the entries and the sums' ends; 256 threads that hold 16 vectors 43.
 // 128 rows of 32000 in bfloat16 13 us: one chain of loads, four barriers and 64-bit exponentials.
 constexpr int kFar = 4;           // vectors of a row that a thread asks for together where it does not hold them
@@ -286,7 +286,7 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
 }
 
 template <typename T, bool kGrad>
-hipError_t launch(const TopDistillArgs& a, hipStream_t stream) {
+hipError_t launch(const TopDistillArgs& a, int n_cu, hipStream_t stream) {
   constexpr int kVec = Vec<T>::kElems;
   const size_t lds = sizeof(uint32_t) * ((size_t)a.in.V / 32 + 2);
   auto go = [&](auto kernel, int threads) {
@@ -297,11 +297,16 @@ hipError_t launch(const TopDistillArgs& a, hipStream_t stream) {
     hipLaunchKernelGGL(kernel, dim3((unsigned)a.in.M), dim3(threads), lds, stream, a);
     return hipGetLastError();
   };
-  // the smallest workgroup that holds the row, else the largest
+  // The smallest workgroup that holds the row.  Beyond 512 threads that is for a row per compute unit (256 rows of 32000 in float32 16.4 us, by
+  // 512 threads 18.8).  More rows: two workgroups of 512 per compute unit wait at barriers in turn, and a row's second reading is a cache's
+  // (2000 of 33706 in bfloat16 74 us, held by 1024 threads 110; of 32000 in float32 99 and 123).  Longer rows too (2000 of 128256 in bfloat16
+  // 242 us, by 1024 threads 336), but for float32 that the caches no longer keep (128256: 479 and 433; 72971: 269 and 267), and where the bitmap leaves
+  // a compute unit one workgroup (512 of 1000000 in bfloat16 639 and 583).  The loss alone takes the same, so that it has the same bits.
   if (a.in.V <= 256 * 4 * kVec) return go(top_distill_kernel<T, 256, 4, kGrad, true>, 256);
   if (a.in.V <= 512 * 8 * kVec) return go(top_distill_kernel<T, 512, 8, kGrad, true>, 512);
-  if (a.in.V <= 1024 * 8 * kVec) return go(top_distill_kernel<T, 1024, 8, kGrad, true>, 1024);
-  return go(top_distill_kernel<T, 1024, 12, kGrad, false>, 1024);   // (the loss alone holds as many: it has the same bits)
+  if (a.in.V <= 1024 * 8 * kVec && a.in.M <= n_cu) return go(top_distill_kernel<T, 1024, 8, kGrad, true>, 1024);
+  if (a.in.V <= (sizeof(T) == 4 ? 80 << 10 : 512 << 10)) return go(top_distill_kernel<T, 512, 8, kGrad, false>, 512);
+  return go(top_distill_kernel<T, 1024, 12, kGrad, false>, 1024);
 }
 
 int run(const char* who, const ot_ctx* ctx, const ot_top_distill_in* in, float* loss, float* kept, const float* grad_loss, void* grad, int64_t ld_grad, bool with_grad) {
@@ -327,8 +332,8 @@ int run(const char* who, const ot_ctx* ctx, const ot_top_distill_in* in, float* 
   if (!grid_fits(in->M, 1024)) return ot_fail(OT_ERR_SHAPE, "%s: %d rows are too many for a launch", who, in->M);
   if (const int bad = ot_check_device(ctx, who)) return bad;
   const TopDistillArgs a{*in, ctx->tmap, ctx->V_t, loss, kept, grad_loss, grad, ld_grad};
-  const hipError_t e = in->dtype == OT_BF16 ? (with_grad ? launch<uint16_t, true>(a, ctx->stream) : launch<uint16_t, false>(a, ctx->stream))
-                                            : (with_grad ? launch<float, true>(a, ctx->stream) : launch<float, false>(a, ctx->stream));
+  const hipError_t e = in->dtype == OT_BF16 ? (with_grad ? launch<uint16_t, true>(a, ctx->n_cu, ctx->stream) : launch<uint16_t, false>(a, ctx->n_cu, ctx->stream))
+                                            : (with_grad ? launch<float, true>(a, ctx->n_cu, ctx->stream) : launch<float, false>(a, ctx->n_cu, ctx->stream));
   return e == hipSuccess ? OT_OK : ot_fail_hip(e, who);
 }
 

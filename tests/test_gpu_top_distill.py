@@ -128,6 +128,15 @@ def test_numbers_of_rows(v, M, V):
 
 
 @pytest.mark.parametrize("rest", RESTS)
+@pytest.mark.parametrize("V,dtype", [(16385, torch.float32), (32767, torch.float32), (32769, torch.bfloat16), (50257, torch.bfloat16)])
+def test_more_long_rows_than_compute_units(v, V, dtype, rest):
+    """Other workgroups than for a few such rows."""
+    rng = np.random.default_rng(V)
+    z, ids, lps = _case(rng, 300, V, 12, dtype)
+    _check(v, z, ids, lps, 0.5 + rng.random(300), rest, rng.standard_normal(300).astype(np.float32))
+
+
+@pytest.mark.parametrize("rest", RESTS)
 @pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16])
 @pytest.mark.parametrize("V", [50, 9000, 70001])
 def test_masks_and_special_values(v, V, dtype, rest):
