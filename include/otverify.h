@@ -409,7 +409,8 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
  * probability of the ids that are kept:
  *   OT_REST_DROP         loss = sum p_i (ln p_i - ln q(id_i)):  the kept terms of the teacher's KL divergence
  *   OT_REST_RENORMALISE  the same with p_i / P
- *   OT_REST_BUCKET       + (1 - P) (ln(1 - P) - ln(1 - Q)):  what is not kept as one token more (P above 1 by rounding counts as 1)
+ *   OT_REST_BUCKET       + (1 - P) (ln(1 - P) - ln(1 - Q)):  what is not kept as one token more; no such term where P is above 1 (by
+ *                        rounding, or by ids that are named twice)
  *   - An id of -1 is none, and so is with through_map a target id without a draft id.  A row without ids adds nothing: loss 0, kept 0,
  *     zero gradient, whatever its logits.  An id outside [-1, V) (through_map: [-1, V_t)) makes loss, kept and gradient of its row NaN.
  *   - An id that is named twice has both terms (and counts once in Q).
@@ -442,7 +443,7 @@ typedef struct ot_top_distill_in {
 /* loss: DEVICE [M].  kept: DEVICE [M] or NULL: P of each row.                                                       */
 int ot_top_distill_loss(ot_ctx* ctx, const ot_top_distill_in* in, float* loss, float* kept_or_null);
 /* The same values, and the gradient of sum grad_loss * loss with respect to the student's logits, in their type:
- *   dz_v = (grad_loss / T) (P q_v - sum of the p_i of v)      OT_REST_BUCKET: q_v - (p_i of v) for kept ids,
+ *   dz_v = (grad_loss / T) (P q_v - sum of the p_i of v)      OT_REST_BUCKET with P below 1: q_v - (p_i of v) for kept ids,
  *                                                             q_v (1 - (1 - P) / (1 - Q)) for the others.
  * grad_loss: DEVICE [M], or NULL: 1.  grad: DEVICE, row m at grad + m * ld_grad elements, ld_grad >= V, written whole up to V; it may
  * be the logits themselves (with the same ld), or share no byte with their rows.                                    */

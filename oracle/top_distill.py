@@ -60,7 +60,8 @@ def top_distill(Z, top_ids, top_logprobs, T=None, rest=DROP, grad_loss=None, tma
                 if left > 0:
                     loss[m] += left * (np.log(left) - (top + np.log(inside.sum()) - lnS if top > -np.inf else -np.inf))
                 back = left * inside / (inside.sum() if top > -np.inf else 1)
-                d, parts = q - own - back, q + own + back
+                mass = max(F(1), P)
+                d, parts = mass * q - own - back, mass * q + own + back
             else:
                 mass = P if rest == DROP else F(P > 0)
                 d, parts = mass * q - own, mass * q + own

@@ -2,7 +2,7 @@
 //
 // With p_i the teacher's probabilities of the ids K that are kept, P their sum (1 where they are renormalised), q = softmax(z / T):
 //   loss = sum p_i (ln p_i - ln q_i)                dz_v = (P q_v - p_v) / T
-//   bucket: + (1 - P) ln((1 - P) / (1 - Q))         dz_v = (q_v - p_v) / T in K, q_v (1 - (1 - P) / (1 - Q)) / T elsewhere.
+//   bucket: + (1 - P) ln((1 - P) / (1 - Q))         dz_v = (q_v - p_v) / T in K, q_v (1 - (1 - P) / (1 - Q)) / T elsewhere; P >= 1: as without.
 // The sums over the kept ids and over the others are held apart, each with its own largest logit: 1 - Q and q_v - p_v then keep their
 // digits where the student is sure.
 #include <math.h>
@@ -236,7 +236,8 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
       if (a.kept) a.kept[row] = broken ? kNan : (float)P;
       if (kGrad) {
         const double scaled = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;
-        const double mass = in.rest == OT_REST_BUCKET ? 1.0 : in.rest == OT_REST_RENORMALISE ? (P > 0.0 ? 1.0 : 0.0) : P;   // in front of q_v
+        // in front of q_v: what the terms of the loss add up to, in OT_REST_BUCKET more than 1 where P is
+        const double mass = in.rest == OT_REST_RENORMALISE ? (P > 0.0 ? 1.0 : 0.0) : left > 0.0 ? 1.0 : P;
         double factor = down == 0.0 ? 0.0 : scaled * mass * down / S;
         if (left > 0.0 && S_rest > 0.0) factor -= scaled * left / S_rest;
         s_coef.rest = nothing ? 0.f : broken || isnan(S) ? kNan : (float)factor;
