@@ -411,6 +411,9 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
  *   OT_REST_RENORMALISE  the same with p_i / P
  *   OT_REST_BUCKET       + (1 - P) (ln(1 - P) - ln(1 - Q)):  what is not kept as one token more; no such term where P is above 1 (by
  *                        rounding, or by ids that are named twice)
+ *                        Where the student gives its other ids no probability in 64 bits (masked, or none are left), 1 - P of up to 2^-20 is the
+ *                        rounding of the log-probabilities and counts as 0; a larger one has no place, and makes the loss +inf (or as
+ *                        large as a finite mask makes it).
  *   - An id of -1 is none, and so is with through_map a target id without a draft id.  A row without ids adds nothing: loss 0, kept 0,
  *     zero gradient, whatever its logits.  An id outside [-1, V) (through_map: [-1, V_t)) makes loss, kept and gradient of its row NaN.
  *   - An id that is named twice has both terms (and counts once in Q).

@@ -2,7 +2,8 @@
 
 Readings: an id of -1, or a target id without a draft id, is none; rows without ids add nothing; an id outside the vocabulary, a NaN or +inf
 among a row's kept log-probabilities or its logits makes loss and gradient NaN; a row that the student masks whole adds nothing; ids at -inf
-get no gradient; temperatures as in oracle/logprobs.py.
+get no gradient; temperatures as in oracle/logprobs.py; where a student's other ids have no probability in 64 bits, a remainder of up to 2^-20 is
+the rounding of the log-probabilities and counts as 0.
 """
 from __future__ import annotations
 
@@ -56,11 +57,13 @@ def top_distill(Z, top_ids, top_logprobs, T=None, rest=DROP, grad_loss=None, tma
                 left = max(F(0), 1 - P)
                 others = np.where(ids, -np.inf, (z - z.max()) / t)
                 top = others.max()
+                if left <= F(2) ** -20 and np.exp(np.float64(top)) == 0:
+                    left = F(0)
                 inside = np.where(others > -np.inf, np.exp(others - (top if top > -np.inf else 0)), 0)
                 if left > 0:
                     loss[m] += left * (np.log(left) - (top + np.log(inside.sum()) - lnS if top > -np.inf else -np.inf))
                 back = left * inside / (inside.sum() if top > -np.inf else 1)
-                mass = max(F(1), P)
+                mass = F(1) if left > 0 else P
                 d, parts = mass * q - own - back, mass * q + own + back
             else:
                 mass = P if rest == DROP else F(P > 0)

@@ -36,6 +36,9 @@ struct TopDistillArgs {
 // 128 rows of 32000 in bfloat16 13 us: one chain of loads, four barriers and 64-bit exponentials.
 constexpr int kFar = 4;           // vectors of a row that a thread asks for together where it does not hold them
 constexpr int kEntryWaves = OT_MAX_TEACHER_TOP / 64;
+// 1 - P that rounding can leave of log-probabilities that add up to 1: each is off by 2^-24 of itself, so P by 2^-24 of their entropy, at most
+// ln 256, and what formed them had sums of its own to round.
+constexpr double kNoRemainder = 0x1p-20;
 struct RowCoef {
   double q, p;              // a kept id's gradient: q exp((z - top) / T) - p (its probability with the teacher)
   float rest;               // of exp((z - mx) / T), mx the others' largest logit, in the others' gradients
@@ -224,8 +227,10 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
     const double S_rest = wave_sum(lane < kWaves ? s_sum[lane] : 0.0);
     const double shift = ((double)mx - ref_top) / temp;  // (-inf: there are no others)
     const double down = mx == -INFINITY && !isnan(S_rest) ? 0.0 : exp(shift);
-    const double S = ((s_E[0] + s_E[1]) + (s_E[2] + s_E[3])) + S_rest * down;
-    const double left = in.rest == OT_REST_BUCKET && P < 1.0 ? 1.0 - P : 0.0;
+    const double S_others = S_rest * down, S = ((s_E[0] + s_E[1]) + (s_E[2] + s_E[3])) + S_others;
+    // Where the others have no probability at all, what the sum of rounded probabilities lacks of 1 has no place to go, and is none.
+    double left = in.rest == OT_REST_BUCKET && P < 1.0 ? 1.0 - P : 0.0;
+    if (S_others == 0.0 && left <= kNoRemainder) left = 0.0;
     const bool nothing = S == 0.0 && top == -INFINITY && !broken;       // masked whole
     const double lnS = log(S);
     double loss = norm > 0.0 ? ((s_L[0] + s_L[1]) + (s_L[2] + s_L[3]) + P * (lnS - log(norm))) / norm : 0.0;
