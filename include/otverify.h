@@ -408,7 +408,7 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
  * of them), and a student's logits z with q = softmax(z / T).  With p_i = exp(top_logprobs_i), P = sum p_i, and Q = the student's
  * probability of the ids that are kept:
  *   OT_REST_DROP         loss = sum p_i (ln p_i - ln q(id_i)):  the kept terms of the teacher's KL divergence
- *   OT_REST_RENORMALISE  the same with p_i / P
+ *   OT_REST_RENORMALISE  the same with p_i / P (also where 64 bits hold none of the p_i)
  *   OT_REST_BUCKET       + (1 - P) (ln(1 - P) - ln(1 - Q)):  what is not kept as one token more; no such term where P is above 1 (by
  *                        rounding, or by ids that are named twice)
  *                        Where the student gives its other ids no probability in 64 bits (masked, or none are left), 1 - P of up to 2^-20 is the

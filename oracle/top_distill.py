@@ -45,14 +45,16 @@ def top_distill(Z, top_ids, top_logprobs, T=None, rest=DROP, grad_loss=None, tma
             lnS = np.log(e.sum())
             lq = (z - z.max()) / t - lnS
             q = np.exp(lq)
-            norm = P if rest == RENORMALISE else F(1)
+            shift = max(lp for _, lp in pairs) if rest == RENORMALISE else F(0)      # (p / P is that of any common factor)
+            shift = shift if shift > -np.inf else F(0)
+            norm = sum(np.exp(lp - shift) for _, lp in pairs) if rest == RENORMALISE else F(1)
             own = np.zeros(V, F)
             ids = np.zeros(V, bool)
             for v, lp in pairs:
                 ids[v] = True
-                if np.exp(lp) > 0 and norm > 0:
-                    loss[m] += np.exp(lp) / norm * (lp - np.log(norm) - lq[v])
-                    own[v] += np.exp(lp) / norm
+                if np.exp(lp - shift) > 0 and norm > 0:
+                    loss[m] += np.exp(lp - shift) / norm * (lp - shift - np.log(norm) - lq[v])
+                    own[v] += np.exp(lp - shift) / norm
             if rest == BUCKET:
                 left = max(F(0), 1 - P)
                 others = np.where(ids, -np.inf, (z - z.max()) / t)
@@ -66,7 +68,7 @@ def top_distill(Z, top_ids, top_logprobs, T=None, rest=DROP, grad_loss=None, tma
                 mass = F(1) if left > 0 else P
                 d, parts = mass * q - own - back, mass * q + own + back
             else:
-                mass = P if rest == DROP else F(P > 0)
+                mass = P if rest == DROP else F(norm > 0)
                 d, parts = mass * q - own, mass * q + own
             d[z == -np.inf] = 0
             grad[m], size[m] = d * g / t, np.abs(parts * g / t)

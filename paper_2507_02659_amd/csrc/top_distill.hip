@@ -39,6 +39,7 @@ constexpr int kEntryWaves = OT_MAX_TEACHER_TOP / 64;
 // 1 - P that rounding can leave of log-probabilities that add up to 1: each is off by 2^-24 of itself, so P by 2^-24 of their entropy, at most
 // ln 256, and what formed them had sums of its own to round.
 constexpr double kNoRemainder = 0x1p-20;
+constexpr float kImprobable = -600.f;
 struct RowCoef {
   double q, p;              // a kept id's gradient: q exp((z - top) / T) - p (its probability with the teacher)
   float rest;               // of exp((z - mx) / T), mx the others' largest logit, in the others' gradients
@@ -92,7 +93,20 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
   float zk = -INFINITY;
   if (id >= 0) zk = Vec<T>::one(z + id);
   const bool broken = __syncthreads_or(wrong);           // (the bitmap is clear from here on)
-  if (!__syncthreads_or(id >= 0) && !broken) {           // no ids: the row's logits do not matter
+  // Renormalised probabilities may all be below what 64 bits hold (a low temperature's, behind ids without a draft id): theirs are then taken
+  // relative to the largest, whose logarithm is subtracted from all (exactly, from any within a factor of two of it; the others are below
+  // exp(-600) of it).  What the row keeps is 0 in float32.
+  const bool renormalise = in.rest == OT_REST_RENORMALISE;
+  const bool some = __syncthreads_or(id >= 0 && (!renormalise || lp > kImprobable)) || broken;
+  const bool improbable = renormalise && !some && __syncthreads_or(id >= 0);
+  if (improbable) {
+    if (tid < in.n_top) s_p[tid] = id >= 0 ? (double)lp : -INFINITY;
+    __syncthreads();
+    float largest = -INFINITY;
+    for (int i = 0; i < in.n_top; ++i) largest = fmaxf(largest, (float)s_p[i]);
+    __syncthreads();
+    if (largest > -INFINITY) lp -= largest;
+  } else if (!some) {                                    // no ids: the row's logits do not matter
     if (tid == 0) {
       a.loss[row] = 0.f;
       if (a.kept) a.kept[row] = 0.f;
@@ -238,7 +252,7 @@ __global__ __launch_bounds__(kThreads, kGrad || !kWhole ? 4 : 8) void top_distil
     if (nothing) loss = 0.0;
     if (lane == 0) {
       a.loss[row] = broken || isnan(S) ? kNan : (float)loss;   // (S: also where no p is above 0)
-      if (a.kept) a.kept[row] = broken ? kNan : (float)P;
+      if (a.kept) a.kept[row] = broken ? kNan : improbable ? 0.f : (float)P;
       if (kGrad) {
         const double scaled = (a.grad_loss ? (double)a.grad_loss[row] : 1.0) / temp;
         // in front of q_v: what the terms of the loss add up to, in OT_REST_BUCKET more than 1 where P is
