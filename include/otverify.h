@@ -295,7 +295,7 @@ int ot_distill_loss_grad(ot_ctx* ctx, const ot_step_in* in, const ot_step_out* s
  *   - Ids masked with -inf have probability 0 and are no alternatives; places of top_ids that remain free hold -1 (top_logprobs -inf).
  *   - A row without any logit above -inf has no distribution: logprob -inf, entropy 0, no alternatives, zero gradients.
  *   - A row that holds a NaN or +inf: logprob and entropy NaN, no alternatives, NaN gradients.
- *   - A temperature that is not above 0 (a greedy sequence) counts as 1, one below 2^-126 as that.
+ *   - A temperature that is not above 0 (a greedy sequence) counts as 1, one below 2^-126 as that, +inf as the largest float.
  *   - A token of -1 is none: logprob 0, no gradient.  A token outside [-1, V): logprob NaN, no gradient.
  *   - given_rows_only != 0: rows all of whose tokens are -1 are not read (entropy 0, no alternatives, zero gradients).
  * Work is enqueued on the context's stream; calls on one context share its workspace.  The logits may be any on the context's
@@ -420,7 +420,7 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
  *   - A log-probability of -inf is one of p = 0 and adds no term.  NaN or +inf make the row's loss, kept and gradient NaN.
  *   - An id that the student masks (-inf) gets a zero gradient; with p above 0 the row's loss is +inf.  A row that the student masks
  *     whole adds nothing.  A NaN or +inf among a row's logits makes its loss and gradient NaN.
- *   - temperature is the student's, as in ot_token_logprobs: not above 0 counts as 1, below 2^-126 as that.
+ *   - temperature is the student's, as in ot_token_logprobs: not above 0 counts as 1, below 2^-126 as that, +inf as the largest float.
  * Work is enqueued on the context's stream.                                                                     */
 #define OT_MAX_TEACHER_TOP 256
 #define OT_MAX_STUDENT_V (1 << 20)

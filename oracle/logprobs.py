@@ -1,12 +1,14 @@
 """Oracle of token log-probabilities, entropy and alternatives of rows of logits, and of their gradient: NumPy float64.
 
 Readings: ids at -inf have probability 0 and are no alternatives; a row without any other id has no distribution (logprob -inf, entropy
-0); one with a NaN or +inf gives NaN; temperatures that are not above 0 count as 1, those below 2^-126 as that; a token of -1 is none (logprob 0), one outside [-1, V)
-gives NaN; of equal logits the lowest id comes first.
+0); one with a NaN or +inf gives NaN; temperatures that are not above 0 count as 1, those below 2^-126 as that, +inf as the largest
+float32; a token of -1 is none (logprob 0), one outside [-1, V) gives NaN; of equal logits the lowest id comes first.
 """
 from __future__ import annotations
 
 import numpy as np
+
+LARGEST = float(np.finfo(np.float32).max)
 
 
 def token_logprobs(Z, tokens, T, n_top: int = 0, given_rows_only: bool = False) -> dict:
@@ -16,7 +18,7 @@ def token_logprobs(Z, tokens, T, n_top: int = 0, given_rows_only: bool = False) 
     out = {"logprob": np.zeros(tokens.shape), "entropy": np.zeros(M), "row_max": np.full(M, -np.inf), "row_sumexp": np.zeros(M),
            "top_ids": np.full((M, n_top), -1, np.int64), "top_logprobs": np.full((M, n_top), -np.inf), "lp": np.full((M, V), -np.inf)}
     for m in range(M):
-        z, t = Z[m], max(float(T[m]), 2.0 ** -126) if T[m] > 0 else 1.0
+        z, t = Z[m], min(max(float(T[m]), 2.0 ** -126), LARGEST) if T[m] > 0 else 1.0
         given = [(i, int(v)) for i, v in enumerate(tokens[m]) if v != -1]
         for i, v in given:
             if not 0 <= v < V:
@@ -65,7 +67,7 @@ def token_logprobs_grad(Z, tokens, T, grad_logprob=None, grad_entropy=None, give
         if np.isnan(fwd["row_sumexp"][m]):
             grad[m] = np.nan
             continue
-        t = max(float(T[m]), 2.0 ** -126) if T[m] > 0 else 1.0
+        t = min(max(float(T[m]), 2.0 ** -126), LARGEST) if T[m] > 0 else 1.0
         lp = fwd["lp"][m]
         p = np.exp(lp)
         G = 0.0

@@ -19,7 +19,7 @@ def top_distill(Z, top_ids, top_logprobs, T=None, rest=DROP, grad_loss=None, tma
     M, V = Z.shape
     loss, kept, grad, size = np.zeros(M, F), np.zeros(M, F), np.zeros((M, V), F), np.zeros((M, V), F)
     for m in range(M):
-        t = 1.0 if T is None or not T[m] > 0 else max(F(T[m]), F(2) ** -126)
+        t = 1.0 if T is None or not T[m] > 0 else min(max(F(T[m]), F(2) ** -126), F(np.finfo(np.float32).max))
         g = F(1) if grad_loss is None else F(grad_loss[m])
         pairs, broken = [], False
         for v, lp in zip(top_ids[m], top_logprobs[m]):

@@ -8,11 +8,12 @@ namespace otv {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr float kNan = __builtin_nanf("");
 
-// Temperature of a row, of which log2(e) / T is finite: one per row, or per sequence of row_off.  By a whole wavefront.
+// Temperature of a row, of which log2(e) / T is finite and above 0 (else a masked id's distance of -inf gave NaN): one per row, or per sequence
+// of row_off.  By a whole wavefront.
 __device__ inline float row_temperature(const float* temperature, const int32_t* row_off, int B, int row, int lane) {
   if (!temperature) return 1.f;
   const float T = temperature[row_off ? find_sequence(row_off, B, row, 0, lane) : row];
-  return T > 0.f ? fmaxf(T, 0x1p-126f) : 1.f;
+  return T > 0.f ? fminf(fmaxf(T, 0x1p-126f), 0x1.fffffep127f) : 1.f;
 }
 
 template <typename T> struct Vec;
