@@ -135,7 +135,8 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
 #pragma unroll
         for (int w = 0; w < kDownWaves; ++w) all += (double)s_part[w][tid];
         const float scale = in.scale ? in.scale[rows.now] : 1.f;
-        const float u = (float)(all * (double)scale);
+        float u = (float)(all * (double)scale);
+        if (!isfinite(u)) u = kNan;                      // (else 0 * inf or a sign would decide what becomes of the row)
         const int l = tid >> 2, rank = r0 + (l >> 4) * 4 + (tid & 3), i = q + (l & 15);
         const int at = block * 64 + rows.row(i);         // (whole wavefronts come here)
         if (i < rows.n) {
