@@ -142,7 +142,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
         if (i < rows.n) {
           if constexpr (sizeof(W) == 2) {                // three parts, whose sum is u
             uint16_t* to = reinterpret_cast<uint16_t*>(a.u) + (int64_t)at * 3 * a.depth + rank;
-            const float hi = (float)(__bf16)u, mid = (float)(__bf16)(u - hi);
+            float hi = (float)(__bf16)u;                 // (from 255.5 2^120 on the nearest is infinite: the largest, and the rest in the others)
+            if (isinf(hi)) hi = copysignf(0x1.fep127f, hi);
+            const float mid = (float)(__bf16)(u - hi);
             store_one(to, hi);
             store_one(to + a.depth, mid);
             store_one(to + 2 * a.depth, u - hi - mid);

@@ -1,4 +1,4 @@
-"""Inner sums of adapters that are not finite: the row is NaN, whatever the type and the rank."""
+"""Inner sums of adapters that are not finite, and those next to the largest float: the row is NaN, or whole, whatever the type and the rank."""
 import numpy as np
 import pytest
 import torch
@@ -47,3 +47,24 @@ def test_rows_of_infinite_inner_sums_are_nan(v, dtype, R, logits_type):
     got = v.adapter_logits(hidden[6:], Adapters(down, up, torch.tensor([3e38, 1.0], device=DEV)), at[6:], z[6:])
     big = (hidden[7:].double() @ down[0].double().t()).abs().amax(1) * 3e38 > 3.5e38
     assert big.all() and got[1:].isnan().all() and not got[0].isnan().any()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float32])
+def test_the_largest_inner_sums(v, dtype):
+    """24 significant bits below 2^128, from three bytes each: float32 holds them, the nearest bfloat16 may be infinite."""
+    from paper_2507_02659_amd.runner import Adapters
+    rng = np.random.default_rng(5)
+    whole = np.concatenate(([2 ** 24 - 1, 0xFF8000, 0xFF7FFF, 0xFF0001], rng.integers(0xFF0000, 2 ** 24, 20))).astype(np.int64)
+    M, d = whole.size, 32
+    hidden = np.zeros((M, d))
+    for k in range(3):
+        hidden[:, k] = ((whole >> (8 * k)) & 255) * 256.0 ** k * 2.0 ** 104
+    hidden[1::2] *= -1
+    down, up = torch.zeros(1, 16, d), torch.zeros(1, 50, 16)
+    down[0, 2, :3] = 1.0
+    up[0, 13, 2], up[0, 14, 2] = 1.0, 0.5
+    a = Adapters(down.to(dtype).to(DEV), up.to(dtype).to(DEV))
+    got = v.adapter_logits(torch.from_numpy(hidden).to(dtype).to(DEV), a, torch.zeros(M, dtype=torch.int32, device=DEV)).cpu().numpy()
+    want = (hidden.sum(1)).astype(np.float32)
+    assert np.isfinite(want).all() and np.array_equal(got[:, 13], want) and np.array_equal(got[:, 14], want * np.float32(0.5))
+    assert (got[:, :13] == 0).all() and (got[:, 15:] == 0).all()
