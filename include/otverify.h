@@ -379,7 +379,7 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
 #define OT_MAX_BIAS    4096            /* entries of a sequence's bias list at most (longer bans: masks)             */
 #define OT_MAX_HISTORY (1 << 29)       /* ids of a sequence's history at most                                       */
 typedef struct ot_adjust_in {
-  int32_t         M, V, B;            /* rows; ids per row; sequences                                              */
+  int32_t         M, V, B;            /* rows, with a window 2^29 at most; ids per row; sequences                     */
   int32_t         dtype;              /* OT_BF16 or OT_F32: type of logits and out                                  */
   int32_t         n_bias, n_masks;    /* entries of a sequence's bias list; masks                                   */
   int32_t         reserved[2];        /* must be 0                                                              */

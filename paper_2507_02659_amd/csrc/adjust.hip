@@ -21,7 +21,8 @@ struct AdjustArgs {
   int32_t bias_slots;       // of the table of biases: a power of two, at least twice n_bias, or 0
 };
 
-// An id's word in a slice's table: how often it was said, and two flags.
+// An id's word in a slice's table: how often it was said, and two flags.  A history of 2^29 ids and a window of 2^29 rows, of which the last has
+// 2^29 - 1 tokens in front, stay below the flags.
 constexpr uint32_t kSeen = 0x80000000u;     // it occurs in the prompt
 constexpr uint32_t kBiased = 0x40000000u;   // the bias list names it
 constexpr uint32_t kNoKey = 0xFFFFFFFFu;
@@ -141,7 +142,7 @@ __global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
     if (!mine(id)) continue;
     const uint32_t o = (uint32_t)(id - s0);
     uint32_t at = slot_of(o);
-    for (;;) {                                           // (half of the slots stay free: it ends)
+    for (int tries = 0; tries < a.bias_slots; ++tries) { // (half of the slots stay free: it ends before)
       const uint32_t key = atomicCAS(&s_key[at], kNoKey, o);
       if (key == kNoKey || key == o) break;
       at = (at + 1) & (uint32_t)(a.bias_slots - 1);
@@ -163,7 +164,7 @@ __global__ __launch_bounds__(kThreads, 8) void adjust_kernel(AdjustArgs a) {
     }
     if (c & kBiased) {
       uint32_t at = slot_of((uint32_t)o);
-      while (s_key[at] != (uint32_t)o) at = (at + 1) & (uint32_t)(a.bias_slots - 1);
+      for (int tries = 0; tries < a.bias_slots && s_key[at] != (uint32_t)o; ++tries) at = (at + 1) & (uint32_t)(a.bias_slots - 1);
       x += (double)in.bias[(int64_t)b * in.n_bias + s_entry[at]];
     }
     return (float)x;
@@ -267,6 +268,7 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
   if (in->n_bias < 0 || in->n_bias > OT_MAX_BIAS || in->n_masks < 0 || in->ld_history < 0 || in->ld_history > OT_MAX_HISTORY || (in->masks && in->ld_mask < ceil_div(in->V, 32)))
     return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: need 0 <= n_bias <= %d, n_masks >= 0, 0 <= ld_history <= 2^29, ld_mask >= ceil(V / 32)", OT_MAX_BIAS);
   if (in->window && !in->row_off) return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: a window needs row_off");
+  if (in->window && in->M > OT_MAX_HISTORY) return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: with a window, at most 2^29 rows (M = %d)", in->M);
   if (in->masks && !in->mask_of_row && in->n_masks < in->M)
     return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: without mask_of_row every row has its own mask (n_masks = %d, M = %d)", in->n_masks, in->M);
   if (in->M == 0 || in->B == 0) return OT_OK;
