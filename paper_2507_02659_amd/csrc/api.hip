@@ -40,11 +40,12 @@ int ot_check_device(const ot_ctx* ctx, const char* who) {
 }
 
 bool ot_rows_overlap(const void* from_rows, int64_t ld_from, const void* to_rows, int64_t ld_to, int64_t M, int64_t V, int64_t size) {
-  const int64_t row = V * size, step = ld_from * size;
-  const uintptr_t from = reinterpret_cast<uintptr_t>(from_rows), to = reinterpret_cast<uintptr_t>(to_rows);
-  if (to == from || to >= from + (uintptr_t)((M - 1) * step + row) || from >= to + (uintptr_t)((M - 1) * ld_to * size + row)) return false;
+  typedef __int128 wide;                                 // (distances up to 2^63 elements are nobody's memory, but may be asked for)
+  const wide row = V * size, step = (wide)ld_from * size;
+  const wide from = reinterpret_cast<uintptr_t>(from_rows), to = reinterpret_cast<uintptr_t>(to_rows);
+  if (to == from || to >= from + (M - 1) * step + row || from >= to + (M - 1) * ((wide)ld_to * size) + row) return false;
   if (ld_to != ld_from) return true;
-  const int64_t apart = (int64_t)(to > from ? (to - from) % (uintptr_t)step : step - (int64_t)((from - to) % (uintptr_t)step));
+  const wide apart = to > from ? (to - from) % step : step - (from - to) % step;
   return apart < row || apart > step - row;              // (a row's end, and the next row's start)
 }
 
