@@ -372,7 +372,8 @@ int ot_adapter_logits(ot_ctx* ctx, const ot_adapter_in* in, void* out, int64_t l
  *      z = z - frequency[b] * n - (n > 0 ? presence[b] : 0);
  *   3. z = z + bias of v (of an id that the list names more than once the last entry counts);
  *   4. the row's mask leaves v out: z = -inf.
- * An id at -inf stays there.  What nothing of this names keeps its bits.  A mask that leaves no id makes a row without a distribution.
+ * An id at -inf stays there.  What nothing of this names keeps its bits; of bfloat16 logits, a NaN next to an id that is named may become
+ * another NaN.  A mask that leaves no id makes a row without a distribution.
  * Ids outside [0, V) in history, window and bias lists are none (so -1 pads them).  A mask_of_row outside [-1, n_masks) makes the
  * row NaN.  Penalties are finite, repetition above 0.
  * Without row_off every row is a sequence of its own (B = M).  Rows that no sequence of row_off has are neither read nor written.    */
