@@ -325,7 +325,12 @@ hipError_t launch(const TopDistillArgs& a, int n_cu, hipStream_t stream) {
   if (a.in.V <= 256 * 4 * kVec) return go(top_distill_kernel<T, 256, 4, kGrad, true>, 256);
   if (a.in.V <= 512 * 8 * kVec) return go(top_distill_kernel<T, 512, 8, kGrad, true>, 512);
   if (a.in.V <= 1024 * 8 * kVec && a.in.M <= n_cu) return go(top_distill_kernel<T, 1024, 8, kGrad, true>, 1024);
-  if (a.in.V <= (sizeof(T) == 4 ? 80 << 10 : 512 << 10)) return go(top_distill_kernel<T, 512, 8, kGrad, false>, 512);
+  // Few rows have no second workgroup to wait beside, and take 1024 threads that hold more of the row: in float32 up to a row for two compute units
+  // (1, 64, 128 rows of 72971 17.7, 21.0, 23.9 us, by 512 threads 22.1, 25.4, 29.1; of 33003 12.7, 14.2, 14.9 and 13.4, 15.0, 16.7, but their
+  // loss alone 9.7, 11.0, 11.3 and 9.8, 10.0, 10.5; for 256 rows 36.8 and 37.3, their loss alone 20.2 and 18.2); in bfloat16 up to a row each
+  // where it is long (300000 ids: 51, 59, 90 us for 1, 64, 256 rows and 57, 67, 93; but 152064: 30, 35, 51 and 33, 36, 44).
+  const bool few = sizeof(T) == 4 ? a.in.M <= n_cu / 2 : a.in.M <= n_cu && a.in.V > 192 << 10;
+  if (!few && a.in.V <= (sizeof(T) == 4 ? 80 << 10 : 512 << 10)) return go(top_distill_kernel<T, 512, 8, kGrad, false>, 512);
   return go(top_distill_kernel<T, 1024, 12, kGrad, false>, 1024);
 }
 
