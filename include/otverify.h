@@ -338,11 +338,12 @@ int ot_token_logprobs_grad(ot_ctx* ctx, const ot_logprob_in* in, const ot_logpro
  * the adapter of its own request, in one call, beside the projection that they share.
  *   - adapter[m] = -1: the row has none, out[m] = logits[m].  Outside [-1, n_adapters): the row is NaN.
  *   - Both matrices lie as linear layers keep them, [outputs, inputs].  Adapters of a lower rank are padded with zeros.
- *   - Sums are fp32; the inner one enters the outer one whole (OT_BF16: as three bfloat16 parts).  A row whose inner sum is not
- *     finite is NaN.
+ *   - Sums are fp32; the inner one, times the scale, enters the outer one whole (OT_BF16: as three bfloat16 parts).  A row where that
+ *     is not finite for some r is NaN.
  *   - Rows of one adapter that lie within 64 rows of each other share what is read of it: keep a request's rows together.
- * Work is enqueued on the context's stream; calls on one context share its workspace.  Any head's logits may be given: the target's
- * (ot_lm_head), the drafter's or another model's.                                                                 */
+ * Work is enqueued on the context's stream; calls on one context share its workspace (3 MB, allocated with the context whether adapters are
+ * used or not: a call that allocated could not be captured).  Any head's logits may be given: the target's (ot_lm_head), the drafter's or
+ * another model's.                                                                                              */
 #define OT_MAX_ADAPTER_RANK 256
 typedef struct ot_adapter_in {
   int32_t        M, d, V;             /* rows; hidden size, up to 2^24 (OT_BF16: a multiple of 8); ids per row, up to 2^30 */
@@ -393,7 +394,11 @@ typedef struct ot_adjust_in {
   const int32_t*  n_history;          /* DEVICE [B] their lengths, or NULL: ld_history                              */
   const int32_t*  n_prompt;           /* DEVICE [B] how many of these are the prompt's, or NULL: 0                  */
   const int32_t*  window;             /* DEVICE [M] proposed tokens in the layout of ot_step_out.mapped_ids: entry row_off[b] + j is
-                                         sequence b's j-th; NULL: none.  Needs row_off                              */
+                                         sequence b's j-th; NULL: none.  Needs row_off.  Target ids: a drafter with the
+                                         target's vocabulary has them at hand; of another vocabulary only a step
+                                         (ot_verify_step) translates them, so a call in front of the step that they are
+                                         for needs one on the plain logits first, or leaves the window out and counts
+                                         its tokens once they are history                                       */
   const float    *repetition, *frequency, *presence;   /* DEVICE [B], or NULL: 1, 0, 0                              */
   const int32_t*  bias_ids;           /* DEVICE [B, n_bias]                                                     */
   const float*    bias;               /* DEVICE [B, n_bias]; -inf bans an id                                        */

@@ -6,7 +6,8 @@
 //
 // Rounding: products of bfloat16 are exact, sums fp32.  u is rounded to float32 and, as an operand of bfloat16 instructions, split into three
 // parts that hold all of its 24 bits; with the nearest bfloat16 alone the sums would be off by 2^-9, a thousand times their own rounding.  The
-// two instructions more per product cost nothing beside the logits (without any products 2000 rows take 97 us of 100).
+// two parts more cost nothing where the logits' bytes do not wait for instructions (144 rows of 128256 ids, rank 16: 38 us, with one part alone
+// 37.5) and a quarter where they do (2000 rows of 32003 in bfloat16, rank 64: 94 us and 72).
 #include <math.h>
 
 #include <algorithm>
@@ -93,8 +94,9 @@ struct Block {
 
 // Grid = slots x 16s of the rank x blocks of 64 rows.  A workgroup takes every slots-th tile of its block; its 16 wavefronts share the hidden
 // indices and add their sums in LDS, in one order.  3.5 us with one row of 1024 indices, 11.4 with 144 of 4096 (rank 16), 13.4 with 2000 of 2056 (rank
-// 64): behind a launch that left many logits to write it waits for the memory (with every load from a cached line the times are the same).  Indices
-// split over four workgroups, whose sums the last one adds, took 10.0 and 16.4; eight steps of loads ahead instead of four changed nothing.
+// 64), as long with nothing in front of it (3.4, 11.2 and 13.6 in a row of such launches alone) and with every load from a cached line: it is bound
+// by its own chain, the adapters' numbers, the loads behind them, the sums through LDS.  Float32 matrices 19.5 instead of 11.4.  Indices split over
+// four workgroups, whose sums the last one adds, took 10.0 and 16.4; eight steps of loads ahead instead of four changed nothing.
 constexpr int kDownWaves = 16, kDownSteps = 4;
 template <typename W>
 __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterArgs a, int slots) {
@@ -163,7 +165,9 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
 // vectors that begin in its kStride ids, and computes the kVec - 1 ids more that the last of them may reach.  In LDS a row is shifted so that
 // its vectors are whole there too.  The next tile's logits are on their way while one is taken.
 // 144 rows of 128256 ids, rank 16, 37 us (208 MB: 5.6 TB/s, a copy's rate); 2000 rows of 32003 in bfloat16, rank 64, 93 us (2.7 TB/s): there a tile's
-// instructions are as long as its bytes (the matrix ones 0.6 us, the others 1.4, LDS 0.5 of 4.7 us that two workgroups' tiles take).  Each lane
+// instructions come on top of its bytes: with one of the three parts 72 us, with rows that all start at 16 bytes (32256 ids) 91.  Ranks 33 to 64
+// of bfloat16 matrices spill 4 to 12 registers, those above 64 leave a compute unit one workgroup: 144 rows of 128256, rank 16, 64, 128 and 256,
+// 38, 89, 128 and 231 us (208, 386, 623 and 1098 MB: 5.5, 4.3, 4.9, 4.8 TB/s); float32 matrices of rank 16, 64, 128 51, 127, 235.  Each lane
 // storing its own four ids without LDS took 48 and 216 us, strips of 64 ids per wavefront 62 and 134, of 256 per workgroup 50 and 127.  Strips follow
 // each other in memory: with the blocks of a strip on one XCD after the other 68 us instead of 50.
 constexpr int kUpWaves = 8, kStrip = 64 * kUpWaves, kFront = 8;

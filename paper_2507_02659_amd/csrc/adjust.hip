@@ -39,7 +39,8 @@ __device__ inline uint32_t bits_at(uint32_t lo, uint32_t hi, int at) { return __
 // way while the table is built.
 // Values are formed in 64 bits and rounded to float32 and the logits' type: only marked ids are, a few thousand of a row.
 // Bound by memory where histories are short: 144 rows of 128256 float32 logits behind histories of 2000 ids 29 us (149 MB, 5.1 TB/s: a copy's rate).
-// 64 rows of 152064 behind 24576 ids each 32 us (2.6 TB/s): every slice's workgroup reads the whole history.  With up to 64 registers eight wavefronts
+// 64 rows of 152064 behind 24576 ids each 33 us (2.6 TB/s), without a history 18: every slice's workgroup reads the whole history, and 640
+// workgroups of which 512 are there at once take a second round (131072 ids, 512 workgroups: 25 us).  With up to 64 registers eight wavefronts
 // are on a SIMD (144 rows: 43 us with 98 registers and rows asked for ahead); slices of 16 ids per thread, since a smaller one reads the history more
 // often and a larger table leaves room for one workgroup per compute unit.
 template <typename T, int kThreads, bool kInPlace>

@@ -363,9 +363,11 @@ class Verifier:
 
         row_off: int32 [B + 1] first rows of the sequences (None: every row is one).  history: int32 [B, L], the first n_history of a row count
         (int32 [B]; None: all) and of these the first n_prompt are its prompt (int32 [B]; None: none).  window: int32 [M] proposed tokens (a step's
-        mapped_ids), those in front of a row count for it.  repetition, frequency, presence: float32 [B].  bias_ids, bias: int32 and float32 [B, n].
+        mapped_ids: target ids, which for a drafter of another vocabulary only a step gives), those in front of a row count for it.  repetition,
+        frequency, presence: float32 [B].  bias_ids, bias: int32 and float32 [B, n].
         masks: int32 [n, words], bit v % 32 of word v / 32 set where id v may come; mask_of_row: int32 [M], -1: none (None: row m has mask m).
-        Ids outside the vocabulary are none.  out: where to (None: new; the logits themselves: in place)."""
+        Ids outside the vocabulary are none.  out: where to (None: new; the logits themselves: in place); rows of no sequence are not written there,
+        so a new one holds anything in them."""
         code, M, V, ld = self._rows("logits", logits)
         B = M if row_off is None else max(0, row_off.numel() - 1)
         out, ld_out = self._out(out, (M, V), logits.dtype)
