@@ -396,9 +396,9 @@ typedef struct ot_adjust_in {
   const int32_t*  window;             /* DEVICE [M] proposed tokens in the layout of ot_step_out.mapped_ids: entry row_off[b] + j is
                                          sequence b's j-th; NULL: none.  Needs row_off.  Target ids: a drafter with the
                                          target's vocabulary has them at hand; of another vocabulary only a step
-                                         (ot_verify_step) translates them, so a call in front of the step that they are
-                                         for needs one on the plain logits first, or leaves the window out and counts
-                                         its tokens once they are history                                       */
+                                         translates them, so a call in front of the step that they are for needs one
+                                         on the plain logits first (ot_verify_step_from_logits; the cache counts its
+                                         uses too), or leaves the window out and counts its tokens as history later */
   const float    *repetition, *frequency, *presence;   /* DEVICE [B], or NULL: 1, 0, 0                              */
   const int32_t*  bias_ids;           /* DEVICE [B, n_bias]                                                     */
   const float*    bias;               /* DEVICE [B, n_bias]; -inf bans an id                                        */
