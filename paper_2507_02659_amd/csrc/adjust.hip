@@ -247,6 +247,10 @@ hipError_t launch(const AdjustArgs& a, hipStream_t stream) {
 }
 
 constexpr int kFewIds = 8192;       // ids of a history up to which workgroups are small
+// Parts of a sequence with a window at most: each reads the tokens in front of its rows, so that a row a workgroup cost the square of a long window
+// (one of 65536 rows of 1000 ids 1259 us, of 16384 of 32003 in bfloat16 1055; in 256 parts 477 and 580, 1024 212 and 599, 4096 200 and 715, 16384
+// 399 and 1055).
+constexpr int kWindowParts = 2048;
 
 }  // namespace
 }  // namespace otv
@@ -288,6 +292,7 @@ int ot_adjust_logits(ot_ctx* ctx, const ot_adjust_in* in, void* out, int64_t ld_
   // A row a workgroup where the table is quickly made (up to as many workgroups as keep every compute unit busy), else a sequence's rows in parts
   // until there is a workgroup for every compute unit (512 rows of 32003: 31 us a row a workgroup, 40 four rows)
   a.parts = (int)std::max<int64_t>(1, std::min<int64_t>(ceil_div(in->M, in->B), threads == 1024 ? ctx->n_cu / groups : (1 << 22) / groups));
+  if (in->window) a.parts = std::min(a.parts, kWindowParts);
   if (in->n_bias > 0)
     for (a.bias_slots = 2; a.bias_slots < 2 * in->n_bias;) a.bias_slots *= 2;
   if (!grid_fits(groups * a.parts, threads)) return ot_fail(OT_ERR_SHAPE, "ot_adjust_logits: %d sequences of %d ids are too many for a launch", in->B, in->V);
