@@ -7,7 +7,7 @@
 // Rounding: products of bfloat16 are exact, sums fp32.  u is rounded to float32 and, as an operand of bfloat16 instructions, split into three
 // parts that hold all of its 24 bits; with the nearest bfloat16 alone the sums would be off by 2^-9, a thousand times their own rounding.  The
 // two parts more cost nothing where the logits' bytes do not wait for instructions (144 rows of 128256 ids, rank 16: 38 us, with one part alone
-// 37.5) and a quarter where they do (2000 rows of 32003 in bfloat16, rank 64: 94 us and 72).
+// 37.5) and a quarter where they do (2000 rows of 32003 in bfloat16, rank 64: 95 us and 72).
 #include <math.h>
 
 #include <algorithm>
@@ -164,7 +164,7 @@ __global__ __launch_bounds__(64 * kDownWaves) void adapter_down_kernel(AdapterAr
 // through LDS to the logits, which a wavefront reads and writes row by row in whole 16-byte vectors, wherever the row starts: a strip has the
 // vectors that begin in its kStride ids, and computes the kVec - 1 ids more that the last of them may reach.  In LDS a row is shifted so that
 // its vectors are whole there too.  The next tile's logits are on their way while one is taken.
-// 144 rows of 128256 ids, rank 16, 37 us (208 MB: 5.6 TB/s, a copy's rate); 2000 rows of 32003 in bfloat16, rank 64, 93 us (2.7 TB/s): there a tile's
+// 144 rows of 128256 ids, rank 16, 38 us (208 MB: 5.5 TB/s, a copy's rate); 2000 rows of 32003 in bfloat16, rank 64, 95 us (2.7 TB/s): there a tile's
 // instructions come on top of its bytes: with one of the three parts 72 us, with rows that all start at 16 bytes (32256 ids) 91.  Ranks 33 to 64
 // of bfloat16 matrices spill 4 to 12 registers, those above 64 leave a compute unit one workgroup: 144 rows of 128256, rank 16, 64, 128 and 256,
 // 38, 89, 128 and 231 us (208, 386, 623 and 1098 MB: 5.5, 4.3, 4.9, 4.8 TB/s); float32 matrices of rank 16, 64, 128 51, 127, 235.  Each lane

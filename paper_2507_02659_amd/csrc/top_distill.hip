@@ -29,7 +29,7 @@ struct TopDistillArgs {
 // gradient and reads what is beyond them again.  The kept ids, one a thread of the first four wavefronts, are taken in 64 bits; where they lie
 // among the others a bitmap in LDS says, by which the held vectors have -inf in their places.  The others' sum is one of float32 exponentials of
 // their distance to their largest, added in 64 bits.
-// 512 rows of 128256 float32 logits with 50 ids, gradient included, 116 to 119 us (525 MB, 4.5 TB/s; a copy of the logits takes 99): bound by memory,
+// 512 rows of 128256 float32 logits with 50 ids, gradient included, 114 to 116 us (525 MB, 4.6 TB/s; a copy of the logits takes 99): bound by memory,
 // and by the 60 % of a row that is read again, from a cache.  16 vectors held 119 to 133 us, 8 123, in workgroups of 512 threads that hold 32 149 (one
 // workgroup, 8 wavefronts, per compute unit).  2000 rows of 128256 in bfloat16, gradient included, 242 us (1.03 GB, 4.2 TB/s).  2000 rows of 32003 in bfloat16 with 256 ids, the loss alone, 42 us (3.1 TB/s): bound by its
 // instructions, 19 per logit, a third of them for the entries and the sums' ends; 256 threads that hold 16 vectors 43.
